@@ -209,6 +209,89 @@ int paged_decode_attention_ext(const void* q, const void* k_cache, const void* v
                                float scale, void* stream);
 
 /*
+ * paged_decode_attention_sink -- paged_decode_attention_ext with a few first
+ * tokens that stay visible under the sliding window [library interface]: the
+ * query at position p sees the keys t <= p with t > p - window or
+ * t < num_sinks.
+ *   window        as for paged_decode_attention_ext; 0 (no window) makes every
+ *                 key visible, whatever num_sinks is.
+ *   num_sinks     >= 0; 0 is paged_decode_attention_ext.
+ * A page none of whose tokens any query of the sequence sees -- wholly past
+ * the sinks and wholly before the window -- is never read and may have been
+ * released (any block_table entry).  The calls run on the matrix cores with
+ * the merge kernel, whatever PDA_OPT_COMPUTE_PATH and PDA_OPT_FUSED_MERGE say.
+ * Everything else is as for paged_decode_attention_ext;
+ * pda_workspace_reserve covers these calls.
+ */
+int paged_decode_attention_sink(const void* q, const void* k_cache, const void* v_cache,
+                                const int32_t* block_table, const int32_t* context_lens, void* out,
+                                int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                int32_t head_dim, int32_t page_size, int32_t num_pages,
+                                int32_t max_pages_per_seq, int32_t num_queries, int32_t window,
+                                int32_t num_sinks, float scale, void* stream);
+
+/*
+ * A cache held in 4 bits [library interface]: 17/64 of the bf16 cache's bytes.
+ * A token's key (or value) of one kv head is head_dim / 32 groups of 32
+ * consecutive elements; a group has a scale byte s and 32 codes, and stands for
+ *     element = code * 2^(s - 127)          (s = 255: NaN)
+ * with 4-bit codes of a sign (bit 3), two exponent bits and one mantissa bit:
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (the E2M1 elements and E8M0
+ * scales of the OCP microscaling formats).
+ *   k_codes, v_codes    uint8 [num_pages, num_kv_heads, head_dim / 32, page_size, 16],
+ *                       16-byte aligned; byte i of a group holds element 2 i in
+ *                       its low four bits and element 2 i + 1 in its high ones.
+ *   k_scales, v_scales  uint8 [num_pages, num_kv_heads, head_dim / 32, page_size].
+ * page_size is a power of two from 16 to 1024; block_table and context_lens are
+ * those of the bf16 cache.
+ *
+ * pda_kv4_append -- quantise the last num_tokens tokens of each sequence into
+ * their page slots:
+ *   k_new, v_new  bf16 [batch, num_tokens, num_kv_heads, head_dim], 16-B aligned;
+ *                 the lengths count them and token j of sequence b lands at
+ *                 position L_b - num_tokens + j; positions below 0 write nothing.
+ *   num_tokens    1 .. 1048576, num_tokens * num_kv_heads * head_dim at most 2^30.
+ * A group's scale is s = max(E - 2, 0), E the largest biased bf16 exponent
+ * among its elements, so its largest element lies in [4, 8) units of
+ * 2^(s - 127); elements are rounded to the nearest code, ties to the even one,
+ * and those past 6 units become 6.  A group with an infinity or a NaN gets
+ * s = 255.  Only the slots of these tokens change.
+ *
+ * pda_kv4_read -- the last num_tokens tokens of each sequence as the bf16
+ * values they stand for (exact: a code times a power of two; only the scales
+ * 253 and 254, which pda_kv4_append never writes, reach past bf16's range, to
+ * infinities), as chunked prefill attends to them: k_out, v_out bf16 [batch, num_tokens, num_kv_heads,
+ * head_dim]; positions below 0 give zeros.
+ *
+ * Both: asynchronous on `stream`, no workspace, no allocation.
+ */
+int pda_kv4_append(const void* k_new, const void* v_new, void* k_codes, void* k_scales, void* v_codes, void* v_scales,
+                   const int32_t* block_table, const int32_t* context_lens, int32_t batch, int32_t num_tokens,
+                   int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
+                   int32_t max_pages_per_seq, void* stream);
+int pda_kv4_read(void* k_out, void* v_out, const void* k_codes, const void* k_scales, const void* v_codes,
+                 const void* v_scales, const int32_t* block_table, const int32_t* context_lens, int32_t batch,
+                 int32_t num_tokens, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
+                 int32_t max_pages_per_seq, void* stream);
+
+/*
+ * paged_decode_attention_kv4 -- paged_decode_attention_sink over a cache held
+ * in 4 bits: the same queries, key ranges (window 0: none; num_sinks 0: none),
+ * released pages and output, on the values that the codes and scales stand
+ * for.  The arithmetic is that of paged_decode_attention (keys and values are
+ * exact in bf16).  Workspace per (device, stream), shared with the other
+ * calls; pda_kv4_workspace_reserve grows it for any num_queries, window and
+ * num_sinks of these sizes, as pda_workspace_reserve does for the bf16 calls.
+ */
+int paged_decode_attention_kv4(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
+                               const void* v_scales, const int32_t* block_table, const int32_t* context_lens, void* out,
+                               int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                               int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, int32_t num_queries,
+                               int32_t window, int32_t num_sinks, float scale, void* stream);
+int pda_kv4_workspace_reserve(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                              int32_t page_size, int32_t max_pages_per_seq, void* stream);
+
+/*
  * pda_kv_append -- write each sequence's newest key and value into its page:
  * the step before attention in the paper's decode loop (Method, "Kernel
  * Customization and Multi-Request Adaptation": a small scatter kernel writes

@@ -113,6 +113,15 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.paged_decode_attention_desc.restype = ctypes.c_int
     lib.paged_decode_attention_ext.argtypes = [vp] * 6 + [i32] * 9 + [f32, vp]
     lib.paged_decode_attention_ext.restype = ctypes.c_int
+    lib.paged_decode_attention_sink.argtypes = [vp] * 6 + [i32] * 10 + [f32, vp]
+    lib.paged_decode_attention_sink.restype = ctypes.c_int
+    lib.paged_decode_attention_kv4.argtypes = [vp] * 8 + [i32] * 10 + [f32, vp]
+    lib.paged_decode_attention_kv4.restype = ctypes.c_int
+    for fn in (lib.pda_kv4_append, lib.pda_kv4_read):
+        fn.argtypes = [vp] * 8 + [i32] * 7 + [vp]
+        fn.restype = ctypes.c_int
+    lib.pda_kv4_workspace_reserve.argtypes = [i32] * 6 + [vp]
+    lib.pda_kv4_workspace_reserve.restype = ctypes.c_int
     dims_p = ctypes.POINTER(PreludeDims)
     lib.pda_pack_weights.argtypes = [vp, vp, i32, i32, vp]
     lib.pda_pack_weights.restype = ctypes.c_int
@@ -467,6 +476,87 @@ def paged_decode_attention_ext(q, k_cache, v_cache, block_table, context_lens, o
         out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"], sz["N"], sz["M"], sz["T"], int(window),
         ctypes.c_float(float(scale)), _stream_ptr(stream)))
     return out
+
+
+def paged_decode_attention_sink(q, k_cache, v_cache, block_table, context_lens, out, scale, window=0, sinks=0,
+                                stream=None):
+    """:func:`paged_decode_attention_ext` with first tokens that stay visible
+    under the window: the query at position p sees the keys t <= p with
+    t > p - ``window`` or t < ``sinks`` (``window`` 0: every key)."""
+    import torch
+    sz = _validate([("q", q, torch.bfloat16, "B T Hq D"), *_cache_specs(k_cache, v_cache, block_table, context_lens),
+                    ("out", out, torch.bfloat16, "B T Hq D")])
+    _check(load().paged_decode_attention_sink(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
+        out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"], sz["N"], sz["M"], sz["T"], int(window), int(sinks),
+        ctypes.c_float(float(scale)), _stream_ptr(stream, q.get_device())))
+    return out
+
+
+KV4_GROUP = 32  # elements of a 4-bit cache's row that share a scale
+
+
+def kv4_cache(num_pages, page_size, num_kv_heads, head_dim, device="cuda"):
+    """Zeroed (codes, scales) of one 4-bit pool: uint8 [N, Hkv, D / 32, P, 16] and [N, Hkv, D / 32, P]."""
+    import torch
+    shape = (num_pages, num_kv_heads, head_dim // KV4_GROUP, page_size)
+    return (torch.zeros((*shape, KV4_GROUP // 2), dtype=torch.uint8, device=device),
+            torch.zeros(shape, dtype=torch.uint8, device=device))
+
+
+def _kv4_specs(k_codes, k_scales, v_codes, v_scales, block_table, context_lens):
+    import torch
+    u8, i32 = torch.uint8, torch.int32
+    return [("k_codes", k_codes, u8, "N Hkv S P 16"), ("k_scales", k_scales, u8, "N Hkv S P"),
+            ("v_codes", v_codes, u8, "N Hkv S P 16"), ("v_scales", v_scales, u8, "N Hkv S P"),
+            ("block_table", block_table, i32, "B M"), ("context_lens", context_lens, i32, "B")]
+
+
+def _kv4_groups(sz):
+    if sz["D"] != KV4_GROUP * sz["S"]:
+        raise ValueError(f"head_dim {sz['D']} needs {sz['D'] / KV4_GROUP:g} groups a row, the cache has {sz['S']}")
+
+
+def _kv4_tokens(call, k, v, names, cache, stream):
+    import torch
+    sz = _validate([(names[0], k, torch.bfloat16, "B T Hkv D"), (names[1], v, torch.bfloat16, "B T Hkv D"), *_kv4_specs(*cache)])
+    _kv4_groups(sz)
+    _check(call(k.data_ptr(), v.data_ptr(), *(t.data_ptr() for t in cache), sz["B"], sz["T"], sz["Hkv"], sz["D"], sz["P"],
+                sz["N"], sz["M"], _stream_ptr(stream, k.get_device())))
+
+
+def kv4_append(k_new, v_new, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, stream=None):
+    """Quantise T new tokens per sequence (k_new, v_new bf16 [B, T, Hkv, D]) into their page slots of a
+    4-bit cache, at positions context_lens[b] - T + j (the lengths count them).
+
+    k_codes, v_codes: uint8 [N, Hkv, D / 32, P, 16]; k_scales, v_scales: uint8 [N, Hkv, D / 32, P]
+    (:func:`kv4_cache`); include/pda.h states the format."""
+    _kv4_tokens(load().pda_kv4_append, k_new, v_new, ("k_new", "v_new"),
+                (k_codes, k_scales, v_codes, v_scales, block_table, context_lens), stream)
+
+
+def kv4_read(k_out, v_out, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, stream=None):
+    """The last T tokens of each sequence as the bf16 values they stand for -> k_out, v_out
+    [B, T, Hkv, D]; positions before a sequence's first token give zeros."""
+    _kv4_tokens(load().pda_kv4_read, k_out, v_out, ("k_out", "v_out"),
+                (k_codes, k_scales, v_codes, v_scales, block_table, context_lens), stream)
+
+
+def paged_decode_attention_kv4(q, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, out, scale, window=0,
+                               sinks=0, stream=None):
+    """:func:`paged_decode_attention_sink` over a 4-bit cache (:func:`kv4_append`): q, out bf16 [B, T, Hq, D]."""
+    import torch
+    cache = (k_codes, k_scales, v_codes, v_scales, block_table, context_lens)
+    sz = _validate([("q", q, torch.bfloat16, "B T Hq D"), *_kv4_specs(*cache), ("out", out, torch.bfloat16, "B T Hq D")])
+    _kv4_groups(sz)
+    _check(load().paged_decode_attention_kv4(
+        q.data_ptr(), *(t.data_ptr() for t in cache), out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"],
+        sz["N"], sz["M"], sz["T"], int(window), int(sinks), ctypes.c_float(float(scale)), _stream_ptr(stream, q.get_device())))
+    return out
+
+
+def kv4_workspace_reserve(batch, hq, hkv, d, page_size, max_pages, stream=None) -> None:
+    _check(load().pda_kv4_workspace_reserve(batch, hq, hkv, d, page_size, max_pages, _stream_ptr(stream)))
 
 
 def kv_append(k_new, v_new, k_cache, v_cache, block_table, context_lens, stream=None):

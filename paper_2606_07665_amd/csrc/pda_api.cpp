@@ -22,6 +22,7 @@
 #include "pda_probe.h"
 #include "pda_gemv.h"
 #include "pda_internal.h"
+#include "pda_kv4.h"
 
 namespace {
 
@@ -192,16 +193,26 @@ int heads_per_group(int hkv, int max_waves) {
   return 1;
 }
 
+// What the planner has to know of the kernel that a plan is for.
+struct Form {
+  int max_waves;        // waves of a workgroup at most
+  int per_cu;           // workgroups of a compute unit that run together
+  int64_t token_bytes;  // K and V of a token and kv head
+  bool options;         // the compute path and the fused merge apply
+};
+Form bf16_form(int d, bool sinks = false) { return {pda::max_waves(d), 1, static_cast<int64_t>(d) * 4, !sinks}; }
+Form kv4_form(int d) { return {pda::kv4_max_waves(d), pda::kKv4WorkgroupsPerCu, static_cast<int64_t>(d) * 17 / 16, false}; }
+
 // Workgroups: one wave per kv head of a group of hgs, times step phases up
-// to max_waves(d) waves (8; 4 at D = 256); as many workgroups as fill the
+// to max_waves waves (8; 4 at D = 256); as many workgroups as fill the
 // device (blocks_per_cu per CU), but none with fewer than min_steps 32-token
 // steps per wave when every sequence has steps_seq steps.  Partial
 // slots: one per (workgroup, sequence piece), at most grid + batch * kv-head
 // groups, each holding `cols` (query token, head) rows per kv head.
-Plan plan_for(int hgs, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols,
-              int min_steps) {
+Plan plan_for(const Form& form, int hgs, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus,
+              int cols, int min_steps) {
   Plan pl;
-  const int max_waves = pda::max_waves(d);
+  const int max_waves = form.max_waves;
   pl.hgs = hgs;
   pl.min_steps = min_steps;
   const int phases = max_waves / pl.hgs;
@@ -210,7 +221,7 @@ Plan plan_for(int hgs, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq,
   const int64_t steps_max = static_cast<int64_t>(batch) * ngroups * steps_seq;
   const int64_t per_block = static_cast<int64_t>(min_steps) * phases;
   int64_t blocks = (steps_max + per_block - 1) / per_block;
-  const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu();
+  const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu;
   if (blocks > target) blocks = target;
   if (blocks < 1) blocks = 1;
   pl.grid = static_cast<int>(blocks);
@@ -225,11 +236,13 @@ Plan plan_for(int hgs, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq,
 }
 
 // Most 32-token steps a sequence can have: what the page table holds, or with
-// a sliding window the steps that window + num_queries - 1 tokens touch.
-int64_t most_steps(int32_t p, int32_t maxp, int num_queries, int window) {
+// a sliding window the steps that window + num_queries - 1 tokens touch, and
+// those of the sinks.
+int64_t most_steps(int32_t p, int32_t maxp, int num_queries, int window, int sinks = 0) {
   const int64_t table = (static_cast<int64_t>(maxp) * p + pda::kStep - 1) / pda::kStep;
   if (window <= 0) return table;
-  const int64_t seen = (static_cast<int64_t>(window) + num_queries - 1 + pda::kStep - 1) / pda::kStep + 1;
+  const int64_t seen = (static_cast<int64_t>(window) + num_queries - 1 + pda::kStep - 1) / pda::kStep + 1 +
+                       (static_cast<int64_t>(sinks) + pda::kStep - 1) / pda::kStep;
   return std::min(table, seen);
 }
 
@@ -243,12 +256,13 @@ int64_t most_steps(int32_t p, int32_t maxp, int num_queries, int window) {
 // a plan with grid 0 where it does not apply: more pairs than half the
 // device's workgroups (the stream-K split balances those better).  One
 // partial slot per workgroup.
-Plan plan_fixed(const Plan& base, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols) {
+Plan plan_fixed(const Form& form, const Plan& base, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus,
+                int cols) {
   Plan pl = base;
   pl.grid = 0;
   const int phases = pl.waves / pl.hgs;
   const int64_t seqs = static_cast<int64_t>(batch) * (hkv / pl.hgs);
-  const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu();
+  const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu;
   const int64_t per_block = static_cast<int64_t>(pl.min_steps) * phases;
   if (base.grid < 1 || 2 * seqs > target) return pl;
   int64_t chunks = 1;
@@ -291,7 +305,7 @@ constexpr int64_t kSmallCallBytes = int64_t{128} << 20;
 constexpr int64_t kSmallCallPieces = 32;
 constexpr int kDefaultMinSteps = 2;
 
-Plan make_split_plan(int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols) {
+Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols) {
   const int cap = kv_group_cap();
   const int ms_opt = min_steps_option();
   // A split piece leaves a partial of cols x head_dim fp32 per kv head it
@@ -299,9 +313,9 @@ Plan make_split_plan(int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, i
   // cost more than the longer token rows save, so at most 4 kv heads go
   // together (multiq: 191.4 -> 188.3 us per call; long70b and ragged, at 8
   // columns or fewer, run slower with 4).
-  const int dflt_most = cols > 8 ? std::min(4, pda::max_waves(d)) : pda::max_waves(d);
-  const int most = cap > 0 && cap < pda::max_waves(d) ? cap : dflt_most;
-  Plan dflt = plan_for(heads_per_group(hkv, most), batch, hkv, d, steps_seq, num_cus, cols,
+  const int dflt_most = cols > 8 ? std::min(4, form.max_waves) : form.max_waves;
+  const int most = cap > 0 && cap < form.max_waves ? cap : dflt_most;
+  Plan dflt = plan_for(form, heads_per_group(hkv, most), batch, hkv, d, steps_seq, num_cus, cols,
                        ms_opt > 0 ? ms_opt : kDefaultMinSteps);
   // Small calls (each 32-token step's K and V is a few KB; the whole call
   // is a chain of latencies):
@@ -321,32 +335,32 @@ Plan make_split_plan(int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, i
   //    first K/V loads leave ~2 us earlier and the merge needs no prefix
   //    (1 x 4096 tokens, 32:8 heads, cold K/V: attention kernel 14.8 ->
   //    11.4 us by events, 16.7 -> 11.9 us per call replayed from a graph).
-  const int64_t kv_bytes = static_cast<int64_t>(batch) * steps_seq * pda::kStep * hkv * d * 4;
+  const int64_t kv_bytes = static_cast<int64_t>(batch) * steps_seq * pda::kStep * hkv * form.token_bytes;
   const bool small = kv_bytes <= kSmallCallBytes;
   if (small) {
-    if (ms_opt == 0 && dflt.grid > 1 && dflt.grid < static_cast<int64_t>(num_cus) * blocks_per_cu())
-      dflt = plan_for(dflt.hgs, batch, hkv, d, steps_seq, num_cus, cols, 1);
+    if (ms_opt == 0 && dflt.grid > 1 && dflt.grid < static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu)
+      dflt = plan_for(form, dflt.hgs, batch, hkv, d, steps_seq, num_cus, cols, 1);
     if (cap == 0) {
       for (int h = dflt.hgs; h >= 1; --h) {
         if (hkv % h) continue;
         if (h == 1 || static_cast<int64_t>(dflt.grid) * h <= kSmallCallPieces * batch * hkv) {
-          if (h != dflt.hgs) dflt = plan_for(h, batch, hkv, d, steps_seq, num_cus, cols, dflt.min_steps);
+          if (h != dflt.hgs) dflt = plan_for(form, h, batch, hkv, d, steps_seq, num_cus, cols, dflt.min_steps);
           break;
         }
       }
     }
   }
   // (the vector-ALU variant, a measurement aid, keeps the merge kernel)
-  if (dflt.grid == 1 || !fused_merge() || compute_path() != 0) {
-    if (small && fixed_split() && compute_path() == 0) {
-      const Plan f = plan_fixed(dflt, batch, hkv, d, steps_seq, num_cus, cols);
+  if (dflt.grid == 1 || !form.options || !fused_merge() || compute_path() != 0) {
+    if (small && fixed_split() && (!form.options || compute_path() == 0)) {
+      const Plan f = plan_fixed(form, dflt, batch, hkv, d, steps_seq, num_cus, cols);
       if (f.grid > 0) return f;
     }
     return dflt;
   }
   // a latency-bound call keeps the fixed split, merged in the kernel
   if (small && fixed_split()) {
-    Plan f = plan_fixed(dflt, batch, hkv, d, steps_seq, num_cus, cols);
+    Plan f = plan_fixed(form, dflt, batch, hkv, d, steps_seq, num_cus, cols);
     if (f.grid > 1 && f.chunks > 1 && f.grid <= pda::kMaxFusedGrid) {
       f.fused = true;
       return f;
@@ -359,7 +373,7 @@ Plan make_split_plan(int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, i
   }
   for (int h = dflt.hgs; h >= 1; --h) {
     if (hkv % h) continue;
-    Plan c = plan_for(h, batch, hkv, d, steps_seq, num_cus, cols, dflt.min_steps);
+    Plan c = plan_for(form, h, batch, hkv, d, steps_seq, num_cus, cols, dflt.min_steps);
     const int64_t most_bytes = static_cast<int64_t>(c.grid) * h * cols * d * 4;
     if (c.grid > 1 && c.grid <= pda::kMaxFusedGrid && most_bytes <= pda::kFusedMergeBytes &&
         c.bytes < (int64_t{1} << 31)) {
@@ -383,15 +397,15 @@ Plan make_split_plan(int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, i
 // x 64 19.9 -> 14.7; 32:2 heads, 128 x 64 17.9 -> 7.8, 256 x 256 22.3 ->
 // 15.9.  With longer sequences a few long ones among short ones would cost
 // more whole.
-Plan plan_whole(const Plan& split, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus) {
+Plan plan_whole(const Form& form, const Plan& split, int32_t batch, int32_t hkv, int64_t steps_seq, int num_cus) {
   Plan pl = split;
   pl.grid = 0;
-  const int max_waves = pda::max_waves(d);
+  const int max_waves = form.max_waves;
   const bool streamed = 2 * static_cast<int64_t>(batch) * (hkv / heads_per_group(hkv, max_waves)) > num_cus;
   const int64_t most_kb = streamed ? 300 : 150;
   for (int h = 1; h <= max_waves; ++h) {
     if (hkv % h || static_cast<int64_t>(batch) * (hkv / h) > num_cus) continue;
-    if (steps_seq * pda::kStep * h * d * 4 > most_kb * 1024) break;
+    if (steps_seq * pda::kStep * h * form.token_bytes > most_kb * 1024) break;
     pl.hgs = h;
     pl.waves = h * (max_waves / h);
     pl.grid = static_cast<int>(static_cast<int64_t>(batch) * (hkv / h));
@@ -405,12 +419,12 @@ Plan plan_whole(const Plan& split, int32_t batch, int32_t hkv, int32_t d, int64_
 
 // The plan of a call: the split plan, or whole sequences where that is
 // faster, unless an option asks for a particular split.
-Plan make_plan(int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols) {
-  const Plan split = make_split_plan(batch, hkv, d, steps_seq, num_cus, cols);
-  if (split.chunks == 1 || !fixed_split() || compute_path() != 0 || fused_merge() || kv_group_cap() ||
+Plan make_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols) {
+  const Plan split = make_split_plan(form, batch, hkv, d, steps_seq, num_cus, cols);
+  if (split.chunks == 1 || !fixed_split() || (form.options && (compute_path() != 0 || fused_merge())) || kv_group_cap() ||
       min_steps_option() || blocks_per_cu() != 1)
     return split;
-  const Plan whole = plan_whole(split, batch, hkv, d, steps_seq, num_cus);
+  const Plan whole = plan_whole(form, split, batch, hkv, steps_seq, num_cus);
   return whole.grid > 0 ? whole : split;
 }
 
@@ -420,11 +434,12 @@ Plan make_plan(int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num
 // also under capture.  A plan has at most one workgroup per compute unit and
 // per (sequence, kv head, step), each with one slot of up to max_waves kv
 // heads beside one per (sequence, kv-head group).
-int64_t workspace_bytes(int32_t batch, int32_t hkv, int32_t d, int32_t p, int32_t maxp, int num_cus, int cols) {
-  const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu();
+int64_t workspace_bytes(const Form& form, int32_t batch, int32_t hkv, int32_t d, int32_t p, int32_t maxp, int num_cus,
+                        int cols) {
+  const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu;
   const int64_t pairs = static_cast<int64_t>(batch) * hkv;
   const int64_t steps = pairs * most_steps(p, maxp, 1, 0);
-  const int64_t rows = (std::min(target * pda::max_waves(d), steps) + pairs) * cols;
+  const int64_t rows = (std::min(target * form.max_waves, steps) + pairs) * cols;
   return align256(rows * d * 4) + align256(rows * 2 * 4) + align256((batch + 1 + std::min(target, steps)) * 4);
 }
 
@@ -872,7 +887,53 @@ int run_prelude(const void* x, const void* w_packed, const void* bias, const voi
   return PDA_OK;
 }
 
+int check_kv4_page(int32_t p) {
+  if (p < 16) return fail(PDA_ERR_UNSUPPORTED, "page_size %d (a 4-bit cache: powers of two from 16 to %d)", p, PDA_MAX_PAGE_SIZE);
+  return PDA_OK;
+}
+
+// The checks of an append to a 4-bit cache and of a read from it (k, v: the
+// bf16 side), and the arguments of their kernels.
+int check_kv4_tokens(pda::Kv4Args* c, const void* k, const void* v, const void* k_codes, const void* k_scales,
+                     const void* v_codes, const void* v_scales, const int32_t* block_table, const int32_t* context_lens,
+                     int32_t batch, int32_t num_tokens, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                     int32_t num_pages, int32_t max_pages_per_seq, void* stream) {
+  g_err.clear();
+  int rc = check_shape(batch, num_kv_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq);
+  if (rc || (rc = check_kv4_page(page_size))) return rc;
+  if (num_tokens < 1 || num_tokens > pda::kKv4MaxTokens)
+    return fail(PDA_ERR_SHAPE, "num_tokens must be in [1, %d] (got %d)", pda::kKv4MaxTokens, num_tokens);
+  if (static_cast<int64_t>(num_tokens) * num_kv_heads * head_dim > (int64_t{1} << 30))
+    return fail(PDA_ERR_UNSUPPORTED, "num_tokens * num_kv_heads * head_dim exceeds 2^30");
+  if (num_pages <= 0) return fail(PDA_ERR_SHAPE, "num_pages must be positive (got %d)", num_pages);
+  if (batch == 0) return PDA_OK;
+  if (!k || !v || !k_codes || !k_scales || !v_codes || !v_scales || !block_table || !context_lens)
+    return fail(PDA_ERR_NULL, "a tensor pointer is NULL");
+  if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_codes, 16) || misaligned(v_codes, 16))
+    return fail(PDA_ERR_ALIGN, "keys, values and codes must be 16-byte aligned");
+  if (misaligned(block_table, 4) || misaligned(context_lens, 4))
+    return fail(PDA_ERR_ALIGN, "block_table and context_lens must be 4-byte aligned");
+  if ((rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages,
+                           static_cast<hipStream_t>(stream))))
+    return rc;
+  c->k = static_cast<uint8_t*>(const_cast<void*>(k_codes));
+  c->ks = static_cast<uint8_t*>(const_cast<void*>(k_scales));
+  c->v = static_cast<uint8_t*>(const_cast<void*>(v_codes));
+  c->vs = static_cast<uint8_t*>(const_cast<void*>(v_scales));
+  c->bt = block_table;
+  c->lens = context_lens;
+  c->batch = batch;
+  c->tokens = num_tokens;
+  c->hkv = num_kv_heads;
+  c->head_dim = head_dim;
+  c->page_shift = log2i(page_size);
+  c->num_pages = num_pages;
+  c->maxp = max_pages_per_seq;
+  return PDA_OK;
+}
+
 // The attention entry points: argument checks, plan, workspace, launches.
+// kv4: the caches are its 4-bit ones (k_cache, v_cache: the codes).
 // noalloc: the workspace is the library's fixed per-device scratch (no
 // allocation, no paging validation, no profiling events) instead of the
 // (device, stream) workspace, and shapes whose plan needs more than it
@@ -881,26 +942,29 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
                    const int32_t* context_lens, void* out, int32_t batch, int32_t num_q_heads,
                    int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
                    int32_t max_pages_per_seq, int32_t num_queries, int32_t window, float scale, void* stream,
-                   bool noalloc) {
+                   bool noalloc, int32_t sinks = 0, const pda::Kv4Args* kv4 = nullptr) {
   g_err.clear();
   int rc = check_attention(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq);
   if (rc) return rc;
+  if (kv4 && (rc = check_kv4_page(page_size))) return rc;
   if (num_pages <= 0) return fail(PDA_ERR_SHAPE, "num_pages must be positive (got %d)", num_pages);
   if (num_queries < 1) return fail(PDA_ERR_SHAPE, "num_queries must be >= 1 (got %d)", num_queries);
   if (window < 0) return fail(PDA_ERR_SHAPE, "window must be >= 0 (got %d)", window);
+  if (sinks < 0) return fail(PDA_ERR_SHAPE, "num_sinks must be >= 0 (got %d)", sinks);
+  if (window == 0) sinks = 0;  // every key is visible
   if (num_queries > pda::kMaxCols || num_queries * (num_q_heads / num_kv_heads) > pda::kMaxCols)
     return fail(PDA_ERR_UNSUPPORTED, "num_queries %d x query group %d exceeds %d", num_queries,
                 num_q_heads / num_kv_heads, pda::kMaxCols);
   if (!std::isfinite(scale)) return fail(PDA_ERR_SCALE, "scale is not finite");
   const int cols = num_queries * (num_q_heads / num_kv_heads);
   int valu_cols = 0;
-  if ((rc = check_compute_path(head_dim, page_size, cols, batch, &valu_cols))) return rc;
+  if (!kv4 && !sinks && (rc = check_compute_path(head_dim, page_size, cols, batch, &valu_cols))) return rc;
   if (batch == 0) return PDA_OK;
-  if (!q || !k_cache || !v_cache || !block_table || !context_lens || !out)
+  if (!q || !k_cache || !v_cache || !block_table || !context_lens || !out || (kv4 && (!kv4->ks || !kv4->vs)))
     return fail(PDA_ERR_NULL, "a tensor pointer is NULL");
   auto misaligned = [](const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; };
   if (misaligned(q, 16) || misaligned(k_cache, 16) || misaligned(v_cache, 16) || misaligned(out, 16))
-    return fail(PDA_ERR_ALIGN, "q, k_cache, v_cache and out must be 16-byte aligned");
+    return fail(PDA_ERR_ALIGN, "q, %s and out must be 16-byte aligned", kv4 ? "k_codes, v_codes" : "k_cache, v_cache");
   if (misaligned(block_table, 4) || misaligned(context_lens, 4))
     return fail(PDA_ERR_ALIGN, "block_table and context_lens must be 4-byte aligned");
   if (!noalloc && (rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size,
@@ -912,9 +976,12 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
   if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
   int cus = 0;
   if ((rc = device_cus(dev, &cus))) return rc;
-  const Plan pl = make_plan(batch, num_kv_heads, head_dim,
-                            most_steps(page_size, max_pages_per_seq, num_queries, window), cus, cols);
-  if (pda::attn_lds_bytes(head_dim, batch, pl.waves, valu_cols > 0) > static_cast<size_t>(pda::kMaxLdsBytes))
+  const Form form = kv4 ? kv4_form(head_dim) : bf16_form(head_dim, sinks > 0);
+  const Plan pl = make_plan(form, batch, num_kv_heads, head_dim,
+                            most_steps(page_size, max_pages_per_seq, num_queries, window, sinks), cus, cols);
+  const size_t lds = kv4 ? pda::kv4_attn_lds_bytes(head_dim, batch, pl.waves)
+                         : pda::attn_lds_bytes(head_dim, batch, pl.waves, valu_cols > 0);
+  if (lds > static_cast<size_t>(pda::kMaxLdsBytes))
     return fail(PDA_ERR_UNSUPPORTED, "batch %d needs more LDS than a workgroup has", batch);
   hipStream_t st = static_cast<hipStream_t>(stream);
   void* ws = nullptr;
@@ -929,7 +996,7 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
     if ((e = pda::noalloc_scratch(dev, &ws)) != hipSuccess) return hip_fail(e, "hipGetSymbolAddress(scratch)");
     cnt = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + PDA_NOALLOC_SCRATCH_BYTES - counter_bytes);
   } else {
-    const int64_t most = workspace_bytes(batch, num_kv_heads, head_dim, page_size, max_pages_per_seq, cus, cols);
+    const int64_t most = workspace_bytes(form, batch, num_kv_heads, head_dim, page_size, max_pages_per_seq, cus, cols);
     if ((rc = workspace_for(dev, st, pl.bytes, most, &ws))) return rc;
     if (pl.fused && (rc = counters_for(dev, st, &cnt))) return rc;
   }
@@ -959,20 +1026,22 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
   a.scale = scale;
   a.nq = num_queries;
   a.window = window;
+  a.sinks = sinks;
   a.valu_cols = valu_cols;
   a.ws_cnt = cnt;
   a.fused = pl.fused;
   a.chunks = pl.chunks;
   a.chunk_steps = pl.chunk_steps;
   // the first-piece stash of stream-K plans, where the LDS holds it
-  a.stash = pl.chunks == 0 && !pl.fused && pl.grid > 1 && valu_cols == 0 &&
+  a.stash = !kv4 && pl.chunks == 0 && !pl.fused && pl.grid > 1 && valu_cols == 0 &&
             pda::attn_stash_lds_bytes(head_dim, batch, pl.waves, pl.hgs, cols, valu_cols > 0) <=
                 static_cast<size_t>(pda::kMaxLdsBytes);
 
   const Rec rec = noalloc ? Rec{nullptr, nullptr, nullptr, 0} : prof_begin(0);
   const bool prof = rec.a != nullptr;
   if (prof && (e = hipEventRecord(rec.a, st)) != hipSuccess) return hip_fail(e, "hipEventRecord");
-  if ((e = pda::launch_attn_kernel(a, st)) != hipSuccess) return hip_fail(e, "attention kernel launch");
+  e = kv4 ? pda::launch_kv4_attn(a, *kv4, st) : pda::launch_attn_kernel(a, st);
+  if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
   if (prof && (e = hipEventRecord(rec.b, st)) != hipSuccess) return hip_fail(e, "hipEventRecord");
   // with one workgroup, or one fixed-split chunk per sequence, every piece
   // is a whole sequence: nothing to merge; a fused plan merged in the
@@ -984,6 +1053,29 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
     prof_push(rec);
   }
   return PDA_OK;
+}
+
+// A workspace for every call of these sizes, for the most (query token, head)
+// columns, so any num_queries fits.
+int reserve_attention(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                      int32_t max_pages_per_seq, bool kv4, void* stream) {
+  g_err.clear();
+  int rc = check_attention(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq);
+  if (rc) return rc;
+  if (kv4 && (rc = check_kv4_page(page_size))) return rc;
+  if (batch == 0) return PDA_OK;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  int cus = 0;
+  if ((rc = device_cus(dev, &cus))) return rc;
+  void* ptr = nullptr;
+  const int64_t need = workspace_bytes(kv4 ? kv4_form(head_dim) : bf16_form(head_dim), batch, num_kv_heads, head_dim,
+                                       page_size, max_pages_per_seq, cus, pda::kMaxCols);
+  if ((rc = workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr))) return rc;
+  if (kv4) return PDA_OK;  // (no fused merge, so no counters)
+  int32_t* cnt = nullptr;
+  return counters_for(dev, static_cast<hipStream_t>(stream), &cnt);
 }
 
 }  // namespace
@@ -1002,33 +1094,24 @@ int pda_plan(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t h
   int rc = check_attention(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq);
   if (rc) return rc;
   if (num_cus <= 0) return fail(PDA_ERR_SHAPE, "num_cus must be positive");
-  Plan pl = make_plan(batch, num_kv_heads, head_dim, most_steps(page_size, max_pages_per_seq, 1, 0), num_cus,
+  const Form form = bf16_form(head_dim);
+  Plan pl = make_plan(form, batch, num_kv_heads, head_dim, most_steps(page_size, max_pages_per_seq, 1, 0), num_cus,
                       num_q_heads / num_kv_heads);
   *grid_blocks = batch ? pl.grid : 0;
   *waves = batch ? pl.grid * pl.waves : 0;
   *workspace_size =
-      batch ? workspace_bytes(batch, num_kv_heads, head_dim, page_size, max_pages_per_seq, num_cus, pda::kMaxCols) : 0;
+      batch ? workspace_bytes(form, batch, num_kv_heads, head_dim, page_size, max_pages_per_seq, num_cus, pda::kMaxCols) : 0;
   return PDA_OK;
 }
 
 int pda_workspace_reserve(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                           int32_t page_size, int32_t max_pages_per_seq, void* stream) {
-  g_err.clear();
-  int rc = check_attention(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq);
-  if (rc) return rc;
-  if (batch == 0) return PDA_OK;
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-  int cus = 0;
-  if ((rc = device_cus(dev, &cus))) return rc;
-  // sized for the most (query token, head) columns, so any num_queries fits
-  void* ptr = nullptr;
-  const int64_t need =
-      workspace_bytes(batch, num_kv_heads, head_dim, page_size, max_pages_per_seq, cus, pda::kMaxCols);
-  if ((rc = workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr))) return rc;
-  int32_t* cnt = nullptr;
-  return counters_for(dev, static_cast<hipStream_t>(stream), &cnt);
+  return reserve_attention(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq, false, stream);
+}
+
+int pda_kv4_workspace_reserve(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                              int32_t page_size, int32_t max_pages_per_seq, void* stream) {
+  return reserve_attention(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq, true, stream);
 }
 
 int pda_release_workspaces(void) {
@@ -1486,6 +1569,55 @@ int pda_prelude_workspace_reserve(const pda_prelude_dims* dims, void* stream) {
   void* ptr = nullptr;
   const int64_t need = prelude_ws_bytes(*dims, cus);
   return workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr);
+}
+
+int paged_decode_attention_sink(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
+                                const int32_t* context_lens, void* out, int32_t batch, int32_t num_q_heads,
+                                int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
+                                int32_t max_pages_per_seq, int32_t num_queries, int32_t window, int32_t num_sinks,
+                                float scale, void* stream) {
+  return attention_call(q, k_cache, v_cache, block_table, context_lens, out, batch, num_q_heads, num_kv_heads, head_dim,
+                        page_size, num_pages, max_pages_per_seq, num_queries, window, scale, stream, false, num_sinks);
+}
+
+int paged_decode_attention_kv4(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
+                               const void* v_scales, const int32_t* block_table, const int32_t* context_lens, void* out,
+                               int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                               int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, int32_t num_queries,
+                               int32_t window, int32_t num_sinks, float scale, void* stream) {
+  pda::Kv4Args c = {};
+  c.k = static_cast<uint8_t*>(const_cast<void*>(k_codes));
+  c.ks = static_cast<uint8_t*>(const_cast<void*>(k_scales));
+  c.v = static_cast<uint8_t*>(const_cast<void*>(v_codes));
+  c.vs = static_cast<uint8_t*>(const_cast<void*>(v_scales));
+  return attention_call(q, k_codes, v_codes, block_table, context_lens, out, batch, num_q_heads, num_kv_heads, head_dim,
+                        page_size, num_pages, max_pages_per_seq, num_queries, window, scale, stream, false, num_sinks, &c);
+}
+
+int pda_kv4_append(const void* k_new, const void* v_new, void* k_codes, void* k_scales, void* v_codes, void* v_scales,
+                   const int32_t* block_table, const int32_t* context_lens, int32_t batch, int32_t num_tokens,
+                   int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
+                   int32_t max_pages_per_seq, void* stream) {
+  pda::Kv4Args c;
+  const int rc = check_kv4_tokens(&c, k_new, v_new, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, batch,
+                                  num_tokens, num_kv_heads, head_dim, page_size, num_pages, max_pages_per_seq, stream);
+  if (rc || batch == 0) return rc;
+  const hipError_t e = pda::launch_kv4_append(c, static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new),
+                                              static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PDA_OK : hip_fail(e, "append kernel launch");
+}
+
+int pda_kv4_read(void* k_out, void* v_out, const void* k_codes, const void* k_scales, const void* v_codes,
+                 const void* v_scales, const int32_t* block_table, const int32_t* context_lens, int32_t batch,
+                 int32_t num_tokens, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
+                 int32_t max_pages_per_seq, void* stream) {
+  pda::Kv4Args c;
+  const int rc = check_kv4_tokens(&c, k_out, v_out, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, batch,
+                                  num_tokens, num_kv_heads, head_dim, page_size, num_pages, max_pages_per_seq, stream);
+  if (rc || batch == 0) return rc;
+  const hipError_t e = pda::launch_kv4_read(c, static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out),
+                                            static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PDA_OK : hip_fail(e, "read kernel launch");
 }
 
 }  // extern "C"

@@ -37,6 +37,7 @@ struct LaunchArgs {
   float scale;
   int nq;      // query tokens per sequence (causal among them)
   int window;  // sliding window in tokens, 0 = none
+  int sinks = 0;  // first tokens that stay visible under a window
   int valu_cols = 0;  // 0: products on the matrix cores; 4 or 8: vector-ALU variant for that many columns
   bool fused = false; // split sequences merged by their last workgroup (no merge kernel)
   // > 0: the fixed split of small calls -- workgroup w takes chunk w % chunks

@@ -38,22 +38,10 @@
 
 #include <atomic>
 
+#include "pda_attn.h"
 #include "pda_internal.h"
 
 namespace pda {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-
-constexpr float kLog2e = 1.4426950408889634f;
 
 // kValu: the vector-ALU variant of the step (see attn_kernel), which keeps
 // one register buffer like D = 256 and reads K and V back from LDS row-wise.
@@ -94,8 +82,6 @@ __host__ __device__ constexpr int pref_offset(int waves) {
   return ml_offset<D, kValu>(waves) + waves * 16 * 2 * 4;
 }
 
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
 // Start of the first-piece stash (16-byte aligned) after `bytes` of LDS.
 __host__ __device__ constexpr int stash_offset(int bytes) { return (bytes + 15) & ~15; }
 
@@ -105,53 +91,6 @@ constexpr int kWaitAllVectorLoads = 0x0F70;
 // s_waitcnt vmcnt(n), n < 64: vmcnt is split over bits 3:0 and 15:14.
 constexpr int wait_vector_loads(int n) { return kWaitAllVectorLoads | (n & 15) | ((n >> 4) << 14); }
 constexpr int kIssueK = 1, kIssueV = 2;  // which loads of a step to issue
-
-__device__ __forceinline__ int clamp_len(int L, int max_ctx) {
-  return L < 0 ? 0 : (L > max_ctx ? max_ctx : L);
-}
-
-// Key range of a sequence.  Its nq query tokens are its last nq tokens:
-// query j sits at position L - nq + j and sees keys up to that position, and
-// with a sliding window of W > 0 tokens only the W keys ending there.  The
-// first key any query sees is seq_start; the steps of the sequence are the
-// 32-token steps from the one holding seq_start to the end.
-__device__ __forceinline__ int seq_start(int L, int nq, int window) {
-  if (window <= 0) return 0;
-  const int s = L - nq + 1 - window;
-  return s > 0 ? s : 0;
-}
-
-__device__ __forceinline__ int seq_steps(int L, int nq, int window) {
-  return (L + kStep - 1) / kStep - seq_start(L, nq, window) / kStep;
-}
-
-__device__ __forceinline__ u32x4 ld16(const uint16_t* p) {
-  return *reinterpret_cast<const u32x4*>(p);
-}
-
-// K and V are read exactly once per call, with raw buffer loads:
-//  * non-temporal (cache policy NT): on MI355X a plain streaming read runs at
-//    ~7.1 TB/s this way against ~6.1 TB/s with default loads;
-//  * the descriptor's base is the page (a wave-uniform 64-bit address) and
-//    its size covers only the valid token rows, so rows past the end of the
-//    sequence, or a step that does not exist, read as zeros without touching
-//    memory.
-constexpr int kBufferDword3 = 0x00020000;  // raw buffer, 32-bit data format (gfx9 family)
-constexpr int kCachePolicyNT = 2;
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_rsrc(const uint16_t* base, int bytes) {
-  // the base is wave-uniform; passing it through readfirstlane keeps the
-  // descriptor in SGPRs (a 64-bit VALU add would otherwise leave it in VGPRs
-  // and every load would be wrapped in a waterfall loop)
-  const uint64_t a = reinterpret_cast<uint64_t>(base);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a >> 32));
-  void* ub = reinterpret_cast<void*>((static_cast<uint64_t>(hi) << 32) | lo);
-  return __builtin_amdgcn_make_buffer_rsrc(ub, 0, uniform(bytes), kBufferDword3);
-}
-__device__ __forceinline__ u32x4 ld16_stream(__amdgpu_buffer_rsrc_t r, int byte_off) {
-  return __builtin_amdgcn_raw_buffer_load_b128(r, byte_off, 0, kCachePolicyNT);
-}
 
 // Split partials that the last workgroup to finish a sequence merges (the
 // fused merge) cross workgroups on different XCDs, whose L2 caches are not
@@ -183,29 +122,6 @@ __device__ __forceinline__ f32x4 load_coherent4(__amdgpu_buffer_rsrc_t r, int64_
 __device__ __forceinline__ f32x2 load_coherent2(__amdgpu_buffer_rsrc_t r, int64_t idx) {
   return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, static_cast<int>(idx * 4), 0,
                                                                          kCachePolicyCoherent));
-}
-
-// Quotients on the way to the first loads of the fixed split and its
-// merge.  The compiler expands a 32-bit integer division into ~25 dependent
-// instructions; these divide in fp64 instead: both operands (0 <= a < 2^31,
-// 0 < b < 2^31) convert exactly and the quotient a/b, correctly rounded,
-// cannot reach the next integer (it is at least 1/b below it, more than the
-// rounding error of a quotient below 2^31), so truncation gives
-// floor(a / b).  div_small_u is the same for wave-uniform operands: the
-// quotient is computed in vector registers (the scalar unit has no fp64)
-// and readfirstlane returns it to scalar registers, so that nothing derived
-// from it takes vector registers.  (The stream-K prologue keeps the
-// compiler's integer division: there the fp64 form measured no faster and
-// cost the main loop vector registers.)
-__device__ __forceinline__ int div_small(int a, int b) {
-  return static_cast<int>(static_cast<double>(a) / static_cast<double>(b));
-}
-__device__ __forceinline__ int div_small_u(int a, int b) { return uniform(div_small(a, b)); }
-
-// Workgroup that owns flattened step x of `total`, when `parts` workgroups
-// split [0, total) into ranges [w*total/parts, (w+1)*total/parts).
-__device__ __forceinline__ int64_t owner_of(int64_t x, int64_t total, int64_t parts) {
-  return ((x + 1) * parts - 1) / total;
 }
 
 // Value of a partner lane in the same 16-lane row (DPP), for the vector-ALU
@@ -317,7 +233,10 @@ __device__ void merge_in_workgroup(uint16_t* __restrict__ out, const float* __re
 // is a chain of memory latencies; the prefix and the stream-K range put
 // ~3 us of them before the first K/V load on MI355X).  The pieces are
 // merged by merge_fixed_kernel.
-template <int D, bool kLanePages, int kNC = 0, bool kFused = false, bool kFixed = false>
+// kSink: a sliding window with `sinks` first tokens that every query sees as
+// well: the steps that hold them come ahead of the window's, and what lies
+// between is masked, and where a 16-token half holds nothing else not read.
+template <int D, bool kLanePages, int kNC = 0, bool kFused = false, bool kFixed = false, bool kSink = false>
 __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc,
     const uint16_t* __restrict__ vc, const int32_t* __restrict__ bt,
@@ -325,10 +244,12 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
     float* __restrict__ ws_acc, float* __restrict__ ws_ml, int32_t* __restrict__ ws_pref,
     int32_t* __restrict__ ws_cnt, int batch, int hq, int hkv, int group, int hgs, int page_shift,
     int num_pages, int maxp, int min_steps, float scale_log2, int nq, int window, int chunks,
-    int chunk_steps, int stash) {
+    int chunk_steps, int stash, int sinks_arg) {
   constexpr bool kValu = kNC > 0;
   static_assert(!kValu || (D == 128 && !kLanePages && (kNC == 4 || kNC == 8)), "vector-ALU variant shapes");
   static_assert(!kFixed || !kValu, "the fixed split runs on the matrix cores");
+  static_assert(!kSink || (!kValu && !kFused), "sinks: matrix cores and the merge kernel");
+  const int sinks = kSink ? sinks_arg : 0;
   // Every argument in SGPRs before anything waits on one: the compiler
   // otherwise requests them in two groups with a wait between (the second
   // group only where the first pointer is used), and since scalar loads
@@ -406,7 +327,7 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
       const int lo = tid * per;
       const int hi = min(batch, lo + per);
       int sum = 0;
-      for (int b = lo; b < hi; ++b) sum += extent(seq_steps(S::kLensInLds ? lens_s[b] : clamp_len(lens[b], max_ctx), nq, window));
+      for (int b = lo; b < hi; ++b) sum += extent(seq_steps(S::kLensInLds ? lens_s[b] : clamp_len(lens[b], max_ctx), nq, window, sinks));
       int incl = sum;  // inclusive prefix within the wave
   #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
@@ -420,7 +341,7 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
       int run = before + incl - sum;
       for (int b = lo; b < hi; ++b) {
         pref[b] = run;
-        run += extent(seq_steps(S::kLensInLds ? lens_s[b] : clamp_len(lens[b], max_ctx), nq, window));
+        run += extent(seq_steps(S::kLensInLds ? lens_s[b] : clamp_len(lens[b], max_ctx), nq, window, sinks));
       }
       if (tid == nthreads - 1) pref[batch] = before + incl;
       __syncthreads();
@@ -513,7 +434,7 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
       first_pids(fx_s0 + ph, fx_pa0, fx_pb0);
       first_pids(fx_s0 + ph + phases, fx_pa1, fx_pb1);
     }
-    fx_nb = seq_steps(clamp_len(uniform(fx_L), max_ctx), nq, window);
+    fx_nb = seq_steps(clamp_len(uniform(fx_L), max_ctx), nq, window, sinks);
     if (fx_s0 >= fx_nb) {  // a chunk past the sequence's end
       if (fx_nb == 0 && fx_s0 == 0) {
         // an empty sequence: chunk 0's workgroup writes its zero rows (the
@@ -588,10 +509,13 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
                          : uniform(S::kLensInLds ? lens_s[b] : clamp_len(lens[b], max_ctx));
     const int npages = (L + page - 1) >> page_shift;
     const int lo_seq = uniform(seq_start(L, nq, window));
-    const int sb = lo_seq / kStep;                  // first step of the sequence
+    // first step of the sequence; with sinks, index i >= nsink is step i + sb
+    const int pinned = kSink ? min(sinks, lo_seq) : 0;  // keys [0, pinned) are seen as sinks
+    const int nsink = kSink ? uniform(sink_steps(L, nq, window, sinks)) : 0;
+    const int sb = lo_seq / kStep - nsink;
     // the piece's steps [t0, t1): its range without the extent ahead of the
     // sequence's steps (a piece within that has none: partial of weight 0)
-    const int lead = kFixed ? 0 : nb - ((L + kStep - 1) / kStep - sb);
+    const int lead = kFixed ? 0 : nb - ((L + kStep - 1) / kStep - sb);  // (sb less the sinks' steps)
     const int t0 = max(s0 - lead, 0), t1 = max(s1 - lead, 0);
     // keys [lo_c, hi_c) of this lane's column; steps that cross a bound mask
     const int hi_c = L - nq + 1 + qj;
@@ -656,6 +580,10 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
     const int nsteps = sw < t1 ? (t1 - sw + phases - 1) / phases : 0;
     auto step_of = [&](int k) {  // k-th step of this wave (absolute), clamped to its last one
       k = k < nsteps ? k : nsteps - 1;
+      if constexpr (kSink) {
+        const int i = sw + k * phases;
+        return i < nsink ? i : i + sb;
+      }
       return sb + sw + k * phases;
     };
     auto load_pids = [&](int k, int& pa, int& pb) {
@@ -690,8 +618,8 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
       // valid token rows in each 16-token half (0 for a step past the wave's last)
       const int live = k < nsteps ? L - t0 : 0;
       // a half wholly before the first key is not read (its page may be released)
-      const int nA = (live < 0 || t0 + 16 <= lo_seq) ? 0 : (live < 16 ? live : 16);
-      const int nB = live < 16 ? 0 : (live < 32 ? live - 16 : 16);
+      const int nA = (live < 0 || (t0 + 16 <= lo_seq && t0 >= pinned)) ? 0 : (live < 16 ? live : 16);
+      const int nB = (live < 16 || (kSink && t0 + 32 <= lo_seq && t0 + 16 >= pinned)) ? 0 : (live < 32 ? live - 16 : 16);
       if constexpr (!kLanePages) {
         // pages of 16 or more tokens: each 16-token half of the step lies in one page
         const int pA = clamp_pid(pa_raw);
@@ -751,7 +679,7 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
     // pages every dead row is selected here.
     auto live_row = [&](int t0, int i) {
       const int tok = t0 + S::kRowsPerLoad * i + vr;
-      return tok < L && tok >= lo_seq;
+      return tok < L && (tok >= lo_seq || (kSink && tok < pinned));
     };
     auto stage_k = [&](const u32x4 (&kr)[S::kLoads], int t0) {
 #pragma unroll
@@ -771,8 +699,10 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
       if constexpr (!kLanePages) {
         if (t0 < lo_seq) {
 #pragma unroll
-          for (int i = 0; i < S::kLoads; ++i)
-            vv[i] = t0 + S::kRowsPerLoad * i + vr >= lo_seq ? vv[i] : u32x4{0u, 0u, 0u, 0u};
+          for (int i = 0; i < S::kLoads; ++i) {
+            const int tok = t0 + S::kRowsPerLoad * i + vr;
+            vv[i] = tok >= lo_seq || (kSink && tok < pinned) ? vv[i] : u32x4{0u, 0u, 0u, 0u};
+          }
         }
       }
 #pragma unroll
@@ -783,7 +713,8 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
 
     auto compute = [&](int s, const u32x4 (&kr)[S::kLoads], const u32x4 (&vv)[S::kLoads]) {
       const int t0 = s * kStep;
-      const bool edge = t0 + kStep > hi_min || t0 < lo_max;  // some key of the step is masked
+      // some key of the step is masked
+      const bool edge = t0 + kStep > hi_min || (t0 < lo_max && (!kSink || t0 + kStep > sinks));
       if constexpr (!S::kOneBuffer) {
         stage_k(kr, t0);
         lds_order();
@@ -815,7 +746,7 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
         for (int i = 0; i < 4; ++i) {
           float v = sacc[T][i] * scale_log2;
           const int t = t0 + 16 * T + 4 * g4 + i;
-          if (edge && (t >= hi_c || t < lo_c)) v = -__builtin_inff();
+          if (edge && (t >= hi_c || (t < lo_c && (!kSink || t >= sinks)))) v = -__builtin_inff();
           sv[T][i] = v;
           mx = fmaxf(mx, v);
         }
@@ -1334,7 +1265,7 @@ template <int D, int kPG>
 __global__ __launch_bounds__(kMergeThreads) void merge_fixed_kernel(
     uint16_t* __restrict__ out, const float* __restrict__ ws_acc, const float* __restrict__ ws_ml,
     const int32_t* __restrict__ lens, int hq, int hkv, int group, int hgs, int nq, int window, int max_ctx,
-    int chunks, int chunk_steps) {
+    int chunks, int chunk_steps, int sinks) {
   constexpr int kCols = D / 4;
   constexpr int kHPB = kMergeThreads / (kPG * kCols);  // query heads per workgroup
   static_assert(kHPB >= 1 && kHPB * kPG * kCols == kMergeThreads, "merge layout");
@@ -1346,7 +1277,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_fixed_kernel(
   // (pointers are inputs only, so their loads stay global loads)
   asm volatile(""
                : "+s"(hq), "+s"(hkv), "+s"(group), "+s"(hgs), "+s"(nq), "+s"(window), "+s"(max_ctx), "+s"(chunks),
-                 "+s"(chunk_steps)
+                 "+s"(chunk_steps), "+s"(sinks)
                : "s"(out), "s"(ws_acc), "s"(ws_ml), "s"(lens));
   const int ngroups = div_small_u(hkv, hgs);
   const int ncols = group * nq;
@@ -1379,7 +1310,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_fixed_kernel(
     aca[i] = *reinterpret_cast<const f32x4*>(ws_acc + row_of(w) * D + 4 * col);
   }
   __builtin_amdgcn_sched_barrier(0);  // every load above issues before the length is used
-  const int nb = seq_steps(clamp_len(len, max_ctx), nq, window);
+  const int nb = seq_steps(clamp_len(len, max_ctx), nq, window, sinks);
   const int n = div_small_u(nb + chunk_steps - 1, chunk_steps);  // pieces: slots e * chunks + [0, n)
   float mm = -__builtin_inff(), ll = 0.f;
   f32x4 nn = {0.f, 0.f, 0.f, 0.f};
@@ -1435,7 +1366,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_fixed_kernel(
       __builtin_bit_cast(u32x2, o);
 }
 
-template <int D, bool kLanePages, int kNC = 0, bool kFused = false, bool kFixed = false>
+template <int D, bool kLanePages, int kNC = 0, bool kFused = false, bool kFixed = false, bool kSink = false>
 static hipError_t launch_attn(const LaunchArgs& a, hipStream_t st) {
   const size_t lds = a.stash ? attn_stash_lds_bytes(D, a.batch, a.waves, a.hgs, a.group * a.nq, kNC > 0)
                              : attn_lds_bytes(D, a.batch, a.waves, kNC > 0);
@@ -1446,21 +1377,33 @@ static hipError_t launch_attn(const LaunchArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
   if (!bit || !(attr_set.load() & bit)) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_kernel<D, kLanePages, kNC, kFused, kFixed>),
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_kernel<D, kLanePages, kNC, kFused, kFixed, kSink>),
                             hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLdsBytes);
     if (e != hipSuccess) return e;
     attr_set.fetch_or(bit);
   }
-  hipLaunchKernelGGL((attn_kernel<D, kLanePages, kNC, kFused, kFixed>), dim3(a.grid), dim3(64 * a.waves), lds, st, a.q,
+  hipLaunchKernelGGL((attn_kernel<D, kLanePages, kNC, kFused, kFixed, kSink>), dim3(a.grid), dim3(64 * a.waves), lds, st, a.q,
                      a.k, a.v, a.bt, a.lens, a.out, a.ws_acc, a.ws_ml, a.ws_pref, a.ws_cnt, a.batch, a.hq, a.hkv,
                      a.group, a.hgs, a.page_shift, a.num_pages, a.maxp, a.min_steps, a.scale * kLog2e, a.nq,
-                     a.window, a.chunks, a.chunk_steps, a.stash ? 1 : 0);
+                     a.window, a.chunks, a.chunk_steps, a.stash ? 1 : 0, a.sinks);
   return hipGetLastError();
+}
+
+template <int D>
+static hipError_t launch_attn_sink(const LaunchArgs& a, bool lane_pages, hipStream_t st) {
+  if (a.valu_cols || a.fused) return hipErrorInvalidValue;
+  if (a.chunks > 0)
+    return lane_pages ? launch_attn<D, true, 0, false, true, true>(a, st) : launch_attn<D, false, 0, false, true, true>(a, st);
+  return lane_pages ? launch_attn<D, true, 0, false, false, true>(a, st) : launch_attn<D, false, 0, false, false, true>(a, st);
 }
 
 hipError_t launch_attn_kernel(const LaunchArgs& a, hipStream_t st) {
   const bool lane_pages = a.page_shift < 4;
   if (a.waves > max_waves(a.head_dim)) return hipErrorInvalidValue;
+  if (a.sinks > 0)
+    return a.head_dim == 128   ? launch_attn_sink<128>(a, lane_pages, st)
+           : a.head_dim == 256 ? launch_attn_sink<256>(a, lane_pages, st)
+                               : launch_attn_sink<64>(a, lane_pages, st);
   if (a.valu_cols) {
     // vector-ALU variant: D = 128, pages of 16 tokens or more, at most 8 columns, merge kernel
     if (a.head_dim != 128 || lane_pages || a.group * a.nq > a.valu_cols || a.fused || a.chunks > 0)
@@ -1512,7 +1455,7 @@ static hipError_t launch_merge_fixed(const LaunchArgs& a, hipStream_t st) {
   const int hchunks = (heads + kHPB - 1) / kHPB;
   const dim3 grid(a.batch * (a.hkv / a.hgs) * hchunks);
   hipLaunchKernelGGL((merge_fixed_kernel<D, kPG>), grid, dim3(kMergeThreads), 0, st, a.out, a.ws_acc, a.ws_ml, a.lens,
-                     a.hq, a.hkv, a.group, a.hgs, a.nq, a.window, a.maxp << a.page_shift, a.chunks, a.chunk_steps);
+                     a.hq, a.hkv, a.group, a.hgs, a.nq, a.window, a.maxp << a.page_shift, a.chunks, a.chunk_steps, a.sinks);
   return hipGetLastError();
 }
 
