@@ -292,6 +292,88 @@ int pda_kv4_workspace_reserve(int32_t batch, int32_t num_q_heads, int32_t num_kv
                               int32_t page_size, int32_t max_pages_per_seq, void* stream);
 
 /*
+ * The pages of a pool [library interface]: what a serving loop does to the
+ * block table between steps.  A pool's pages are counted in
+ *   refcount  int32 [num_pages] on the device: how many holders a page has --
+ *             each reference of a block table's live entries, and any others
+ *             the caller counts (a cache of prompts); 0 is a free page.
+ * Both calls below read a table and its counts and write new ones (the caller
+ * swaps them), with the list of pages whose contents have to move;
+ * pda_pages_copy then copies those in the pools of every layer.  All integers
+ * are exact and do not depend on the launch: the lowest row and the lowest
+ * page come first.
+ *
+ * pda_pages_update -- the table of the next step: fork, reorder, free,
+ * truncate, release and grow sequences, in one call.
+ *   block_table   int32 [batch, max_pages_per_seq], context_lens int32 [batch]:
+ *                 the present table.  Its first ceil(L_b / page_size) entries
+ *                 are references; entries outside [0, num_pages) refer to
+ *                 nothing (released pages).
+ *   parents       int32 [rows], or NULL: row r continues sequence parents[r]
+ *                 (NULL: sequence r); outside [0, batch): a new, empty one.  A
+ *                 sequence that no row continues is freed.
+ *   new_lens      int32 [rows]: tokens of each row, n_r, clamped to the table.
+ *                 It keeps the first k = min(L, n_r) of its parent's L tokens
+ *                 (fewer: the rest is dropped, as rejected drafts are) and has
+ *                 room for the others, which are yet to be appended.
+ *   window, num_sinks, num_queries  as for paged_decode_attention_sink: a page
+ *                 of kept tokens only that no query of the row, at length n_r,
+ *                 sees is released; window 0 releases nothing.
+ * Row r's pages j < ceil(k / page_size) are its parent's, shared.  One page is
+ * written into: that of token k - 1 where tokens follow it in the page
+ * (k % page_size != 0 and n_r > k).  The lowest row that writes into a page keeps
+ * it, if nothing else holds it; every other takes a fresh page and a copy.  The
+ * pages up to ceil(n_r / page_size) are fresh.  Fresh pages are the lowest free
+ * ones, where the pages that this update frees count as free, dealt in row
+ * order, a row's copy first.
+ *   table_out     int32 [rows, max_pages_per_seq]: the new table, -1 where a row
+ *                 has no page.
+ *   refcount_out  int32 [num_pages]: refcount less the present table's
+ *                 references plus the new one's.
+ *   copy_src, copy_dst  int32 [rows]: the page to copy for each row, -1 for none.
+ *   info          int32 [2]: fresh pages taken, and how many were lacking (their
+ *                 entries are -1; nothing may be appended there).
+ *
+ * pda_pages_compact -- the live pages (refcount > 0), n of them, to the front:
+ * those at n and above move, in order, into the free ones below n, in order.
+ *   table_out     int32 [batch, max_pages_per_seq]: the table with the new
+ *                 numbers, -1 past each sequence's pages and for released ones.
+ *   refcount_out, page_map  int32 [num_pages]: the counts by new number; the new
+ *                 number of each page, -1 for a free one (for other holders).
+ *   copy_src, copy_dst  int32 [num_pages]: the pages that move, then -1.
+ *   info          int32 [2]: n, and how many move.
+ *
+ * pda_pages_copy -- page copy_dst[i] of every pool becomes a copy of page
+ * copy_src[i], for i < max_copies (and i < *count, where count, a device
+ * pointer, is not NULL); pairs with an entry outside [0, num_pages) are skipped.
+ *   pools         host array of num_pools pools of num_pages pages each: a device
+ *                 pointer, 16-byte aligned, and the bytes of a page, a multiple
+ *                 of 16 (every layer's K and V, codes and scales).
+ * No page may be the destination of two pairs, nor the destination of one and
+ * the source of another (the lists above keep to that).
+ *
+ * num_pages at most 16777216, batch and rows at most 8192; outputs may not
+ * overlap inputs or each other (PDA_ERR_LAYOUT).  Asynchronous on `stream`;
+ * update and compact use the (device, stream) workspace: 8 bytes a page, which
+ * pda_pages_workspace_reserve allocates ahead of a graph capture.
+ */
+typedef struct {
+  void* data;
+  int64_t page_bytes;
+} pda_pool;
+int pda_pages_update(const int32_t* block_table, const int32_t* context_lens, const int32_t* parents,
+                     const int32_t* new_lens, const int32_t* refcount, int32_t* table_out, int32_t* refcount_out,
+                     int32_t* copy_src, int32_t* copy_dst, int32_t* info, int32_t batch, int32_t rows, int32_t page_size,
+                     int32_t num_pages, int32_t max_pages_per_seq, int32_t num_queries, int32_t window, int32_t num_sinks,
+                     void* stream);
+int pda_pages_compact(const int32_t* block_table, const int32_t* context_lens, const int32_t* refcount, int32_t* table_out,
+                      int32_t* refcount_out, int32_t* page_map, int32_t* copy_src, int32_t* copy_dst, int32_t* info,
+                      int32_t batch, int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, void* stream);
+int pda_pages_copy(const pda_pool* pools, int32_t num_pools, const int32_t* copy_src, const int32_t* copy_dst,
+                   const int32_t* count, int32_t max_copies, int32_t num_pages, void* stream);
+int pda_pages_workspace_reserve(int32_t rows, int32_t num_pages, void* stream);
+
+/*
  * pda_kv_append -- write each sequence's newest key and value into its page:
  * the step before attention in the paper's decode loop (Method, "Kernel
  * Customization and Multi-Request Adaptation": a small scatter kernel writes

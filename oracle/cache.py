@@ -103,3 +103,106 @@ def kv4_read(codes, scales, tokens, block_table, context_lens):
             if t >= 0:
                 out[b, j] = x[int(block_table[b][t // x.shape[1]]), t % x.shape[1]]
     return out
+
+
+# ---------------------------------------------------------------------- pages
+def pages_update(table, lens, parents, new_lens, refcount, page, window=0, sinks=0, num_queries=1):
+    """Row by row from the rules of pda_pages_update: (table, refcount, copy_src, copy_dst, [taken, lacking])."""
+    table = np.asarray(table)
+    batch, m = table.shape
+    count = np.array(refcount, dtype=np.int64)
+    n_pages = len(count)
+
+    def length(b):
+        return min(max(int(lens[b]), 0), m * page)
+
+    def entry(b, j):
+        e = int(table[b, j])
+        return e if 0 <= e < n_pages else -1
+
+    for b in range(batch):
+        for j in range(-(-length(b) // page)):
+            if entry(b, j) >= 0:
+                count[entry(b, j)] -= 1
+    rows = len(new_lens)
+    out = np.full((rows, m), -1, dtype=np.int32)
+    src, dst = np.full(rows, -1, np.int32), np.full(rows, -1, np.int32)
+    plans = []
+    for r in range(rows):
+        b = r if parents is None else int(parents[r])
+        has = 0 <= b < batch
+        total = min(max(int(new_lens[r]), 0), m * page)
+        kept = min(length(b), total) if has else 0
+        first_seen = max(0, total - num_queries + 1 - window) if window > 0 else 0
+        write = None
+        for j in range(-(-kept // page)):
+            tokens = range(j * page, (j + 1) * page)
+            if tokens[-1] < kept and all(sinks <= t < first_seen for t in tokens):
+                continue
+            if tokens[-1] >= kept and total > kept:
+                write = (j, entry(b, j))
+                continue
+            out[r, j] = entry(b, j)
+            if out[r, j] >= 0:
+                count[out[r, j]] += 1
+        plans.append((kept, total, write))
+    held = count.copy()  # by others than the rows that write
+    lowest = {}
+    for r, (_, _, write) in enumerate(plans):
+        if write and write[1] >= 0:
+            lowest.setdefault(write[1], r)
+    copies = set()
+    for r, (_, _, write) in enumerate(plans):
+        if write is None:
+            continue
+        j, p = write
+        if p >= 0 and lowest[p] == r and held[p] == 0:
+            out[r, j] = p
+            count[p] = 1
+        else:
+            copies.add(r)
+    free = [p for p in range(n_pages) if count[p] == 0]
+    taken = lacking = 0
+
+    def fresh():
+        nonlocal taken, lacking
+        if taken < len(free):
+            taken += 1
+            count[free[taken - 1]] = 1
+            return free[taken - 1]
+        lacking += 1
+        return -1
+
+    for r, (kept, total, write) in enumerate(plans):
+        if r in copies:
+            j, p = write
+            out[r, j] = fresh()
+            if p >= 0 and out[r, j] >= 0:
+                src[r], dst[r] = p, out[r, j]
+        for j in range(-(-kept // page), -(-total // page)):
+            out[r, j] = fresh()
+    return out, count.astype(np.int32), src, dst, np.array([taken, lacking], np.int32)
+
+
+def pages_compact(table, lens, refcount, page):
+    """(table, refcount, page_map, copy_src, copy_dst, [live, moved]) of pda_pages_compact."""
+    table = np.asarray(table)
+    n_pages, m = len(refcount), table.shape[1]
+    live = [p for p in range(n_pages) if refcount[p] > 0]
+    n = len(live)
+    holes = [p for p in range(n) if refcount[p] <= 0]
+    movers = [p for p in live if p >= n]
+    page_map = np.full(n_pages, -1, np.int32)
+    page_map[live] = live
+    page_map[movers] = holes
+    count = np.zeros(n_pages, np.int32)
+    for p in live:
+        count[page_map[p]] = refcount[p]
+    out = np.full(table.shape, -1, np.int32)
+    for b in range(table.shape[0]):
+        for j in range(-(-min(max(int(lens[b]), 0), m * page) // page)):
+            if 0 <= table[b, j] < n_pages:
+                out[b, j] = page_map[table[b, j]]
+    src, dst = np.full(n_pages, -1, np.int32), np.full(n_pages, -1, np.int32)
+    src[:len(movers)], dst[:len(movers)] = movers, holes
+    return out, count, page_map, src, dst, np.array([n, len(movers)], np.int32)

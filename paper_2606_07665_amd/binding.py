@@ -59,6 +59,11 @@ class Projection(ctypes.Structure):
                                                     "workgroups", "ss_parts")] + [("workspace_bytes", ctypes.c_int64)]
 
 
+class Pool(ctypes.Structure):
+    """pda_pool of include/pda.h."""
+    _fields_ = [("data", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
+
+
 DTYPE_BF16, DTYPE_F16, DTYPE_F32, DTYPE_I32, DTYPE_I64 = range(5)  # pda_dtype
 MAX_DIMS = 4
 
@@ -119,6 +124,12 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.paged_decode_attention_kv4.restype = ctypes.c_int
     for fn in (lib.pda_kv4_append, lib.pda_kv4_read):
         fn.argtypes = [vp] * 8 + [i32] * 7 + [vp]
+        fn.restype = ctypes.c_int
+    lib.pda_pages_update.argtypes = [vp] * 10 + [i32] * 8 + [vp]
+    lib.pda_pages_compact.argtypes = [vp] * 9 + [i32] * 4 + [vp]
+    lib.pda_pages_copy.argtypes = [ctypes.POINTER(Pool), i32, vp, vp, vp, i32, i32, vp]
+    lib.pda_pages_workspace_reserve.argtypes = [i32, i32, vp]
+    for fn in (lib.pda_pages_update, lib.pda_pages_compact, lib.pda_pages_copy, lib.pda_pages_workspace_reserve):
         fn.restype = ctypes.c_int
     lib.pda_kv4_workspace_reserve.argtypes = [i32] * 6 + [vp]
     lib.pda_kv4_workspace_reserve.restype = ctypes.c_int
@@ -557,6 +568,73 @@ def paged_decode_attention_kv4(q, k_codes, k_scales, v_codes, v_scales, block_ta
 
 def kv4_workspace_reserve(batch, hq, hkv, d, page_size, max_pages, stream=None) -> None:
     _check(load().pda_kv4_workspace_reserve(batch, hq, hkv, d, page_size, max_pages, _stream_ptr(stream)))
+
+
+def pages_update(block_table, context_lens, parents, new_lens, refcount, table_out, refcount_out, copy_src, copy_dst, info,
+                 page_size, window=0, sinks=0, num_queries=1, stream=None):
+    """The table of the next step: row r continues sequence parents[r] (``parents`` None: sequence r)
+    with new_lens[r] tokens -- forked, reordered, truncated, grown, and with the pages released that
+    ``window`` and ``sinks`` leave invisible; sequences that no row continues are freed.
+
+    block_table int32 [B, M], context_lens [B], parents and new_lens [R], refcount [N] -> table_out
+    [R, M], refcount_out [N], copy_src and copy_dst [R] (for :func:`pages_copy`), info [2]: fresh pages
+    taken, and lacking.  include/pda.h states the rules."""
+    import torch
+    i32 = torch.int32
+    sz = _validate([("block_table", block_table, i32, "B M"), ("context_lens", context_lens, i32, "B"),
+                    ("parents", parents, i32, "R"), ("new_lens", new_lens, i32, "R"), ("refcount", refcount, i32, "N"),
+                    ("table_out", table_out, i32, "R M"), ("refcount_out", refcount_out, i32, "N"),
+                    ("copy_src", copy_src, i32, "R"), ("copy_dst", copy_dst, i32, "R"), ("info", info, i32, "2")])
+    _check(load().pda_pages_update(
+        block_table.data_ptr(), context_lens.data_ptr(), _ptr(parents), new_lens.data_ptr(), refcount.data_ptr(),
+        table_out.data_ptr(), refcount_out.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), info.data_ptr(), sz["B"],
+        sz["R"], int(page_size), sz["N"], sz["M"], int(num_queries), int(window), int(sinks),
+        _stream_ptr(stream, refcount.get_device())))
+
+
+def pages_compact(block_table, context_lens, refcount, table_out, refcount_out, page_map, copy_src, copy_dst, info, page_size,
+                  stream=None):
+    """The live pages to the front of the pool: table_out, refcount_out and page_map [N] by the new
+    numbers, the pages to move in copy_src and copy_dst [N], info [2]: live pages, and how many move."""
+    import torch
+    i32 = torch.int32
+    sz = _validate([("block_table", block_table, i32, "B M"), ("context_lens", context_lens, i32, "B"),
+                    ("refcount", refcount, i32, "N"), ("table_out", table_out, i32, "B M"),
+                    ("refcount_out", refcount_out, i32, "N"), ("page_map", page_map, i32, "N"),
+                    ("copy_src", copy_src, i32, "N"), ("copy_dst", copy_dst, i32, "N"), ("info", info, i32, "2")])
+    _check(load().pda_pages_compact(
+        block_table.data_ptr(), context_lens.data_ptr(), refcount.data_ptr(), table_out.data_ptr(), refcount_out.data_ptr(),
+        page_map.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), info.data_ptr(), sz["B"], int(page_size), sz["N"],
+        sz["M"], _stream_ptr(stream, refcount.get_device())))
+
+
+def pages_copy(pools, copy_src, copy_dst, count=None, stream=None):
+    """Page copy_dst[i] of every pool becomes a copy of page copy_src[i] (pairs with a negative entry
+    are skipped; ``count`` int32 [1]: only the first ones).  ``pools``: tensors whose first dimension is
+    the pages, every layer's K and V, of any type."""
+    import torch
+    sz = _validate([("copy_src", copy_src, torch.int32, "C"), ("copy_dst", copy_dst, torch.int32, "C"),
+                    ("count", count, torch.int32, "1")])
+    dev = copy_src.get_device()
+    if not pools:
+        return
+    n = pools[0].shape[0] if pools[0].dim() else 0
+    arr = (Pool * len(pools))()
+    for i, t in enumerate(pools):
+        if t.dim() < 2 or t.shape[0] != n:
+            raise ValueError(f"pool {i} must be [{n}, ...], got shape {tuple(t.shape)}")
+        if t.get_device() != dev:
+            raise ValueError(f"pool {i} must be on the GPU of copy_src")
+        if not t.is_contiguous():
+            raise ValueError(f"pool {i} must be contiguous")
+        arr[i].data = t.data_ptr()
+        arr[i].page_bytes = t.numel() // n * t.element_size() if n else 0
+    _check(load().pda_pages_copy(arr, len(pools), copy_src.data_ptr(), copy_dst.data_ptr(), _ptr(count), sz["C"], n,
+                                 _stream_ptr(stream, dev)))
+
+
+def pages_workspace_reserve(rows, num_pages, stream=None) -> None:
+    _check(load().pda_pages_workspace_reserve(rows, num_pages, _stream_ptr(stream)))
 
 
 def kv_append(k_new, v_new, k_cache, v_cache, block_table, context_lens, stream=None):

@@ -23,6 +23,7 @@
 #include "pda_gemv.h"
 #include "pda_internal.h"
 #include "pda_kv4.h"
+#include "pda_pages.h"
 
 namespace {
 
@@ -1055,6 +1056,48 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
   return PDA_OK;
 }
 
+// ---------------------------------------------------------------- pages
+// Checks shared by the calls that rewrite a table: its sizes, and that no
+// output lies over an input or another output.
+int check_pages(int32_t batch, int32_t rows, int32_t page_size, int32_t num_pages, int32_t maxp) {
+  int rc = check_shape(batch, 1, 1, 64, page_size, maxp);
+  if (rc || (rc = check_shape(rows, 1, 1, 64, page_size, maxp))) return rc;
+  if (num_pages <= 0) return fail(PDA_ERR_SHAPE, "num_pages must be positive (got %d)", num_pages);
+  if (num_pages > pda::kMaxPoolPages)
+    return fail(PDA_ERR_UNSUPPORTED, "num_pages %d exceeds %d", num_pages, pda::kMaxPoolPages);
+  if (static_cast<int64_t>(std::max(batch, rows)) * maxp >= (int64_t{1} << 31))
+    return fail(PDA_ERR_UNSUPPORTED, "rows * max_pages_per_seq exceeds 2^31");
+  return PDA_OK;
+}
+
+struct Span {
+  const char* name;
+  const void* p;
+  int64_t words;
+};
+
+// All present (but for empty ones), 4-byte aligned, and the outputs, which come
+// last from `first_out` on, apart from everything else.
+template <size_t kN>
+int check_spans(const Span (&s)[kN], size_t first_out) {
+  for (const Span& x : s) {
+    if (x.words > 0 && !x.p) return fail(PDA_ERR_NULL, "%s is NULL", x.name);
+    if (misaligned(x.p, 4)) return fail(PDA_ERR_ALIGN, "%s must be 4-byte aligned", x.name);
+  }
+  for (size_t i = first_out; i < kN; ++i)
+    for (size_t j = 0; j < i; ++j)
+      if (overlaps(s[i].p, 4 * s[i].words, s[j].p, 4 * s[j].words))
+        return fail(PDA_ERR_LAYOUT, "%s overlaps %s", s[i].name, s[j].name);
+  return PDA_OK;
+}
+
+int64_t update_ws_bytes(int32_t rows, int32_t num_pages) {
+  return align256((2 * static_cast<int64_t>(num_pages) + rows) * 4);
+}
+int64_t compact_ws_bytes(int32_t num_pages) {
+  return align256((static_cast<int64_t>(num_pages) + num_pages / pda::kCompactPages + 1) * 4);
+}
+
 // A workspace for every call of these sizes, for the most (query token, head)
 // columns, so any num_queries fits.
 int reserve_attention(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
@@ -1592,6 +1635,155 @@ int paged_decode_attention_kv4(const void* q, const void* k_codes, const void* k
   c.vs = static_cast<uint8_t*>(const_cast<void*>(v_scales));
   return attention_call(q, k_codes, v_codes, block_table, context_lens, out, batch, num_q_heads, num_kv_heads, head_dim,
                         page_size, num_pages, max_pages_per_seq, num_queries, window, scale, stream, false, num_sinks, &c);
+}
+
+int pda_pages_update(const int32_t* block_table, const int32_t* context_lens, const int32_t* parents,
+                     const int32_t* new_lens, const int32_t* refcount, int32_t* table_out, int32_t* refcount_out,
+                     int32_t* copy_src, int32_t* copy_dst, int32_t* info, int32_t batch, int32_t rows, int32_t page_size,
+                     int32_t num_pages, int32_t max_pages_per_seq, int32_t num_queries, int32_t window, int32_t num_sinks,
+                     void* stream) {
+  g_err.clear();
+  int rc = check_pages(batch, rows, page_size, num_pages, max_pages_per_seq);
+  if (rc) return rc;
+  if (num_queries < 1) return fail(PDA_ERR_SHAPE, "num_queries must be >= 1 (got %d)", num_queries);
+  if (window < 0 || num_sinks < 0)
+    return fail(PDA_ERR_SHAPE, "window and num_sinks must be >= 0 (got %d, %d)", window, num_sinks);
+  const int64_t table = static_cast<int64_t>(batch) * max_pages_per_seq;
+  const Span spans[] = {{"block_table", block_table, table}, {"context_lens", context_lens, batch},
+                        {"parents", parents, parents ? rows : 0}, {"new_lens", new_lens, rows},
+                        {"refcount", refcount, num_pages}, {"table_out", table_out, static_cast<int64_t>(rows) * max_pages_per_seq},
+                        {"refcount_out", refcount_out, num_pages}, {"copy_src", copy_src, rows},
+                        {"copy_dst", copy_dst, rows}, {"info", info, 2}};
+  if ((rc = check_spans(spans, 5))) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  void* ws = nullptr;
+  const int64_t need = update_ws_bytes(rows, num_pages);
+  if ((rc = workspace_for(dev, st, need, need, &ws))) return rc;
+  pda::PagesUpdateArgs a;
+  a.table = block_table;
+  a.lens = context_lens;
+  a.parents = parents;
+  a.new_lens = new_lens;
+  a.refcount = refcount;
+  a.table_out = table_out;
+  a.refcount_out = refcount_out;
+  a.src = copy_src;
+  a.dst = copy_dst;
+  a.info = info;
+  a.writer = static_cast<int32_t*>(ws);
+  a.fresh = a.writer + num_pages;
+  a.start = a.fresh + num_pages;
+  a.batch = batch;
+  a.rows = rows;
+  a.page_shift = log2i(page_size);
+  a.num_pages = num_pages;
+  a.maxp = max_pages_per_seq;
+  a.nq = num_queries;
+  a.window = window;
+  a.sinks = num_sinks;
+  if ((e = pda::launch_pages_update(a, st)) != hipSuccess) return hip_fail(e, "page update launch");
+  return PDA_OK;
+}
+
+int pda_pages_compact(const int32_t* block_table, const int32_t* context_lens, const int32_t* refcount, int32_t* table_out,
+                      int32_t* refcount_out, int32_t* page_map, int32_t* copy_src, int32_t* copy_dst, int32_t* info,
+                      int32_t batch, int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, void* stream) {
+  g_err.clear();
+  int rc = check_pages(batch, batch, page_size, num_pages, max_pages_per_seq);
+  if (rc) return rc;
+  const int64_t table = static_cast<int64_t>(batch) * max_pages_per_seq;
+  const Span spans[] = {{"block_table", block_table, table}, {"context_lens", context_lens, batch},
+                        {"refcount", refcount, num_pages}, {"table_out", table_out, table},
+                        {"refcount_out", refcount_out, num_pages}, {"page_map", page_map, num_pages},
+                        {"copy_src", copy_src, num_pages}, {"copy_dst", copy_dst, num_pages}, {"info", info, 2}};
+  if ((rc = check_spans(spans, 3))) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  void* ws = nullptr;
+  const int64_t need = compact_ws_bytes(num_pages);
+  if ((rc = workspace_for(dev, st, need, need, &ws))) return rc;
+  pda::PagesCompactArgs a;
+  a.table = block_table;
+  a.lens = context_lens;
+  a.refcount = refcount;
+  a.table_out = table_out;
+  a.refcount_out = refcount_out;
+  a.map = page_map;
+  a.src = copy_src;
+  a.dst = copy_dst;
+  a.info = info;
+  a.place = static_cast<int32_t*>(ws);
+  a.counts = a.place + num_pages;
+  a.batch = batch;
+  a.page_shift = log2i(page_size);
+  a.num_pages = num_pages;
+  a.maxp = max_pages_per_seq;
+  if ((e = pda::launch_pages_compact(a, st)) != hipSuccess) return hip_fail(e, "page compaction launch");
+  return PDA_OK;
+}
+
+int pda_pages_copy(const pda_pool* pools, int32_t num_pools, const int32_t* copy_src, const int32_t* copy_dst,
+                   const int32_t* count, int32_t max_copies, int32_t num_pages, void* stream) {
+  g_err.clear();
+  if (num_pools < 0 || max_copies < 0)
+    return fail(PDA_ERR_SHAPE, "num_pools and max_copies must be >= 0 (got %d, %d)", num_pools, max_copies);
+  if (num_pages <= 0) return fail(PDA_ERR_SHAPE, "num_pages must be positive (got %d)", num_pages);
+  if (num_pools == 0 || max_copies == 0) return PDA_OK;
+  if (!pools || !copy_src || !copy_dst) return fail(PDA_ERR_NULL, "a pointer is NULL");
+  if (misaligned(copy_src, 4) || misaligned(copy_dst, 4) || misaligned(count, 4))
+    return fail(PDA_ERR_ALIGN, "copy_src, copy_dst and count must be 4-byte aligned");
+  for (int32_t i = 0; i < num_pools; ++i) {
+    const pda_pool& p = pools[i];
+    if (!p.data) return fail(PDA_ERR_NULL, "pool %d is NULL", i);
+    if (p.page_bytes <= 0 || p.page_bytes > (int64_t{1} << 30))
+      return fail(PDA_ERR_SHAPE, "pool %d: page_bytes %lld outside [16, 2^30]", i, static_cast<long long>(p.page_bytes));
+    if (misaligned(p.data, 16) || p.page_bytes % 16)
+      return fail(PDA_ERR_ALIGN, "pool %d must be 16-byte aligned, its pages a multiple of 16 bytes", i);
+    if (static_cast<int64_t>(max_copies) * pda::kMaxCopyPools * pda::pages_copy_parts(p.page_bytes) >= (int64_t{1} << 31))
+      return fail(PDA_ERR_UNSUPPORTED, "max_copies %d of pages of %lld bytes", max_copies, static_cast<long long>(p.page_bytes));
+  }
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  int cus = 0;
+  const int rc = device_cus(dev, &cus);
+  if (rc) return rc;
+  for (int32_t at = 0; at < num_pools; at += pda::kMaxCopyPools) {
+    pda::PagesCopyArgs a = {};
+    a.pools = std::min(pda::kMaxCopyPools, num_pools - at);
+    int64_t most = 0;
+    for (int i = 0; i < a.pools; ++i) {
+      a.pool[i].data = static_cast<char*>(pools[at + i].data);
+      a.pool[i].bytes = pools[at + i].page_bytes;
+      most = std::max(most, pools[at + i].page_bytes);
+    }
+    a.src = copy_src;
+    a.dst = copy_dst;
+    a.count = count;
+    a.most = max_copies;
+    a.num_pages = num_pages;
+    if ((e = pda::launch_pages_copy(a, most, cus, static_cast<hipStream_t>(stream))) != hipSuccess)
+      return hip_fail(e, "page copy launch");
+  }
+  return PDA_OK;
+}
+
+int pda_pages_workspace_reserve(int32_t rows, int32_t num_pages, void* stream) {
+  g_err.clear();
+  if (rows < 0 || rows > PDA_MAX_BATCH) return fail(PDA_ERR_SHAPE, "rows must be in [0, %d] (got %d)", PDA_MAX_BATCH, rows);
+  if (num_pages <= 0 || num_pages > pda::kMaxPoolPages)
+    return fail(PDA_ERR_SHAPE, "num_pages must be in [1, %d] (got %d)", pda::kMaxPoolPages, num_pages);
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  void* ptr = nullptr;
+  const int64_t need = std::max(update_ws_bytes(rows, num_pages), compact_ws_bytes(num_pages));
+  return workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr);
 }
 
 int pda_kv4_append(const void* k_new, const void* v_new, void* k_codes, void* k_scales, void* v_codes, void* v_scales,

@@ -83,3 +83,82 @@ def test_kv4_reserve(lib):
     assert lib.pda_kv4_workspace_reserve(2, 32, 8, 128, 8, 8, None) == UNSUPPORTED
     assert lib.pda_kv4_workspace_reserve(2, 32, 7, 128, 16, 8, None) == SHAPE
     assert lib.pda_kv4_workspace_reserve(0, 32, 8, 128, 16, 8, None) == 0
+
+
+# ---------------------------------------------------------------------- pages
+LAYOUT = 8
+
+
+def spread(n, size=1 << 20):
+    return [(1 + i) * size for i in range(n)]
+
+
+@pytest.mark.parametrize("kw,code,text", [
+    (dict(null=0), NULL, "block_table"),
+    (dict(null=3), NULL, "new_lens"),
+    (dict(null=9), NULL, "info"),
+    (dict(odd=5), ALIGN, "table_out"),
+    (dict(batch=-1), SHAPE, "batch"),
+    (dict(rows=8193), UNSUPPORTED, "batch"),
+    (dict(p=3), UNSUPPORTED, "page_size"),
+    (dict(n=0), SHAPE, "num_pages"),
+    (dict(n=(1 << 24) + 1), UNSUPPORTED, "num_pages"),
+    (dict(nq=0), SHAPE, "num_queries"),
+    (dict(window=-1), SHAPE, "window"),
+    (dict(sinks=-1), SHAPE, "num_sinks"),
+    (dict(same=(5, 0)), LAYOUT, "table_out overlaps block_table"),
+    (dict(same=(8, 7)), LAYOUT, "copy_dst overlaps copy_src"),
+])
+def test_pages_update(lib, kw, code, text):
+    a = dict(dict(batch=2, rows=3, p=16, n=64, maxp=8, nq=1, window=0, sinks=0), **kw)
+    ptr = spread(10)
+    if "null" in a:
+        ptr[a["null"]] = 0
+    if "odd" in a:
+        ptr[a["odd"]] += 2
+    if "same" in a:
+        ptr[a["same"][0]] = ptr[a["same"][1]]
+    assert lib.pda_pages_update(*ptr, a["batch"], a["rows"], a["p"], a["n"], a["maxp"], a["nq"], a["window"], a["sinks"],
+                                None) == code
+    assert text in B.last_error()
+
+
+@pytest.mark.parametrize("null,odd,same,code,text", [
+    (2, None, None, NULL, "refcount"), (None, 8, None, ALIGN, "info"), (None, None, (4, 2), LAYOUT, "refcount_out"),
+    (None, None, (3, 0), LAYOUT, "table_out")])
+def test_pages_compact(lib, null, odd, same, code, text):
+    ptr = spread(9)
+    if null is not None:
+        ptr[null] = 0
+    if odd is not None:
+        ptr[odd] += 1
+    if same:
+        ptr[same[0]] = ptr[same[1]]
+    assert lib.pda_pages_compact(*ptr, 2, 16, 64, 8, None) == code
+    assert text in B.last_error()
+
+
+@pytest.mark.parametrize("kw,code,text", [
+    (dict(data=0), NULL, "pool 0"),
+    (dict(data=8), ALIGN, "16-byte"),
+    (dict(size=24), ALIGN, "multiple of 16"),
+    (dict(size=0), SHAPE, "page_bytes"),
+    (dict(src=0), NULL, "NULL"),
+    (dict(src=2), ALIGN, "copy_src"),
+    (dict(most=-1), SHAPE, "max_copies"),
+    (dict(most=1 << 24, size=1 << 15), UNSUPPORTED, "max_copies"),
+    (dict(n=0), SHAPE, "num_pages"),
+    (dict(pools=-1), SHAPE, "num_pools"),
+])
+def test_pages_copy(lib, kw, code, text):
+    a = dict(dict(data=16, size=32, src=16, most=4, n=8, pools=1), **kw)
+    pools = (B.Pool * 1)(B.Pool(a["data"], a["size"]))
+    assert lib.pda_pages_copy(pools, a["pools"], a["src"], 16, None, a["most"], a["n"], None) == code
+    assert text in B.last_error()
+
+
+def test_pages_no_ops(lib):
+    assert lib.pda_pages_copy(None, 0, None, None, None, 5, 8, None) == 0
+    assert lib.pda_pages_copy(None, 3, None, None, None, 0, 8, None) == 0
+    assert lib.pda_pages_workspace_reserve(-1, 5, None) == SHAPE
+    assert lib.pda_pages_workspace_reserve(1, 0, None) == SHAPE

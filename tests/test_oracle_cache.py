@@ -98,3 +98,52 @@ def test_sinks_change_only_what_a_window_hides():
     far = C.attend(*args, window=30, sinks=4)
     assert np.abs(far - C.attend(*args, window=30)).max() > 1e-4
     assert np.array_equal(C.attend(*args, window=0, sinks=4), C.attend(*args))
+
+
+# ---------------------------------------------------------------------- pages
+def test_update_keeps_counts_tables_and_contents_together():
+    """Random histories of a small cache whose tokens carry their sequence's own numbers: after every update, the
+    copies and the appends, each row reads back what it should hold, and counts equal references."""
+    page, n_pages, m = 4, 60, 8
+    for seed in range(20):
+        rng = np.random.default_rng(seed)
+        pool = np.full((n_pages, page), -1)
+        table, lens, count = np.full((1, m), -1, np.int32), np.zeros(1, np.int64), np.zeros(n_pages, np.int32)
+        held = [[]]
+        for _ in range(25):
+            rows = int(rng.integers(1, 5))
+            parents = rng.integers(-1, len(held), rows)
+            new = np.array([max(0, min(m * page, (len(held[p]) if p >= 0 else 0) + int(rng.choice([-3, 0, 1, 1, 2, 6]))))
+                            for p in parents])
+            table, count, src, dst, info = C.pages_update(table, lens, parents, new, count, page)
+            assert info[1] == 0
+            before = pool.copy()
+            for a, b in zip(src, dst):
+                if b >= 0:
+                    pool[b] = before[a]
+            kept = [held[p][:n] if p >= 0 else [] for p, n in zip(parents, new)]
+            held = [k + rng.integers(0, 1000, n - len(k)).tolist() for k, n in zip(kept, new)]
+            for r, (k, h) in enumerate(zip(kept, held)):
+                for t in range(len(k), len(h)):
+                    pool[table[r, t // page], t % page] = h[t]
+            lens = new
+            for r, h in enumerate(held):
+                assert [pool[table[r, t // page], t % page] for t in range(len(h))] == h
+                assert (table[r, -(-len(h) // page):] == -1).all()
+            used = table[table >= 0]
+            assert np.array_equal(np.bincount(used, minlength=n_pages), count)
+            table2, count2, page_map, s2, d2, info2 = C.pages_compact(table, lens, count, page)
+            before = pool.copy()
+            pool[d2[:info2[1]]] = before[s2[:info2[1]]]
+            assert (count2[:info2[0]] > 0).all() and (count2[info2[0]:] == 0).all()
+            table, count = table2, count2
+            for r, h in enumerate(held):
+                assert [pool[table[r, t // page], t % page] for t in range(len(h))] == h
+
+
+def test_update_releases_what_a_window_hides_and_keeps_sinks():
+    page, table = 4, np.arange(10, dtype=np.int32)[None]
+    out, count, *_ = C.pages_update(table, [40], None, [41], np.ones(12, np.int32), page, window=9, sinks=5)
+    assert out.shape == (1, 10)  # 41 tokens are clamped to the table's 40
+    assert out[0].tolist() == [0, 1, -1, -1, -1, -1, -1, 7, 8, 9]
+    assert count.tolist() == [1, 1, 0, 0, 0, 0, 0, 1, 1, 1, 1, 1]
