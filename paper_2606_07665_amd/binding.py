@@ -37,7 +37,8 @@ _DECLINED = -1     # its answer where the Python checks are to be run
 # entry points the native module calls
 _NATIVE_CALLS = ("paged_decode_attention_ext", "paged_decode_attention_noalloc", "paged_decode_attention_append",
                  "pda_kv_append_n", "pda_attention_prelude", "pda_attention_prelude_append",
-                 "pda_o_proj_residual_norm")
+                 "pda_o_proj_residual_norm", "paged_decode_attention_sink", "paged_decode_attention_kv4", "pda_kv4_append",
+                 "pda_kv4_read", "pda_pages_update", "pda_pages_compact", "pda_pages_copy")
 
 
 class PdaError(RuntimeError):
@@ -208,6 +209,7 @@ class _Declining:
         return _DECLINED
 
     attention = kv_append = attention_append = prelude = o_proj = _decline
+    attention_sink = attention_kv4 = kv4_tokens = pages_update = pages_compact = pages_copy = _decline
 
 
 def _built_for() -> str:
@@ -494,13 +496,19 @@ def paged_decode_attention_sink(q, k_cache, v_cache, block_table, context_lens, 
     """:func:`paged_decode_attention_ext` with first tokens that stay visible
     under the window: the query at position p sees the keys t <= p with
     t > p - ``window`` or t < ``sinks`` (``window`` 0: every key)."""
+    rc = (_nat or _load_native()).attention_sink(q, k_cache, v_cache, block_table, context_lens, out, scale, window, sinks,
+                                                 stream)
+    if rc == PDA_OK:
+        return out
+    if rc != _DECLINED:
+        _check(rc)
     import torch
     sz = _validate([("q", q, torch.bfloat16, "B T Hq D"), *_cache_specs(k_cache, v_cache, block_table, context_lens),
                     ("out", out, torch.bfloat16, "B T Hq D")])
     _check(load().paged_decode_attention_sink(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
         out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"], sz["N"], sz["M"], sz["T"], int(window), int(sinks),
-        ctypes.c_float(float(scale)), _stream_ptr(stream, q.get_device())))
+        ctypes.c_float(float(scale)), _stream_ptr(stream)))
     return out
 
 
@@ -529,11 +537,16 @@ def _kv4_groups(sz):
 
 
 def _kv4_tokens(call, k, v, names, cache, stream):
+    rc = (_nat or _load_native()).kv4_tokens(k, v, *cache, call == "pda_kv4_read", stream)
+    if rc == PDA_OK:
+        return
+    if rc != _DECLINED:
+        _check(rc)
     import torch
     sz = _validate([(names[0], k, torch.bfloat16, "B T Hkv D"), (names[1], v, torch.bfloat16, "B T Hkv D"), *_kv4_specs(*cache)])
     _kv4_groups(sz)
-    _check(call(k.data_ptr(), v.data_ptr(), *(t.data_ptr() for t in cache), sz["B"], sz["T"], sz["Hkv"], sz["D"], sz["P"],
-                sz["N"], sz["M"], _stream_ptr(stream, k.get_device())))
+    _check(getattr(load(), call)(k.data_ptr(), v.data_ptr(), *(t.data_ptr() for t in cache), sz["B"], sz["T"], sz["Hkv"],
+                                 sz["D"], sz["P"], sz["N"], sz["M"], _stream_ptr(stream)))
 
 
 def kv4_append(k_new, v_new, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, stream=None):
@@ -542,27 +555,33 @@ def kv4_append(k_new, v_new, k_codes, k_scales, v_codes, v_scales, block_table, 
 
     k_codes, v_codes: uint8 [N, Hkv, D / 32, P, 16]; k_scales, v_scales: uint8 [N, Hkv, D / 32, P]
     (:func:`kv4_cache`); include/pda.h states the format."""
-    _kv4_tokens(load().pda_kv4_append, k_new, v_new, ("k_new", "v_new"),
+    _kv4_tokens("pda_kv4_append", k_new, v_new, ("k_new", "v_new"),
                 (k_codes, k_scales, v_codes, v_scales, block_table, context_lens), stream)
 
 
 def kv4_read(k_out, v_out, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, stream=None):
     """The last T tokens of each sequence as the bf16 values they stand for -> k_out, v_out
     [B, T, Hkv, D]; positions before a sequence's first token give zeros."""
-    _kv4_tokens(load().pda_kv4_read, k_out, v_out, ("k_out", "v_out"),
+    _kv4_tokens("pda_kv4_read", k_out, v_out, ("k_out", "v_out"),
                 (k_codes, k_scales, v_codes, v_scales, block_table, context_lens), stream)
 
 
 def paged_decode_attention_kv4(q, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, out, scale, window=0,
                                sinks=0, stream=None):
     """:func:`paged_decode_attention_sink` over a 4-bit cache (:func:`kv4_append`): q, out bf16 [B, T, Hq, D]."""
+    rc = (_nat or _load_native()).attention_kv4(q, k_codes, k_scales, v_codes, v_scales, block_table, context_lens, out, scale,
+                                                window, sinks, stream)
+    if rc == PDA_OK:
+        return out
+    if rc != _DECLINED:
+        _check(rc)
     import torch
     cache = (k_codes, k_scales, v_codes, v_scales, block_table, context_lens)
     sz = _validate([("q", q, torch.bfloat16, "B T Hq D"), *_kv4_specs(*cache), ("out", out, torch.bfloat16, "B T Hq D")])
     _kv4_groups(sz)
     _check(load().paged_decode_attention_kv4(
         q.data_ptr(), *(t.data_ptr() for t in cache), out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"],
-        sz["N"], sz["M"], sz["T"], int(window), int(sinks), ctypes.c_float(float(scale)), _stream_ptr(stream, q.get_device())))
+        sz["N"], sz["M"], sz["T"], int(window), int(sinks), ctypes.c_float(float(scale)), _stream_ptr(stream)))
     return out
 
 
@@ -579,6 +598,12 @@ def pages_update(block_table, context_lens, parents, new_lens, refcount, table_o
     block_table int32 [B, M], context_lens [B], parents and new_lens [R], refcount [N] -> table_out
     [R, M], refcount_out [N], copy_src and copy_dst [R] (for :func:`pages_copy`), info [2]: fresh pages
     taken, and lacking.  include/pda.h states the rules."""
+    rc = (_nat or _load_native()).pages_update(block_table, context_lens, parents, new_lens, refcount, table_out, refcount_out,
+                                               copy_src, copy_dst, info, page_size, window, sinks, num_queries, stream)
+    if rc == PDA_OK:
+        return
+    if rc != _DECLINED:
+        _check(rc)
     import torch
     i32 = torch.int32
     sz = _validate([("block_table", block_table, i32, "B M"), ("context_lens", context_lens, i32, "B"),
@@ -589,13 +614,19 @@ def pages_update(block_table, context_lens, parents, new_lens, refcount, table_o
         block_table.data_ptr(), context_lens.data_ptr(), _ptr(parents), new_lens.data_ptr(), refcount.data_ptr(),
         table_out.data_ptr(), refcount_out.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), info.data_ptr(), sz["B"],
         sz["R"], int(page_size), sz["N"], sz["M"], int(num_queries), int(window), int(sinks),
-        _stream_ptr(stream, refcount.get_device())))
+        _stream_ptr(stream)))
 
 
 def pages_compact(block_table, context_lens, refcount, table_out, refcount_out, page_map, copy_src, copy_dst, info, page_size,
                   stream=None):
     """The live pages to the front of the pool: table_out, refcount_out and page_map [N] by the new
     numbers, the pages to move in copy_src and copy_dst [N], info [2]: live pages, and how many move."""
+    rc = (_nat or _load_native()).pages_compact(block_table, context_lens, refcount, table_out, refcount_out, page_map,
+                                                copy_src, copy_dst, info, page_size, stream)
+    if rc == PDA_OK:
+        return
+    if rc != _DECLINED:
+        _check(rc)
     import torch
     i32 = torch.int32
     sz = _validate([("block_table", block_table, i32, "B M"), ("context_lens", context_lens, i32, "B"),
@@ -605,13 +636,18 @@ def pages_compact(block_table, context_lens, refcount, table_out, refcount_out, 
     _check(load().pda_pages_compact(
         block_table.data_ptr(), context_lens.data_ptr(), refcount.data_ptr(), table_out.data_ptr(), refcount_out.data_ptr(),
         page_map.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), info.data_ptr(), sz["B"], int(page_size), sz["N"],
-        sz["M"], _stream_ptr(stream, refcount.get_device())))
+        sz["M"], _stream_ptr(stream)))
 
 
 def pages_copy(pools, copy_src, copy_dst, count=None, stream=None):
     """Page copy_dst[i] of every pool becomes a copy of page copy_src[i] (pairs with a negative entry
     are skipped; ``count`` int32 [1]: only the first ones).  ``pools``: tensors whose first dimension is
     the pages, every layer's K and V, of any type."""
+    rc = (_nat or _load_native()).pages_copy(pools, copy_src, copy_dst, count, stream)
+    if rc == PDA_OK:
+        return
+    if rc != _DECLINED:
+        _check(rc)
     import torch
     sz = _validate([("copy_src", copy_src, torch.int32, "C"), ("copy_dst", copy_dst, torch.int32, "C"),
                     ("count", count, torch.int32, "1")])
@@ -630,7 +666,7 @@ def pages_copy(pools, copy_src, copy_dst, count=None, stream=None):
         arr[i].data = t.data_ptr()
         arr[i].page_bytes = t.numel() // n * t.element_size() if n else 0
     _check(load().pda_pages_copy(arr, len(pools), copy_src.data_ptr(), copy_dst.data_ptr(), _ptr(count), sz["C"], n,
-                                 _stream_ptr(stream, dev)))
+                                 _stream_ptr(stream)))
 
 
 def pages_workspace_reserve(rows, num_pages, stream=None) -> None:

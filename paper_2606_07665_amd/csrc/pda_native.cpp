@@ -19,6 +19,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <vector>
 
 #include "pda.h"
 
@@ -35,6 +36,13 @@ struct Lib {
   decltype(&pda_attention_prelude) prelude = nullptr;
   decltype(&pda_attention_prelude_append) prelude_append = nullptr;
   decltype(&pda_o_proj_residual_norm) o_proj = nullptr;
+  decltype(&paged_decode_attention_sink) attention_sink = nullptr;
+  decltype(&paged_decode_attention_kv4) attention_kv4 = nullptr;
+  decltype(&pda_kv4_append) kv4_append = nullptr;
+  decltype(&pda_kv4_read) kv4_read = nullptr;
+  decltype(&pda_pages_update) pages_update = nullptr;
+  decltype(&pda_pages_compact) pages_compact = nullptr;
+  decltype(&pda_pages_copy) pages_copy = nullptr;
 } g_lib;
 PyObject* g_raw_stream = nullptr;  // torch._C._cuda_getCurrentRawStream
 PyObject* g_device = nullptr;      // torch._C._cuda_getDevice
@@ -117,7 +125,7 @@ struct Checker {
   }
 };
 
-const at::ScalarType kBf = at::ScalarType::BFloat16, kI32 = at::ScalarType::Int;
+const at::ScalarType kBf = at::ScalarType::BFloat16, kI32 = at::ScalarType::Int, kU8 = at::ScalarType::Byte;
 
 // k_cache, v_cache [N, P, Hkv, D], block_table [B, M], context_lens [B].
 struct Cache {
@@ -327,6 +335,186 @@ PyObject* o_proj(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   });
 }
 
+// (q, k, v, bt, lens, out, scale, window, sinks, stream); q [B, T, Hq, D]
+PyObject* attention_sink(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 10, [&]() -> int {
+    Checker c;
+    const at::Tensor* q = c.take(a[0], kBf, 4);
+    if (!c.ok) return kDeclined;
+    Cache kv(c, a + 1, q->size(0));
+    const at::Tensor* out = c.take(a[5], kBf, 4);
+    if (!c.ok) return kDeclined;
+    c.ok = out->sizes() == q->sizes();
+    const int32_t b = c.i32(q->size(0)), t = c.i32(q->size(1)), hq = c.i32(q->size(2)), d = c.i32(q->size(3));
+    c.same(kv.d, d);
+    const int32_t hkv = c.i32(kv.hkv), p = c.i32(kv.p), n = c.i32(kv.n), m = c.i32(kv.m);
+    const float scale = c.number(a[6]);
+    const int32_t window = c.integer(a[7]), sinks = c.integer(a[8]);
+    void* st = c.stream(a[9], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    void *qp = q->data_ptr(), *kp = kv.k->data_ptr(), *vp = kv.v->data_ptr(), *op = out->data_ptr();
+    int32_t *bp = ints(kv.bt), *lp = ints(kv.lens);
+    return released([&] { return g_lib.attention_sink(qp, kp, vp, bp, lp, op, b, hq, hkv, d, p, n, m, t, window, sinks, scale, st); });
+  });
+}
+
+// k codes, k scales, v codes, v scales, block_table [B, M], context_lens [B]
+struct Cache4 {
+  const at::Tensor* t[4];
+  const at::Tensor *bt, *lens;
+  int64_t n = 0, p = 0, hkv = 0, d = 0, m = 0;
+  Cache4(Checker& c, PyObject* const* a, int64_t batch) {
+    for (int i = 0; i < 4; ++i) t[i] = c.take(a[i], kU8, i % 2 ? 4 : 5);
+    bt = c.take(a[4], kI32, 2);
+    lens = c.take(a[5], kI32, 1);
+    if (!c.ok) return;
+    n = t[0]->size(0), hkv = t[0]->size(1), d = 32 * t[0]->size(2), p = t[0]->size(3), m = bt->size(1);
+    c.ok = t[2]->sizes() == t[0]->sizes() && t[3]->sizes() == t[1]->sizes();
+    c.same(t[0]->size(4), 16);
+    for (int i = 0; i < 4; ++i) c.same(t[1]->size(i), t[0]->size(i));
+    c.same(bt->size(0), batch);
+    c.same(lens->size(0), batch);
+  }
+  void* at(int i) const { return t[i]->data_ptr(); }
+};
+
+// (q, k codes, k scales, v codes, v scales, bt, lens, out, scale, window, sinks, stream); q [B, T, Hq, D]
+PyObject* attention_kv4(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 12, [&]() -> int {
+    Checker c;
+    const at::Tensor* q = c.take(a[0], kBf, 4);
+    if (!c.ok) return kDeclined;
+    Cache4 kv(c, a + 1, q->size(0));
+    const at::Tensor* out = c.take(a[7], kBf, 4);
+    if (!c.ok) return kDeclined;
+    c.ok = out->sizes() == q->sizes();
+    const int32_t b = c.i32(q->size(0)), t = c.i32(q->size(1)), hq = c.i32(q->size(2)), d = c.i32(q->size(3));
+    c.same(kv.d, d);
+    const int32_t hkv = c.i32(kv.hkv), p = c.i32(kv.p), n = c.i32(kv.n), m = c.i32(kv.m);
+    const float scale = c.number(a[8]);
+    const int32_t window = c.integer(a[9]), sinks = c.integer(a[10]);
+    void* st = c.stream(a[11], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    void *qp = q->data_ptr(), *op = out->data_ptr(), *kp = kv.at(0), *ksp = kv.at(1), *vp = kv.at(2), *vsp = kv.at(3);
+    int32_t *bp = ints(kv.bt), *lp = ints(kv.lens);
+    return released([&] {
+      return g_lib.attention_kv4(qp, kp, ksp, vp, vsp, bp, lp, op, b, hq, hkv, d, p, n, m, t, window, sinks, scale, st);
+    });
+  });
+}
+
+// (k, v, k codes, k scales, v codes, v scales, bt, lens, read, stream); k, v [B, T, Hkv, D]: the new
+// tokens, or with `read` True what they are read to
+PyObject* kv4_tokens(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 10, [&]() -> int {
+    Checker c;
+    const at::Tensor* k = c.take(a[0], kBf, 4);
+    const at::Tensor* v = c.take(a[1], kBf, 4);
+    if (!c.ok) return kDeclined;
+    Cache4 kv(c, a + 2, k->size(0));
+    if (!c.ok) return kDeclined;
+    c.ok = v->sizes() == k->sizes();
+    const int32_t b = c.i32(k->size(0)), t = c.i32(k->size(1)), hkv = c.i32(kv.hkv), d = c.i32(kv.d);
+    c.same(k->size(2), kv.hkv);
+    c.same(k->size(3), kv.d);
+    const int32_t p = c.i32(kv.p), n = c.i32(kv.n), m = c.i32(kv.m);
+    const bool read = a[8] == Py_True;
+    void* st = c.stream(a[9], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    void *k_p = k->data_ptr(), *v_p = v->data_ptr(), *kp = kv.at(0), *ksp = kv.at(1), *vp = kv.at(2), *vsp = kv.at(3);
+    int32_t *bp = ints(kv.bt), *lp = ints(kv.lens);
+    return released([&] {
+      return read ? g_lib.kv4_read(k_p, v_p, kp, ksp, vp, vsp, bp, lp, b, t, hkv, d, p, n, m, st)
+                  : g_lib.kv4_append(k_p, v_p, kp, ksp, vp, vsp, bp, lp, b, t, hkv, d, p, n, m, st);
+    });
+  });
+}
+
+// (block_table, lens, parents or None, new_lens, refcount, table_out, refcount_out, src, dst, info,
+//  page_size, window, sinks, num_queries, stream)
+PyObject* pages_update(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 15, [&]() -> int {
+    Checker c;
+    const at::Tensor* t[10];
+    for (int i = 0; i < 10; ++i) t[i] = i == 2 && a[2] == Py_None ? nullptr : c.take(a[i], kI32, i == 0 || i == 5 ? 2 : 1);
+    if (!c.ok) return kDeclined;
+    const int64_t b = t[0]->size(0), m = t[0]->size(1), r = t[3]->size(0), n = t[4]->size(0);
+    c.same(t[1]->size(0), b);
+    if (t[2]) c.same(t[2]->size(0), r);
+    c.same(t[5]->size(0), r);
+    c.same(t[5]->size(1), m);
+    c.same(t[6]->size(0), n);
+    c.same(t[7]->size(0), r);
+    c.same(t[8]->size(0), r);
+    c.same(t[9]->size(0), 2);
+    const int32_t page = c.integer(a[10]), window = c.integer(a[11]), sinks = c.integer(a[12]), nq = c.integer(a[13]);
+    const int32_t bi = c.i32(b), mi = c.i32(m), ri = c.i32(r), ni = c.i32(n);
+    void* st = c.stream(a[14], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    int32_t* p[10];
+    for (int i = 0; i < 10; ++i) p[i] = t[i] ? ints(t[i]) : nullptr;
+    return released([&] {
+      return g_lib.pages_update(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], bi, ri, page, ni, mi, nq, window,
+                                sinks, st);
+    });
+  });
+}
+
+// (block_table, lens, refcount, table_out, refcount_out, page_map, src, dst, info, page_size, stream)
+PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 11, [&]() -> int {
+    Checker c;
+    const at::Tensor* t[9];
+    for (int i = 0; i < 9; ++i) t[i] = c.take(a[i], kI32, i == 0 || i == 3 ? 2 : 1);
+    if (!c.ok) return kDeclined;
+    const int64_t b = t[0]->size(0), m = t[0]->size(1), n = t[2]->size(0);
+    c.same(t[1]->size(0), b);
+    c.ok = c.ok && t[3]->sizes() == t[0]->sizes();
+    for (int i = 4; i < 8; ++i) c.same(t[i]->size(0), n);
+    c.same(t[8]->size(0), 2);
+    const int32_t page = c.integer(a[9]), bi = c.i32(b), mi = c.i32(m), ni = c.i32(n);
+    void* st = c.stream(a[10], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    int32_t* p[9];
+    for (int i = 0; i < 9; ++i) p[i] = ints(t[i]);
+    return released(
+        [&] { return g_lib.pages_compact(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], bi, page, ni, mi, st); });
+  });
+}
+
+// (pools, src, dst, count or None, stream); pools: a list or tuple of tensors of any type
+PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 5, [&]() -> int {
+    if (!PyList_CheckExact(a[0]) && !PyTuple_CheckExact(a[0])) return kDeclined;
+    const Py_ssize_t k = PySequence_Fast_GET_SIZE(a[0]);
+    PyObject** items = PySequence_Fast_ITEMS(a[0]);
+    Checker c;
+    const at::Tensor* src = c.take(a[1], kI32, 1);
+    const at::Tensor* dst = c.take(a[2], kI32, 1);
+    const at::Tensor* count = a[3] != Py_None ? c.take(a[3], kI32, 1) : nullptr;
+    if (!c.ok || k == 0) return kDeclined;
+    c.same(dst->size(0), src->size(0));
+    if (count) c.same(count->size(0), 1);
+    std::vector<pda_pool> pools(static_cast<size_t>(k));
+    int64_t n = 0;
+    for (Py_ssize_t i = 0; i < k && c.ok; ++i) {
+      if (!THPVariable_CheckExact(items[i])) return kDeclined;
+      const at::Tensor& t = THPVariable_Unpack(items[i]);
+      if (!t.defined() || t.dim() < 2 || !t.is_cuda() || !t.is_contiguous() || t.get_device() != c.device) return kDeclined;
+      if (i == 0) n = t.size(0);
+      c.same(t.size(0), n);
+      if (!c.ok || n == 0) return kDeclined;
+      pools[i].data = t.data_ptr();
+      pools[i].page_bytes = t.numel() / n * t.element_size();
+    }
+    const int32_t ki = c.i32(k), ni = c.i32(n), most = c.i32(src->size(0));
+    void* st = c.stream(a[4], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    int32_t *sp = ints(src), *dp = ints(dst), *cp = count ? ints(count) : nullptr;
+    return released([&] { return g_lib.pages_copy(pools.data(), ki, sp, dp, cp, most, ni, st); });
+  });
+}
+
 // ({name: address}, raw_stream, device): the loaded library's entry points,
 // torch's current raw stream of a device and its current device
 PyObject* init(PyObject*, PyObject* args) {
@@ -347,7 +535,10 @@ PyObject* init(PyObject*, PyObject* args) {
       !set("paged_decode_attention_append", g_lib.attention_append) || !set("pda_kv_append_n", g_lib.kv_append_n) ||
       !set("pda_attention_prelude", g_lib.prelude) ||
       !set("pda_attention_prelude_append", g_lib.prelude_append) ||
-      !set("pda_o_proj_residual_norm", g_lib.o_proj))
+      !set("pda_o_proj_residual_norm", g_lib.o_proj) || !set("paged_decode_attention_sink", g_lib.attention_sink) ||
+      !set("paged_decode_attention_kv4", g_lib.attention_kv4) || !set("pda_kv4_append", g_lib.kv4_append) ||
+      !set("pda_kv4_read", g_lib.kv4_read) || !set("pda_pages_update", g_lib.pages_update) ||
+      !set("pda_pages_compact", g_lib.pages_compact) || !set("pda_pages_copy", g_lib.pages_copy))
     return nullptr;
   Py_INCREF(raw);
   Py_XDECREF(g_raw_stream);
@@ -360,6 +551,8 @@ PyObject* init(PyObject*, PyObject* args) {
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(attention), FAST(kv_append), FAST(attention_append), FAST(prelude), FAST(o_proj),
+                          FAST(attention_sink), FAST(attention_kv4), FAST(kv4_tokens), FAST(pages_update),
+                          FAST(pages_compact), FAST(pages_copy),
                           {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "pda_native", "Native marshalling of the binding's hot calls.", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
