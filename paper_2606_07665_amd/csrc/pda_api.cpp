@@ -194,6 +194,14 @@ int heads_per_group(int hkv, int max_waves) {
   return 1;
 }
 
+// The same for workgroups of more than 8 waves, of which at least three in
+// four should have work: 8 heads go to 12 waves as 4 heads x 3 step phases.
+int heads_of_waves(int hkv, int max_waves, int most) {
+  for (int d = std::min(max_waves, most); d > 1; --d)
+    if (hkv % d == 0 && 4 * d * (max_waves / d) >= 3 * max_waves) return d;
+  return 1;
+}
+
 // What the planner has to know of the kernel that a plan is for.
 struct Form {
   int max_waves;        // waves of a workgroup at most
@@ -202,7 +210,18 @@ struct Form {
   bool options;         // the compute path and the fused merge apply
 };
 Form bf16_form(int d, bool sinks = false) { return {pda::max_waves(d), 1, static_cast<int64_t>(d) * 4, !sinks}; }
-Form kv4_form(int d) { return {pda::kv4_max_waves(d), pda::kKv4WorkgroupsPerCu, static_cast<int64_t>(d) * 17 / 16, false}; }
+// Workgroups of 4 waves, as many as fill a CU's registers, where their LDS (the
+// tiles, and the prefix over the batch) allows it; one of all the waves, or
+// what fits, where it does not.
+Form kv4_form(int d, int batch) {
+  int waves = 4, per_cu = pda::kv4_max_waves(d) / 4;
+  if (per_cu * pda::kv4_attn_lds_bytes(d, batch, waves) > static_cast<size_t>(pda::kMaxLdsBytes)) {
+    per_cu = 1;
+    for (waves = pda::kv4_max_waves(d); waves > 4; waves -= 4)
+      if (pda::kv4_attn_lds_bytes(d, batch, waves) <= static_cast<size_t>(pda::kMaxLdsBytes)) break;
+  }
+  return {waves, per_cu, static_cast<int64_t>(d) * 17 / 16, false};
+}
 
 // Workgroups: one wave per kv head of a group of hgs, times step phases up
 // to max_waves waves (8; 4 at D = 256); as many workgroups as fill the
@@ -316,8 +335,8 @@ Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, in
   // columns or fewer, run slower with 4).
   const int dflt_most = cols > 8 ? std::min(4, form.max_waves) : form.max_waves;
   const int most = cap > 0 && cap < form.max_waves ? cap : dflt_most;
-  Plan dflt = plan_for(form, heads_per_group(hkv, most), batch, hkv, d, steps_seq, num_cus, cols,
-                       ms_opt > 0 ? ms_opt : kDefaultMinSteps);
+  const int together = form.max_waves > 8 ? heads_of_waves(hkv, form.max_waves, most) : heads_per_group(hkv, most);
+  Plan dflt = plan_for(form, together, batch, hkv, d, steps_seq, num_cus, cols, ms_opt > 0 ? ms_opt : kDefaultMinSteps);
   // Small calls (each 32-token step's K and V is a few KB; the whole call
   // is a chain of latencies):
   //  - a plan that splits the work but leaves CUs idle gives each wave one
@@ -977,7 +996,7 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
   if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
   int cus = 0;
   if ((rc = device_cus(dev, &cus))) return rc;
-  const Form form = kv4 ? kv4_form(head_dim) : bf16_form(head_dim, sinks > 0);
+  const Form form = kv4 ? kv4_form(head_dim, batch) : bf16_form(head_dim, sinks > 0);
   const Plan pl = make_plan(form, batch, num_kv_heads, head_dim,
                             most_steps(page_size, max_pages_per_seq, num_queries, window, sinks), cus, cols);
   const size_t lds = kv4 ? pda::kv4_attn_lds_bytes(head_dim, batch, pl.waves)
@@ -1113,7 +1132,7 @@ int reserve_attention(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, 
   int cus = 0;
   if ((rc = device_cus(dev, &cus))) return rc;
   void* ptr = nullptr;
-  const int64_t need = workspace_bytes(kv4 ? kv4_form(head_dim) : bf16_form(head_dim), batch, num_kv_heads, head_dim,
+  const int64_t need = workspace_bytes(kv4 ? kv4_form(head_dim, batch) : bf16_form(head_dim), batch, num_kv_heads, head_dim,
                                        page_size, max_pages_per_seq, cus, pda::kMaxCols);
   if ((rc = workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr))) return rc;
   if (kv4) return PDA_OK;  // (no fused merge, so no counters)

@@ -30,8 +30,7 @@ hipError_t launch_kv4_read(const Kv4Args& a, uint16_t* k_out, uint16_t* v_out, h
 // which `c` names (a.k and a.v are not read).
 hipError_t launch_kv4_attn(const LaunchArgs& a, const Kv4Args& c, hipStream_t st);
 size_t kv4_attn_lds_bytes(int head_dim, int batch, int waves);
-// Waves of a workgroup at most, and the workgroups of a CU that run together.
-constexpr int kv4_max_waves(int head_dim) { return head_dim == 256 ? 4 : 8; }
-constexpr int kKv4WorkgroupsPerCu = 2;
+// Waves of a CU: 12 leave a wave 168 registers, 8 (D = 256) 256.
+constexpr int kv4_max_waves(int head_dim) { return head_dim == 256 ? 8 : 12; }
 
 }  // namespace pda

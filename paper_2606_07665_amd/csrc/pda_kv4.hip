@@ -135,10 +135,15 @@ __global__ __launch_bounds__(kKv4Threads) void kv4_read_kernel(Kv4Args a, uint16
 }
 
 // --------------------------------------------------------------- attention
+typedef const __attribute__((address_space(1))) uint8_t global_u8;
+typedef const __attribute__((address_space(1))) u32x4 global_u32x4;
+
 template <int D>
 struct Shape4 {
-  static constexpr int kParts = D == 256 ? 2 : 1;      // loads of codes per 16-token tile (K and V each)
-  static constexpr int kWords = D == 64 ? 2 : 4;       // 32-bit words of codes per load and lane
+  static constexpr int kParts = D == 256 ? 2 : 1;      // 128-wide parts of a key (K's loads and products per tile)
+  static constexpr int kQK = D / 32;                   // products of K and q per tile
+  static constexpr int kVLoads = D / 64;               // 16-byte loads per lane of a step's V
+  static constexpr int kRing = 2;                      // steps of loads in flight per wave
   static constexpr int kDT = D / 16;                   // 16-wide d tiles of the output
   static constexpr int kRowBytes = 2 * D + 32;         // a V row in LDS, padded as in the bf16 kernel
   static constexpr int kTileBytes = kStep * kRowBytes;
@@ -150,17 +155,17 @@ __host__ __device__ constexpr int ml_offset4(int waves) { return waves * Shape4<
 template <int D>
 __host__ __device__ constexpr int pref_offset4(int waves) { return ml_offset4<D>(waves) + waves * 16 * 2 * 4; }
 
+// What is not a pointer: those are arguments of their own, so that the compiler
+// knows what is only read and takes page ids through the scalar cache.
 struct Attn4 {
-  const uint16_t* q;
-  const uint8_t *k, *ks, *v, *vs;
-  const int32_t *bt, *lens;
-  uint16_t* out;
-  float *ws_acc, *ws_ml;
-  int32_t* ws_pref;
   int batch, hq, hkv, group, hgs, page_shift, num_pages, maxp, min_steps, nq, window, sinks, chunks, chunk_steps;
-  float scale;  // in log2 units, >= 0
-  unsigned flip;  // 0x80008000 where the caller's scale is negative: q's signs are turned
+  float scale;  // in log2 units, > 0
+  // q as the products take it: its bits and `keep`, then exclusive or `flip`:
+  // the signs turned for a negative scale, zeros (and a scale of 1) for a zero
+  unsigned keep, flip;
 };
+
+constexpr float kLazy = 8.f;  // see the online softmax
 
 // One pass over the cache with the split, the columns and the partials of the
 // bf16 kernel (pda_kernels.hip): a wave takes 32-token steps of one kv head,
@@ -170,11 +175,30 @@ struct Attn4 {
 //    16-token tile.  Converted, its four runs of 8 elements are the A operand
 //    of four v_mfma_f32_16x16x32_bf16 as they stand, since the order of d
 //    inside a product is free as long as q's operand has the same: K does not
-//    pass through LDS.
+//    pass through LDS.  (The matrix cores also multiply E2M1 codes with their
+//    scales directly, q as two E4M3 parts: 32 conversions a step fewer, the
+//    same time, and scores off by ~2^-15 of themselves, which is why not.)
 //  * V: loaded the same way, converted with its scales to bf16 rows in LDS
 //    and read back transposed, as in the bf16 kernel.
+//
+// A quarter of the bf16 kernel's bytes leaves a step ~1300 cycles of a SIMD at
+// 7 TB/s, and it takes ~160 vector, 32 matrix and 25 LDS instructions: the time
+// goes where a wave waits.  So:
+//  * 12 waves a CU (3 a SIMD, 168 registers each), each with the loads of two
+//    steps in flight, as three workgroups of 4 waves where the prefix over the
+//    batch leaves LDS for them: one takes up its next sequence while the others
+//    stream.  4 x 131072 tokens, 64:8 heads: 16 waves with one step in flight
+//    and vector page ids 131 us a call, scalar page ids 115, 8 waves with four
+//    steps 120, 12 waves with two 107; a batch of 64, U[128, 8192] at 32:8
+//    heads: 85, 70, 75, 63; loads alone, nothing computed: 97 and 54 + the merge.
+//  * every loop value that is the same for the wave is kept in scalar registers
+//    (divisions and LDS reads leave theirs in vector ones).
 template <int D, bool kFixed>
-__global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv4_max_waves(D) / 8) void attn4_kernel(Attn4 p) {
+__global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void attn4_kernel(
+    const uint16_t* __restrict__ q, const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_scales,
+    const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_scales, const int32_t* __restrict__ bt,
+    const int32_t* __restrict__ lens, uint16_t* __restrict__ out, float* __restrict__ ws_acc, float* __restrict__ ws_ml,
+    int32_t* __restrict__ ws_pref, Attn4 p) {
   using S = Shape4<D>;
   extern __shared__ __align__(16) unsigned char smem[];
   const int nthreads = blockDim.x;
@@ -190,13 +214,18 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
   const int tid = threadIdx.x;
   const int page = 1 << p.page_shift;
   const int max_ctx = p.maxp << p.page_shift;
-  const int extra = (phases > 1 || D == 256) ? phases : 0;
-  auto extent = [&](int steps) { return steps + (steps > 0 && steps < 8 * phases ? extra : 0); };
+  // What a sequence counts for in the stream-K ranges: its steps, and four for
+  // each step phase ahead of them, for taking up another piece (page ids, then
+  // the first loads, q's operand, the exchange of the phases: ~5 us of a
+  // workgroup, where a step takes 1.5).  Batches of 101 (Zipf) and 64 (uniform)
+  // sequences: 168 and 62 us without, 139 and 59 with two, 124 and 59 with four.
+  const int extra = 4 * phases;
+  auto extent = [&](int steps) { return steps + (steps > 0 ? extra : 0); };
 
   if constexpr (!kFixed) {
     // prefix over the batch of what each sequence counts for
 #pragma unroll 8
-    for (int b = tid; b < p.batch; b += nthreads) lens_s[b] = clamp_len(p.lens[b], max_ctx);
+    for (int b = tid; b < p.batch; b += nthreads) lens_s[b] = clamp_len(lens[b], max_ctx);
     __syncthreads();
     const int per = (p.batch + nthreads - 1) / nthreads;
     const int lo = tid * per;
@@ -221,7 +250,7 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
     if (tid == nthreads - 1) pref[p.batch] = before + incl;
     __syncthreads();
     if (blockIdx.x == 0) {  // the merge kernel's copy, and the zero rows of empty sequences
-      for (int b = tid; b <= p.batch; b += nthreads) p.ws_pref[b] = pref[b];
+      for (int b = tid; b <= p.batch; b += nthreads) ws_pref[b] = pref[b];
       const int row16 = nq * p.hq * D / 8;
       const int ln = tid & 63;
       for (int c = (tid >> 6) * 64; c < p.batch; c += nwaves * 64) {
@@ -229,7 +258,7 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
         while (empty) {
           const int j = __builtin_ctzll(empty);
           empty &= empty - 1;
-          u32x4* orow = reinterpret_cast<u32x4*>(p.out + static_cast<int64_t>(c + j) * nq * p.hq * D);
+          u32x4* orow = reinterpret_cast<u32x4*>(out + static_cast<int64_t>(c + j) * nq * p.hq * D);
           for (int i = ln; i < row16; i += 64) orow[i] = u32x4{0u, 0u, 0u, 0u};
         }
       }
@@ -239,14 +268,14 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
 
   const int lane = tid & 63;
   const int wid = uniform(tid >> 6);
-  const int hi_w = wid % hgs;  // kv head of this wave within the group
-  const int ph = wid / hgs;    // step phase of this wave
+  const int hi_w = uniform(wid % hgs);  // kv head of this wave within the group
+  const int ph = uniform(wid / hgs);    // step phase of this wave
   const int g4 = lane >> 4;    // lane group: MFMA k block / C row block
   const int c = lane & 15;     // MFMA row (A) / column (B, C)
   const int qj = c < ncols ? c / group : nq - 1;
   const int qh = c - (c / group) * group;
   const int blk = blockIdx.x;
-  int32_t* ws_split = p.ws_pref + p.batch + 1;
+  int32_t* ws_split = ws_pref + p.batch + 1;
 
   int b, hg, s0, nb;
   int64_t x = 0, xend, total = 1, beff = 1;
@@ -255,13 +284,13 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
     b = div_small_u(e, ngroups);
     hg = e - b * ngroups;
     s0 = (blk - e * p.chunks) * p.chunk_steps;
-    nb = seq_steps(clamp_len(uniform(p.lens[b]), max_ctx), nq, window, sinks);
+    nb = seq_steps(clamp_len(uniform(lens[b]), max_ctx), nq, window, sinks);
     if (s0 >= nb) {  // a chunk past the sequence's end
       if (nb == 0 && s0 == 0) {  // an empty sequence: zero rows
         const int row16 = hgs * group * D / 8;
         for (int j = 0; j < nq; ++j) {
           u32x4* orow = reinterpret_cast<u32x4*>(
-              p.out + ((static_cast<int64_t>(b) * nq + j) * p.hq + hg * hgs * group) * D);
+              out + ((static_cast<int64_t>(b) * nq + j) * p.hq + hg * hgs * group) * D);
           for (int i = tid; i < row16; i += nthreads) orow[i] = u32x4{0u, 0u, 0u, 0u};
         }
       }
@@ -269,7 +298,7 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
     }
     xend = nb - s0 < p.chunk_steps ? nb - s0 : p.chunk_steps;
   } else {
-    total = static_cast<int64_t>(pref[p.batch]) * ngroups;
+    total = static_cast<int64_t>(uniform(pref[p.batch])) * ngroups;
     const int64_t per_block_min = static_cast<int64_t>(p.min_steps) * phases;
     beff = (total + per_block_min - 1) / per_block_min;
     beff = beff < gridDim.x ? beff : gridDim.x;
@@ -293,20 +322,26 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
     if (tid == 0) ws_split[blk] = (s0 > 0 && owner_of(x - s0, total, beff) == blk - 1) ? b * ngroups + hg : -1;
   }
 
+  int left = static_cast<int>(xend - x);  // steps of the workgroup (fewer than 2^31: a call has no more)
   unsigned char* tile = smem + wid * S::kTileBytes;
-  const int64_t head_bytes = static_cast<int64_t>(D / 2) << p.page_shift;  // codes of a kv head's page
-  const int64_t head_scales = static_cast<int64_t>(D / kKv4Group) << p.page_shift;
-  // this lane's codes and scale within a tile: token c, group g4 (and g4 + 4
-  // at D = 256; at D = 64 half a group)
-  const int grp0 = D == 64 ? g4 >> 1 : g4;
-  const int soff = (grp0 << p.page_shift) + c;
-  const int coff = 16 * soff + (D == 64 ? 8 * (g4 & 1) : 0);
-  const int dof = D == 64 ? 16 * g4 : 32 * g4;  // d of the lane's first element
+  const int head_bytes = (D / 2) << p.page_shift;  // codes of a kv head's page; its scales: head_bytes / 16
+  const unsigned page_bytes = static_cast<unsigned>(head_bytes) * p.hkv;  // at most 2^27
+  // K: this lane's codes and scale within a tile: token c, group g4 (and g4 + 4
+  // at D = 256; at D = 64 lanes g4 and g4 + 2 share a group, half each)
+  const unsigned ksoff = ((D == 64 ? g4 & 1 : g4) << p.page_shift) + c;
+  const int dof = D == 64 ? 32 * (g4 & 1) + 16 * (g4 >> 1) : 32 * g4;  // its first d
+  // V: load i takes token c of tile vtile(i), group vgrp(i)
+  auto vtile = [&](int i) { return D == 64 ? g4 >> 1 : D == 256 ? i >> 1 : i; };
+  auto vgrp = [&](int i) { return D == 64 ? g4 & 1 : D == 256 ? g4 + 4 * (i & 1) : g4; };
 
   while (true) {
-    const int64_t remaining = xend - x;
-    const int s1 = remaining < nb - s0 ? s0 + static_cast<int>(remaining) : nb;
-    const int L = uniform(kFixed ? clamp_len(p.lens[b], max_ctx) : lens_s[b]);
+    b = uniform(b);
+    hg = uniform(hg);
+    s0 = uniform(s0);
+    nb = uniform(nb);
+    left = uniform(left);
+    const int s1 = left < nb - s0 ? s0 + left : nb;
+    const int L = uniform(kFixed ? clamp_len(lens[b], max_ctx) : lens_s[b]);
     const int npages = (L + page - 1) >> p.page_shift;
     const int lo_seq = uniform(seq_start(L, nq, window));
     const int pinned = window > 0 ? min(sinks, lo_seq) : 0;  // keys [0, pinned) are seen as sinks
@@ -314,76 +349,88 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
     const int sb = lo_seq / kStep - nsink;  // absolute step of index i >= nsink: i + sb
     const int lead = kFixed ? 0 : nb - seq_steps(L, nq, window, sinks);
     const int t0 = max(s0 - lead, 0), t1 = max(s1 - lead, 0);
-    const int hi_c = L - nq + 1 + qj;  // this column sees keys [lo_c, hi_c) and [0, sinks)
+    // The wave's steps of the piece: sw, sw + phases, ...  One with none takes a
+    // step all the same, of a sequence of no tokens: everything in it is masked
+    // (skipping it cost the loop 60 registers in spills).
+    const int sw = uniform(t0 + ph);
+    const int steps = sw < t1 ? (t1 - sw + phases - 1) / phases : 0;
+    const int nsteps = uniform(steps > 0 ? steps : 1);
+    const int Lw = steps > 0 ? L : 0;
+    const int hi_c = Lw - nq + 1 + qj;  // this column sees keys [lo_c, hi_c) and [0, min(hi_c, sinks))
     const int lo_c = window > 0 ? max(0, hi_c - window) : 0;
-    const int hi_min = L - nq + 1;
-    const int lo_max = window > 0 ? max(0, L - window) : 0;
-    const int32_t* bt_row = p.bt + static_cast<int64_t>(b) * p.maxp;
-    const int g = hg * hgs + hi_w;
+    const int hi_min = Lw - nq + 1;
+    const int lo_max = window > 0 ? max(0, Lw - window) : 0;
+    const int32_t* bt_row = bt + static_cast<int64_t>(b) * p.maxp;
+    const int g = uniform(hg * hgs + hi_w);
 
-    bf16x8 qop[D / 32];
-    {
-      const uint16_t* qrow = p.q + ((static_cast<int64_t>(b) * nq + qj) * p.hq + g * group + qh) * D + dof;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if (c < ncols) w = ld16(qrow + (D == 256 ? 128 * (i >> 2) + 8 * (i & 3) : 8 * i)) ^ p.flip;
-        qop[i] = __builtin_bit_cast(bf16x8, w);
-      }
-    }
     f32x4 acc[S::kDT];
 #pragma unroll
     for (int dt = 0; dt < S::kDT; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -__builtin_inff();
-    float l_lane = 0.f;
+    f32x4 l_acc = {0.f, 0.f, 0.f, 0.f};  // the column's sum of probabilities, in every row
 
-    const int sw = t0 + ph;
-    const int nsteps = sw < t1 ? (t1 - sw + phases - 1) / phases : 0;
-    auto token_of = [&](int k) {  // first token of the wave's k-th step (clamped to its last)
-      k = k < nsteps ? k : nsteps - 1;
-      const int i = sw + k * phases;
+    // first token of the wave's k-th step (clamped to its last)
+    auto token_of = [&](int k) {
+      const int i = sw + (k < nsteps ? k : nsteps - 1) * phases;
       return (i < nsink ? i : i + sb) * kStep;
     };
-    struct Codes {
-      unsigned w[2][S::kParts][S::kWords];  // [tile][part][word]
-      unsigned s[2][S::kParts];
+    // page ids of the two tiles of the step at token t
+    auto load_pids = [&](int t, int& pa, int& pb) {
+      const int ja = t >> p.page_shift, jb = (t + 16) >> p.page_shift;
+      pa = bt_row[ja < npages ? ja : npages - 1];
+      pb = bt_row[jb < npages ? jb : npages - 1];
     };
-    // page ids of a step's two tiles
-    auto load_pids = [&](int k, int& pa, int& pb) {
-      const int t = token_of(k);
-      int ja = t >> p.page_shift, jb = (t + 16) >> p.page_shift;
-      ja = ja < npages ? ja : npages - 1;
-      jb = jb < npages ? jb : npages - 1;
-      pa = bt_row[ja];
-      pb = bt_row[jb];
+    // Where a tile's codes lie from the head's first page on (its scales: a
+    // sixteenth of that).  A tile that no query sees -- past the end, or between
+    // the sinks and the window, where its page may have been released -- is
+    // read from the page that its id is clamped to and masked: that is at most
+    // two tiles a piece, and spares every other one a descriptor.
+    auto tile_at = [&](int t, int id) {
+      const unsigned raw = static_cast<unsigned>(uniform(id));
+      const unsigned pid = raw < static_cast<unsigned>(p.num_pages) ? raw : p.num_pages - 1;
+      return static_cast<uint64_t>(pid) * page_bytes + 16 * (t & (page - 1));
     };
-    auto load = [&](int k, int pa, int pb, const uint8_t* codes, const uint8_t* scales, Codes& r) {
-      const int t = token_of(k);
+    const uint8_t* kg = k_codes + static_cast<int64_t>(g) * head_bytes;
+    const uint8_t* vg = v_codes + static_cast<int64_t>(g) * head_bytes;
+    const uint8_t* ksg = k_scales + static_cast<int64_t>(g) * (head_bytes >> 4);
+    const uint8_t* vsg = v_scales + static_cast<int64_t>(g) * (head_bytes >> 4);
+    const unsigned part = 4u << p.page_shift;  // scales between the 128-wide parts of a key
+    // a scalar base and a 32-bit offset per lane, as the loads take them (left
+    // to itself the compiler adds the tile's place to a pointer per lane)
+    auto at_scalar = [](const uint8_t* x) {
+      asm volatile("" : "+s"(x));
+      return (global_u8*)x;
+    };
+    struct Set {  // a step's codes and scales
+      u32x4 kw[2][S::kParts], vw[S::kVLoads];
+      unsigned ks[2][S::kParts], vs[S::kVLoads];
+    };
+    // Loads of a step past the wave's last have `only` = 0: every lane asks for
+    // the first 16 bytes of the last step's tile, one request instead of a
+    // branch (at whose join the compiler would wait for the path with fewer
+    // loads in flight).
+    auto load_k = [&](const uint64_t (&at)[2], unsigned only, Set& r) {
+      const unsigned o = ksoff & only;
 #pragma unroll
-      for (int T = 0; T < 2; ++T) {
-        const int tt = t + 16 * T;
-        // a tile past the end, or wholly between the sinks and the window (its
-        // page may have been released), is not read
-        const bool dead = k >= nsteps || tt >= L || (tt >= pinned && tt + 16 <= lo_seq);
-        const unsigned raw = static_cast<unsigned>(uniform(T ? pb : pa));
-        const int64_t pid = raw < static_cast<unsigned>(p.num_pages) ? raw : p.num_pages - 1;
-        const int slot = tt & (page - 1);
-        const int64_t hp = pid * p.hkv + g;
-        const __amdgpu_buffer_rsrc_t rc = page_rsrc(codes + hp * head_bytes + 16 * slot, dead ? 0 : static_cast<int>(head_bytes) - 16 * slot);
-        const __amdgpu_buffer_rsrc_t rs = page_rsrc(scales + hp * head_scales + slot, dead ? 0 : static_cast<int>(head_scales) - slot);
+      for (int T = 0; T < 2; ++T)
 #pragma unroll
         for (int i = 0; i < S::kParts; ++i) {
-          const int po = 4 * i << p.page_shift;
-          if constexpr (S::kWords == 4) {
-            const u32x4 w = ld16_stream(rc, coff + 16 * po);
+          r.kw[T][i] = __builtin_nontemporal_load((global_u32x4*)(at_scalar(kg + at[T] + 16 * i * part) + 16 * o));
+          r.ks[T][i] = at_scalar(ksg + (at[T] >> 4) + i * part)[o];
+        }
+    };
+    auto load_v = [&](const uint64_t (&at)[2], unsigned only, Set& r) {
+      const unsigned o = ksoff & only;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r.w[T][i][j] = w[j];
-          } else {
-            const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(rc, coff, 0, kCachePolicyNT);
-            r.w[T][i][0] = w[0];
-            r.w[T][i][1] = w[1];
-          }
-          r.s[T][i] = __builtin_amdgcn_raw_buffer_load_b8(rs, soff + po, 0, 0);
+      for (int i = 0; i < S::kVLoads; ++i) {
+        if constexpr (D == 64) {  // a lane for each token of the step and group
+          const uint64_t from = g4 >> 1 ? at[1] : at[0];
+          r.vw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vg + from + 16 * o));
+          r.vs[i] = (vsg + (from >> 4))[o];
+        } else {
+          const int T = D == 256 ? i >> 1 : i, h = D == 256 ? i & 1 : 0;
+          r.vw[i] = __builtin_nontemporal_load((global_u32x4*)(at_scalar(vg + at[T] + 16 * h * part) + 16 * o));
+          r.vs[i] = at_scalar(vsg + (at[T] >> 4) + h * part)[o];
         }
       }
     };
@@ -393,90 +440,124 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
 
-    if (nsteps > 0) {
-      Codes kr, vr;
-      int pa, pb, pa1, pb1;
-      load_pids(0, pa, pb);
-      load_pids(1, pa1, pb1);
-      load(0, pa, pb, p.k, p.ks, kr);
-      load(0, pa, pb, p.v, p.vs, vr);
-      for (int k = 0; k < nsteps; ++k) {
+    // Loads run kRing steps ahead: a set's registers are loaded again as soon as
+    // its step has used them, K after the products with q, V after its rows are
+    // in LDS.  Page ids (scalar loads) run one step further.
+    Set ring[S::kRing];
+    int pa, pb;
+#pragma unroll
+    for (int i = 0; i < S::kRing; ++i) {
+      const int t = token_of(i);
+      load_pids(t, pa, pb);
+      const uint64_t at[2] = {tile_at(t, pa), tile_at(t + 16, pb)};
+      const unsigned only = i < nsteps ? ~0u : 0u;
+      load_k(at, only, ring[i]);
+      load_v(at, only, ring[i]);
+    }
+    load_pids(token_of(S::kRing), pa, pb);
+    // q as the B operand: column c, elements 8 j .. +7 of the lane's part of d
+    bf16x8 qop[S::kQK];
+    {
+      const uint16_t* qrow = q + ((static_cast<int64_t>(b) * nq + qj) * p.hq + g * group + qh) * D + dof;
+#pragma unroll
+      for (int i = 0; i < S::kQK; ++i) {
+        u32x4 w = {0u, 0u, 0u, 0u};
+        if (c < ncols) w = (ld16(qrow + 128 * (i >> 2) + 8 * (i & 3)) & p.keep) ^ p.flip;
+        qop[i] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    {
+      auto step = [&](int k, Set& r) {
         const int t = token_of(k);
-        const bool edge = t + kStep > hi_min || (t < lo_max && t + kStep > sinks);  // some key is masked
+        const bool edge = (t + kStep > hi_min) | ((t < lo_max) & (t + kStep > sinks));  // some key is masked
         // S^T = K Q^T: rows = tokens 16 T + 4 g4 + i, column c
         f32x4 sacc[2];
 #pragma unroll
         for (int T = 0; T < 2; ++T) {
           sacc[T] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < S::kParts; ++i)
-#pragma unroll
-            for (int j = 0; j < S::kWords; ++j)
-              sacc[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(kr.w[T][i][j], scale_of(kr.s[T][i])),
-                                                                 qop[i * S::kWords + j], sacc[T], 0, 0, 0);
+          for (int i = 0; i < S::kQK; ++i) {
+            const u32x4 w = r.kw[T][i >> 2];
+            const unsigned word = D == 64 ? (g4 > 1 ? w[2 + (i & 1)] : w[i & 1]) : w[i & 3];
+            sacc[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(word, scale_of(r.ks[T][i >> 2])), qop[i], sacc[T], 0, 0, 0);
+          }
         }
-        load_pids(k + 2, pa, pb);
-        load(k + 1, pa1, pb1, p.k, p.ks, kr);
-        // V rows that no query of the sequence sees: zeros, never NaN * 0
-        if (t + kStep > L || (t < lo_seq && t + kStep > pinned)) {
+        const int ta = token_of(k + S::kRing);
+        const uint64_t at[2] = {tile_at(ta, pa), tile_at(ta + 16, pb)};
+        const unsigned only = k + S::kRing < nsteps ? ~0u : 0u;
+        load_k(at, only, r);
+        load_pids(token_of(k + S::kRing + 1), pa, pb);
+        // V rows that no query of the sequence sees (only where some key is
+        // masked): zeros, never NaN * 0
+        if (edge) {
 #pragma unroll
-          for (int T = 0; T < 2; ++T) {
-            const int tok = t + 16 * T + c;
-            const bool live = tok < L && (tok >= lo_seq || tok < pinned);
-#pragma unroll
-            for (int i = 0; i < S::kParts; ++i) {
-              vr.s[T][i] = live ? vr.s[T][i] : 0;
-#pragma unroll
-              for (int j = 0; j < S::kWords; ++j) vr.w[T][i][j] = live ? vr.w[T][i][j] : 0;
-            }
+          for (int i = 0; i < S::kVLoads; ++i) {
+            const int tok = t + 16 * vtile(i) + c;
+            const bool live = (tok < Lw) & ((tok >= lo_seq) | (tok < pinned));
+            r.vs[i] = live ? r.vs[i] : 0;  // (2^-127 times codes that are finite, times a probability of zero)
           }
         }
         lds_order();  // the previous step's reads of the tile are done
 #pragma unroll
-        for (int T = 0; T < 2; ++T)
+        for (int i = 0; i < S::kVLoads; ++i) {
+          unsigned char* row = tile + (16 * vtile(i) + c) * S::kRowBytes + 64 * vgrp(i);
+          const float unit = scale_of(r.vs[i]);
 #pragma unroll
-          for (int i = 0; i < S::kParts; ++i)
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<u32x4*>(row + 16 * j) = __builtin_bit_cast(u32x4, decode8(r.vw[i][j], unit));
+        }
+        load_v(at, only, r);
+        // Online softmax in log2 units, against a reference m_run of each column
+        // that follows its maximum only when a score passes it by 2^kLazy: the
+        // probabilities are then at most 2^kLazy, which costs fp32 and the hi +
+        // lo pairs nothing, and most steps neither reduce a maximum across
+        // lanes nor rescale the accumulator.
+        if (edge) {
 #pragma unroll
-            for (int j = 0; j < S::kWords; ++j)
-              *reinterpret_cast<u32x4*>(tile + (16 * T + c) * S::kRowBytes + 2 * (dof + 128 * i + 8 * j)) =
-                  __builtin_bit_cast(u32x4, decode8(vr.w[T][i][j], scale_of(vr.s[T][i])));
-        load(k + 1, pa1, pb1, p.v, p.vs, vr);
-        // online softmax in log2 units
-        float sv[2][4];
-        float mx = -__builtin_inff();
+          for (int T = 0; T < 2; ++T)
 #pragma unroll
-        for (int T = 0; T < 2; ++T)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float s = sacc[T][i] * p.scale;
-            if (edge) {
+            for (int i = 0; i < 4; ++i) {
               const int tok = t + 16 * T + 4 * g4 + i;
-              if (tok >= hi_c || (tok < lo_c && tok >= sinks)) s = -__builtin_inff();
+              const bool masked = (tok >= hi_c) | ((tok < lo_c) & (tok >= sinks));
+              sacc[T][i] = masked ? -__builtin_inff() : sacc[T][i];
             }
-            sv[T][i] = s;
-            mx = fmaxf(mx, s);
+        }
+        const float mx0 = fmaxf(fmaxf(sacc[0][0], sacc[0][1]), fmaxf(sacc[0][2], sacc[0][3]));
+        const float mx1 = fmaxf(fmaxf(sacc[1][0], sacc[1][1]), fmaxf(sacc[1][2], sacc[1][3]));
+        float mx = fmaxf(mx0, mx1);
+        if (__any(mx * p.scale > m_run + kLazy)) {  // (no key yet: m_run = -inf)
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          const float m_new = fmaxf(m_run, mx * p.scale);
+          // (a column that has still seen no key keeps 0 in its place)
+          const float alpha = m_run == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+          m_run = m_new;
+          l_acc *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < S::kDT; ++dt) acc[dt] *= alpha;
+        }
+        const float m_ref = m_run == -__builtin_inff() ? 0.f : m_run;
+        // p = hi + lo, two bf16 values: the products carry it to ~2^-17
+        unsigned hi_w2[4], lo_w2[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x2 pf;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int e = 2 * i + j;
+            pf[j] = __builtin_amdgcn_exp2f(fmaf(sacc[e >> 2][e & 3], p.scale, -m_ref));
           }
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float m_new = fmaxf(m_run, mx);
-        const float m_ref = m_new == -__builtin_inff() ? 0.f : m_new;  // a column that has seen no key yet
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_ref);
-        m_run = m_new;
-        bf16x8 pop, pop_lo;  // p = hi + lo: the products carry it to ~2^-17
-        float psum = 0.f;
-#pragma unroll
-        for (int T = 0; T < 2; ++T)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float pf = __builtin_amdgcn_exp2f(sv[T][i] - m_ref);
-            const __bf16 hi = static_cast<__bf16>(pf);
-            pop[4 * T + i] = hi;
-            pop_lo[4 * T + i] = static_cast<__bf16>(pf - static_cast<float>(hi));
-            psum += pf;
-          }
-        l_lane = l_lane * alpha + psum;
-#pragma unroll
-        for (int dt = 0; dt < S::kDT; ++dt) acc[dt] *= alpha;
+          hi_w2[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(pf, bf16x2));
+          const f32x2 rest = {pf[0] - __builtin_bit_cast(float, hi_w2[i] << 16),
+                              pf[1] - __builtin_bit_cast(float, hi_w2[i] & 0xFFFF0000u)};
+          lo_w2[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, bf16x2));
+        }
+        const bf16x8 pop = __builtin_bit_cast(bf16x8, u32x4{hi_w2[0], hi_w2[1], hi_w2[2], hi_w2[3]});
+        const bf16x8 pop_lo = __builtin_bit_cast(bf16x8, u32x4{lo_w2[0], lo_w2[1], lo_w2[2], lo_w2[3]});
+        // their sum is a product with a row of ones (the matrix cores have time)
+        const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+        l_acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pop, l_acc, 0, 0, 0);
+        l_acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pop_lo, l_acc, 0, 0, 0);
         lds_order();
         const unsigned char* r0 = tile + (4 * g4 + (c >> 2)) * S::kRowBytes + 8 * (c & 3);
         const unsigned char* r1 = r0 + 16 * S::kRowBytes;
@@ -488,15 +569,20 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
           acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pop, acc[dt], 0, 0, 0);
           acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pop_lo, acc[dt], 0, 0, 0);
         }
-        pa1 = pa;
-        pb1 = pb;
+      };
+      for (int k = 0;;) {
+        step(k, ring[0]);
+        if (++k >= nsteps) break;
+        if constexpr (S::kRing > 1) {
+          step(k, ring[1]);
+          if (++k >= nsteps) break;
+        }
       }
       lds_order();
     }
 
     // ---- finish the piece: combine the phases of each kv head, then write
-    float l_tot = l_lane + __shfl_xor(l_lane, 16);
-    l_tot += __shfl_xor(l_tot, 32);
+    const float l_tot = l_acc[0];
     float big_m = m_run, den = l_tot;
     if (phases > 1) {
       f32x4* accx = reinterpret_cast<f32x4*>(smem);  // [wave][dt][lane], reuses the tiles
@@ -526,8 +612,8 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
     }
     if (ph == 0 && c < ncols) {
       if (s0 == 0 && s1 == nb) {
-        const float inv = den > 0.f ? 1.0f / den : (den == 0.f ? 0.f : den);  // no key: a zero row; NaN stays
-        uint16_t* orow = p.out + ((static_cast<int64_t>(b) * nq + qj) * p.hq + g * group + qh) * D + 4 * g4;
+        const float inv = den > 0.f ? 1.0f / den : 0.f;  // a query that sees no key: zero row
+        uint16_t* orow = out + ((static_cast<int64_t>(b) * nq + qj) * p.hq + g * group + qh) * D + 4 * g4;
 #pragma unroll
         for (int dt = 0; dt < S::kDT; ++dt) {
           bf16x4 o;
@@ -538,16 +624,16 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), 2 * kKv4WorkgroupsPerCu * kv
       } else {
         const int64_t slot = kFixed ? static_cast<int64_t>(blk) : static_cast<int64_t>(blk) + static_cast<int64_t>(b) * ngroups + hg;
         const int64_t row = (slot * hgs + hi_w) * ncols + c;
-        float* arow = p.ws_acc + row * D + 4 * g4;
+        float* arow = ws_acc + row * D + 4 * g4;
 #pragma unroll
         for (int dt = 0; dt < S::kDT; ++dt) *reinterpret_cast<f32x4*>(arow + 16 * dt) = acc[dt];
-        if (g4 == 0) *reinterpret_cast<f32x2*>(p.ws_ml + row * 2) = f32x2{big_m, den};
+        if (g4 == 0) *reinterpret_cast<f32x2*>(ws_ml + row * 2) = f32x2{big_m, den};
       }
     }
     if (phases > 1) __syncthreads();  // the exchange area is a tile again
 
-    x += s1 - s0;
-    if (kFixed || x >= xend) break;
+    left -= s1 - s0;
+    if (kFixed || left <= 0) break;
     s0 = 0;
     if (++hg == ngroups) {
       hg = 0;
@@ -573,17 +659,6 @@ hipError_t launch_attn4(const LaunchArgs& a, const Kv4Args& c, hipStream_t st) {
     attr_set.fetch_or(bit);
   }
   Attn4 p;
-  p.q = a.q;
-  p.k = c.k;
-  p.ks = c.ks;
-  p.v = c.v;
-  p.vs = c.vs;
-  p.bt = a.bt;
-  p.lens = a.lens;
-  p.out = a.out;
-  p.ws_acc = a.ws_acc;
-  p.ws_ml = a.ws_ml;
-  p.ws_pref = a.ws_pref;
   p.batch = a.batch;
   p.hq = a.hq;
   p.hkv = a.hkv;
@@ -599,10 +674,11 @@ hipError_t launch_attn4(const LaunchArgs& a, const Kv4Args& c, hipStream_t st) {
   p.chunks = a.chunks;
   p.chunk_steps = a.chunk_steps;
   const float s = a.scale * kLog2e;
-  p.scale = s < 0.f ? -s : s;
+  p.scale = s == 0.f ? 1.f : s < 0.f ? -s : s;
+  p.keep = s == 0.f ? 0u : ~0u;
   p.flip = s < 0.f ? 0x80008000u : 0u;
   hipLaunchKernelGGL((attn4_kernel<D, kFixed>), dim3(a.grid), dim3(64 * a.waves), kv4_attn_lds_bytes(D, a.batch, a.waves),
-                     st, p);
+                     st, a.q, c.k, c.ks, c.v, c.vs, a.bt, a.lens, a.out, a.ws_acc, a.ws_ml, a.ws_pref, p);
   return hipGetLastError();
 }
 
