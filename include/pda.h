@@ -354,7 +354,7 @@ int pda_kv4_workspace_reserve(int32_t batch, int32_t num_q_heads, int32_t num_kv
  *
  * num_pages at most 16777216, batch and rows at most 8192; outputs may not
  * overlap inputs or each other (PDA_ERR_LAYOUT).  Asynchronous on `stream`;
- * update and compact use the (device, stream) workspace: 8 bytes a page, which
+ * update and compact use the (device, stream) workspace: 12 bytes a page, which
  * pda_pages_workspace_reserve allocates ahead of a graph capture.
  */
 typedef struct {

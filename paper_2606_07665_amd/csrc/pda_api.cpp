@@ -1111,10 +1111,10 @@ int check_spans(const Span (&s)[kN], size_t first_out) {
 }
 
 int64_t update_ws_bytes(int32_t rows, int32_t num_pages) {
-  return align256((2 * static_cast<int64_t>(num_pages) + rows) * 4);
+  return align256((3 * static_cast<int64_t>(num_pages) + 3 * static_cast<int64_t>(rows)) * 4);
 }
 int64_t compact_ws_bytes(int32_t num_pages) {
-  return align256((static_cast<int64_t>(num_pages) + num_pages / pda::kCompactPages + 1) * 4);
+  return align256((2 * static_cast<int64_t>(num_pages) + num_pages / pda::kCompactPages + 1) * 4);
 }
 
 // A workspace for every call of these sizes, for the most (query token, head)
@@ -1695,6 +1695,9 @@ int pda_pages_update(const int32_t* block_table, const int32_t* context_lens, co
   a.writer = static_cast<int32_t*>(ws);
   a.fresh = a.writer + num_pages;
   a.start = a.fresh + num_pages;
+  a.written = a.start + rows;
+  a.grows = a.written + rows;
+  a.cnt = a.grows + rows;
   a.batch = batch;
   a.rows = rows;
   a.page_shift = log2i(page_size);
@@ -1737,7 +1740,8 @@ int pda_pages_compact(const int32_t* block_table, const int32_t* context_lens, c
   a.dst = copy_dst;
   a.info = info;
   a.place = static_cast<int32_t*>(ws);
-  a.counts = a.place + num_pages;
+  a.ranked = a.place + num_pages;
+  a.counts = a.ranked + num_pages;
   a.batch = batch;
   a.page_shift = log2i(page_size);
   a.num_pages = num_pages;

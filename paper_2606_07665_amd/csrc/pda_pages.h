@@ -19,9 +19,12 @@ struct PagesUpdateArgs {
   int32_t* src;             // [rows]
   int32_t* dst;             // [rows]
   int32_t* info;            // [2]
+  int32_t* cnt;             // workspace [num_pages]: references without those of the rows that write into a page
   int32_t* writer;          // workspace [num_pages]: the lowest row that writes into a page
   int32_t* fresh;           // workspace [num_pages]: the free pages, ascending, as many as are wanted
   int32_t* start;           // workspace [rows]: a row's place among the fresh pages, and bit 31: it copies
+  int32_t* written;         // workspace [rows]: the page a row writes into
+  int32_t* grows;           // workspace [rows]: fresh pages it takes, a copy apart
   int batch, rows, page_shift, num_pages, maxp, nq, window, sinks;
 };
 
@@ -36,10 +39,11 @@ struct PagesCompactArgs {
   int32_t* dst;           // [num_pages]
   int32_t* info;          // [2]
   int32_t* counts;        // workspace [ceil(num_pages / kCompactPages)]
-  int32_t* place;         // workspace [num_pages]: a moving page's place in the list
+  int32_t* place;         // workspace [num_pages]: a moving page's rank among the live ones
+  int32_t* ranked;        // workspace [num_pages]: the moving page of each rank
   int batch, page_shift, num_pages, maxp;
 };
-constexpr int kCompactPages = 4096;  // pages per workgroup of the counting passes
+constexpr int kCompactPages = 1024;  // pages per workgroup of the counting passes
 
 struct PagesCopyArgs {
   struct Pool {
