@@ -278,12 +278,25 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
   int32_t* ws_split = ws_pref + p.batch + 1;
 
   int b, hg, s0, nb;
+  int fx_a[S::kRing] = {}, fx_b[S::kRing] = {};  // fixed split: page ids of the first steps
   int64_t x = 0, xend, total = 1, beff = 1;
   if constexpr (kFixed) {
     const int e = div_small_u(blk, p.chunks);
     b = div_small_u(e, ngroups);
     hg = e - b * ngroups;
     s0 = (blk - e * p.chunks) * p.chunk_steps;
+    // without a window the first steps' page ids do not depend on the length:
+    // both are requested together (entries past the sequence's pages are
+    // clamped into the pool like any other, and masked)
+    if (window == 0) {
+#pragma unroll
+      for (int i = 0; i < S::kRing; ++i) {
+        const int t = (s0 + ph + i * phases) * kStep;
+        const int ja = t >> p.page_shift, jb = (t + 16) >> p.page_shift;
+        fx_a[i] = bt[static_cast<int64_t>(b) * p.maxp + (ja < p.maxp ? ja : p.maxp - 1)];
+        fx_b[i] = bt[static_cast<int64_t>(b) * p.maxp + (jb < p.maxp ? jb : p.maxp - 1)];
+      }
+    }
     nb = seq_steps(clamp_len(uniform(lens[b]), max_ctx), nq, window, sinks);
     if (s0 >= nb) {  // a chunk past the sequence's end
       if (nb == 0 && s0 == 0) {  // an empty sequence: zero rows
@@ -443,12 +456,26 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
     // Loads run kRing steps ahead: a set's registers are loaded again as soon as
     // its step has used them, K after the products with q, V after its rows are
     // in LDS.  Page ids (scalar loads) run one step further.
+    // q's rows are requested first: vector loads arrive in order.
+    u32x4 qraw[S::kQK];
+    {
+      // (a padding column reads a row inside q, and is zeroed below)
+      const uint16_t* qrow = q + ((static_cast<int64_t>(b) * nq + qj) * p.hq + g * group + qh) * D + dof;
+#pragma unroll
+      for (int i = 0; i < S::kQK; ++i) qraw[i] = ld16(qrow + 128 * (i >> 2) + 8 * (i & 3));
+    }
     Set ring[S::kRing];
     int pa, pb;
 #pragma unroll
     for (int i = 0; i < S::kRing; ++i) {
-      const int t = token_of(i);
-      load_pids(t, pa, pb);
+      int t = token_of(i);
+      if (kFixed && window == 0) {
+        t = (sw + i * phases) * kStep;
+        pa = fx_a[i];
+        pb = fx_b[i];
+      } else {
+        load_pids(t, pa, pb);
+      }
       const uint64_t at[2] = {tile_at(t, pa), tile_at(t + 16, pb)};
       const unsigned only = i < nsteps ? ~0u : 0u;
       load_k(at, only, ring[i]);
@@ -457,15 +484,9 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
     load_pids(token_of(S::kRing), pa, pb);
     // q as the B operand: column c, elements 8 j .. +7 of the lane's part of d
     bf16x8 qop[S::kQK];
-    {
-      const uint16_t* qrow = q + ((static_cast<int64_t>(b) * nq + qj) * p.hq + g * group + qh) * D + dof;
 #pragma unroll
-      for (int i = 0; i < S::kQK; ++i) {
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if (c < ncols) w = (ld16(qrow + 128 * (i >> 2) + 8 * (i & 3)) & p.keep) ^ p.flip;
-        qop[i] = __builtin_bit_cast(bf16x8, w);
-      }
-    }
+    for (int i = 0; i < S::kQK; ++i)
+      qop[i] = __builtin_bit_cast(bf16x8, c < ncols ? (qraw[i] & p.keep) ^ p.flip : u32x4{0u, 0u, 0u, 0u});
     {
       auto step = [&](int k, Set& r) {
         const int t = token_of(k);
