@@ -208,8 +208,9 @@ struct Form {
   int per_cu;           // workgroups of a compute unit that run together
   int64_t token_bytes;  // K and V of a token and kv head
   bool options;         // the compute path and the fused merge apply
+  bool light;           // 4-bit steps: small calls by small_plan_light
 };
-Form bf16_form(int d, bool sinks = false) { return {pda::max_waves(d), 1, static_cast<int64_t>(d) * 4, !sinks}; }
+Form bf16_form(int d, bool sinks = false) { return {pda::max_waves(d), 1, static_cast<int64_t>(d) * 4, !sinks, false}; }
 // Workgroups of 4 waves, as many as fill a CU's registers, where their LDS (the
 // tiles, and the prefix over the batch) allows it; one of all the waves, or
 // what fits, where it does not.
@@ -220,7 +221,7 @@ Form kv4_form(int d, int batch) {
     for (waves = pda::kv4_max_waves(d); waves > 4; waves -= 4)
       if (pda::kv4_attn_lds_bytes(d, batch, waves) <= static_cast<size_t>(pda::kMaxLdsBytes)) break;
   }
-  return {waves, per_cu, static_cast<int64_t>(d) * 17 / 16, false};
+  return {waves, per_cu, static_cast<int64_t>(d) * 17 / 16, false, true};
 }
 
 // Workgroups: one wave per kv head of a group of hgs, times step phases up
@@ -325,6 +326,29 @@ constexpr int64_t kSmallCallBytes = int64_t{128} << 20;
 constexpr int64_t kSmallCallPieces = 32;
 constexpr int kDefaultMinSteps = 2;
 
+// Small calls over a 4-bit cache, whose steps are a quarter of the bytes: a wave
+// takes four of them before another is worth its partials and its place in the
+// merge (two where the call has fewer than 2048 in all; below 1024 the bf16
+// rule stands, which a 2048-token window of 1 sequence at 32:8 needs: 8.9 us, 9.8 by this one), and a workgroup the
+// fewest kv heads with which the fixed split still applies, its waves as step
+// phases that are joined in LDS.  Replayed from a graph over three caches, the
+// bf16 rules -> these: 8 x 2048 tokens at 32:8 heads 14.5 -> 12.0 us, 1 x 32768
+// at 64:8 20.7 -> 17.3, 2 x 16384 at 32:2 16.6 -> 12.1, 4 x 8192 at 8:2, D = 64
+// 10.8 -> 9.1, 16 sequences at 12:4, D = 256, under a 4096-token window 26.3 ->
+// 23.2; 1 x 4096 at 32:8 10.0 -> 9.9.
+constexpr int64_t kLightSteps = 1024;
+Plan small_plan_light(const Form& form, const Plan& dflt, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq,
+                      int num_cus, int cols, int cap, int ms_opt) {
+  const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu;
+  const int64_t steps = static_cast<int64_t>(batch) * hkv * steps_seq;
+  const int ms = ms_opt > 0 ? ms_opt : steps < 2 * kLightSteps ? 2 : 4;
+  int h = dflt.hgs;
+  if (cap == 0)
+    for (h = 1; h < dflt.hgs; ++h)
+      if (hkv % h == 0 && 2 * static_cast<int64_t>(batch) * (hkv / h) <= target) break;
+  return plan_for(form, h, batch, hkv, d, steps_seq, num_cus, cols, ms);
+}
+
 Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols) {
   const int cap = kv_group_cap();
   const int ms_opt = min_steps_option();
@@ -357,7 +381,9 @@ Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, in
   //    11.4 us by events, 16.7 -> 11.9 us per call replayed from a graph).
   const int64_t kv_bytes = static_cast<int64_t>(batch) * steps_seq * pda::kStep * hkv * form.token_bytes;
   const bool small = kv_bytes <= kSmallCallBytes;
-  if (small) {
+  if (small && form.light && batch * hkv * steps_seq >= kLightSteps) {
+    dflt = small_plan_light(form, dflt, batch, hkv, d, steps_seq, num_cus, cols, cap, ms_opt);
+  } else if (small) {
     if (ms_opt == 0 && dflt.grid > 1 && dflt.grid < static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu)
       dflt = plan_for(form, dflt.hgs, batch, hkv, d, steps_seq, num_cus, cols, 1);
     if (cap == 0) {
