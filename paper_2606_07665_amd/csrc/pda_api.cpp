@@ -329,7 +329,8 @@ constexpr int kDefaultMinSteps = 2;
 // Small calls over a 4-bit cache, whose steps are a quarter of the bytes: a wave
 // takes four of them before another is worth its partials and its place in the
 // merge (two where the call has fewer than 2048 in all; below 1024 the bf16
-// rule stands, which a 2048-token window of 1 sequence at 32:8 needs: 8.9 us, 9.8 by this one), and a workgroup the
+// rule stands, which a 2048-token window of 1 sequence at 32:8 needs: 8.9 us, 9.8
+// by this one), and a workgroup the
 // fewest kv heads with which the fixed split still applies, its waves as step
 // phases that are joined in LDS.  Replayed from a graph over three caches, the
 // bf16 rules -> these: 8 x 2048 tokens at 32:8 heads 14.5 -> 12.0 us, 1 x 32768
