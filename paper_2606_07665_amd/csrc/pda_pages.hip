@@ -231,9 +231,11 @@ __global__ __launch_bounds__(kThreads) void update_table_kernel(PagesUpdateArgs 
 
 // The same where every workgroup finds the places for itself, in LDS, instead of
 // a kernel in between: for few rows and pages, whose places take less than a
-// launch (32 rows, 2900 pages: 16 us for the update's kernels, 14 so).
+// launch (32 rows, 2900 pages: 16 us for the update's kernels, 14 so), and no
+// more workgroups than run at once, since each repeats the work.
+constexpr int kOwnPlaceLds = 60 * 1024;  // places and starts: what any launch may ask for, less `part`
 constexpr int kOwnPlaceRows = kScanThreads;
-constexpr int kOwnPlacePages = 4 * 4 * kScanThreads;  // 64 KB of LDS
+constexpr int kOwnPlaceBlocks = 256;
 __global__ __launch_bounds__(kScanThreads) void update_place_table_kernel(PagesUpdateArgs a) {
   extern __shared__ int32_t lds[];  // [num_pages] fresh pages, [rows] starts
   __shared__ int part[kScanThreads / 64];
@@ -402,13 +404,15 @@ __global__ __launch_bounds__(kThreads) void copy_kernel(PagesCopyArgs a, int par
 
 hipError_t launch_pages_update(const PagesUpdateArgs& args, hipStream_t st) {
   PagesUpdateArgs a = args;
-  const bool own_place = a.rows > 0 && a.rows <= kOwnPlaceRows && a.num_pages <= kOwnPlacePages;
+  const int64_t entries = static_cast<int64_t>(a.rows) * a.maxp;
+  const bool own_place = a.rows > 0 && a.rows <= kOwnPlaceRows && entries <= kOwnPlaceBlocks * kScanThreads &&
+                         4 * (static_cast<int64_t>(a.num_pages) + a.rows) <= kOwnPlaceLds;
   if (!own_place) a.cnt = a.refcount_out;
   const unsigned over_pages = (a.num_pages + kThreads - 1) / kThreads, over_row = (a.maxp + kThreads - 1) / kThreads;
   hipLaunchKernelGGL(update_start_kernel, dim3(over_pages), dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL(update_count_kernel, dim3(over_row, a.batch + a.rows), dim3(kThreads), 0, st, a);
+  if (a.batch + a.rows > 0)
+    hipLaunchKernelGGL(update_count_kernel, dim3(over_row, a.batch + a.rows), dim3(kThreads), 0, st, a);
   if (own_place) {
-    const int64_t entries = static_cast<int64_t>(a.rows) * a.maxp;
     hipLaunchKernelGGL(update_place_table_kernel, dim3(static_cast<unsigned>((entries + kScanThreads - 1) / kScanThreads)),
                        dim3(kScanThreads), 4 * (a.num_pages + a.rows), st, a);
     return hipGetLastError();
