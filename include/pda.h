@@ -220,6 +220,9 @@ int paged_decode_attention_ext(const void* q, const void* k_cache, const void* v
  * the sinks and wholly before the window -- is never read and may have been
  * released (any block_table entry).  The calls run on the matrix cores with
  * the merge kernel, whatever PDA_OPT_COMPUTE_PATH and PDA_OPT_FUSED_MERGE say.
+ * An infinity or a NaN among a token's values reaches only the queries that see
+ * the token (with num_sinks 0, as in paged_decode_attention_ext, it can reach
+ * the other queries of its sequence as a NaN).
  * Everything else is as for paged_decode_attention_ext;
  * pda_workspace_reserve covers these calls.
  */
@@ -279,8 +282,9 @@ int pda_kv4_read(void* k_out, void* v_out, const void* k_codes, const void* k_sc
  * in 4 bits: the same queries, key ranges (window 0: none; num_sinks 0: none),
  * released pages and output, on the values that the codes and scales stand
  * for.  The arithmetic is that of paged_decode_attention (keys and values are
- * exact in bf16).  Workspace per (device, stream), shared with the other
- * calls; pda_kv4_workspace_reserve grows it for any num_queries, window and
+ * exact in bf16), and what is not finite reaches only the queries that see it,
+ * with or without a window.  Workspace per (device, stream), shared with the
+ * other calls; pda_kv4_workspace_reserve grows it for any num_queries, window and
  * num_sinks of these sizes, as pda_workspace_reserve does for the bf16 calls.
  */
 int paged_decode_attention_kv4(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,

@@ -97,6 +97,50 @@ __device__ __forceinline__ int div_small(int a, int b) {
 }
 __device__ __forceinline__ int div_small_u(int a, int b) { return uniform(div_small(a, b)); }
 
+// Values with an infinity or a NaN that some query tokens of a sequence see and
+// others do not (drafted tokens after a query, the far end of its window): as a
+// row of the product P V they would reach every column, 0 * NaN of those that
+// do not see them.  Such a row is taken out of the product: its token's
+// probabilities times the row are added here to the columns that see it, and
+// the row in LDS becomes zeros.  hi, lo: the lane's probabilities as the product
+// takes them, element 4 T + i that of token 16 T + 4 (lane / 16) + i; r: the
+// token's row in the tile at `rows`; acc: lane (g4, c) holds column c, element i
+// of tile dt that of d = 16 dt + 4 g4 + i.
+template <int D, int kRowBytes>
+__device__ __forceinline__ void add_row_apart(f32x4 (&acc)[D / 16], u32x4 hi, u32x4 lo, unsigned char* rows, int r, bool sees) {
+  const int lane = threadIdx.x & 63;
+  const int word = 2 * (r >> 4) + ((r & 3) >> 1);
+  unsigned h = hi[0], l = lo[0];
+#pragma unroll
+  for (int k = 1; k < 4; ++k) {
+    h = word == k ? hi[k] : h;
+    l = word == k ? lo[k] : l;
+  }
+  const int from = 16 * ((r >> 2) & 3) + (lane & 15);
+  h = static_cast<unsigned>(__shfl(static_cast<int>(h), from, 64));
+  l = static_cast<unsigned>(__shfl(static_cast<int>(l), from, 64));
+  const int shift = r & 1 ? 0 : 16;
+  const float p = __builtin_bit_cast(float, (h << shift) & 0xFFFF0000u) + __builtin_bit_cast(float, (l << shift) & 0xFFFF0000u);
+  unsigned char* row = rows + r * kRowBytes;
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const u32x2 v = *reinterpret_cast<const u32x2*>(row + 32 * dt + 8 * (lane >> 4));
+    f32x4 add;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned w = v[i >> 1];
+      const float x = __builtin_bit_cast(float, i & 1 ? w & 0xFFFF0000u : w << 16);
+      add[i] = sees ? p * x : 0.f;
+    }
+    acc[dt] += add;
+    __builtin_amdgcn_sched_barrier(0);  // (a tile at a time: rare, and no registers of the loop for it)
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // every lane's reads before the zeros
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  if (8 * lane < 2 * D) *reinterpret_cast<u32x2*>(row + 8 * lane) = u32x2{0u, 0u};
+}
+
 // Workgroup that owns flattened step x of `total`, when `parts` workgroups
 // split [0, total) into ranges [w*total/parts, (w+1)*total/parts).
 __device__ __forceinline__ int64_t owner_of(int64_t x, int64_t total, int64_t parts) {

@@ -776,6 +776,29 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
 #pragma unroll
       for (int dt = 0; dt < S::kDT; ++dt) acc[dt] *= alpha;
       lds_order();
+      if constexpr (kSink) {
+        if (edge && nq > 1) {
+          // the rows that some of the queries see, if they hold an infinity or a NaN
+          const int tl = t0 + (lane & 31);
+          const bool some = tl < L && (tl >= lo_seq || tl < pinned) && !(tl < hi_min && (tl >= lo_max || tl < sinks));
+          unsigned apart = static_cast<unsigned>(__ballot(some));
+          while (apart) {
+            const int row = __builtin_ctz(apart), tok = t0 + row;
+            apart &= apart - 1;
+            unsigned char* v = tile + S::kVOffset;
+            u32x2 x = {0u, 0u};
+            if (8 * lane < 2 * D) x = *reinterpret_cast<const u32x2*>(v + row * S::kVRowBytes + 8 * lane);
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) odd |= (x[i] & 0x7F80u) == 0x7F80u || (x[i] & 0x7F800000u) == 0x7F800000u;
+            if (__any(odd)) {
+              add_row_apart<D, S::kVRowBytes>(acc, __builtin_bit_cast(u32x4, pop), __builtin_bit_cast(u32x4, pop_lo), v, row,
+                                              tok < hi_c && (tok >= lo_c || tok < sinks));
+              lds_order();
+            }
+          }
+        }
+      }
       // O^T += V^T P^T ; V^T operand via transposed LDS reads
       const unsigned char* r0 = tile + S::kVOffset + (4 * g4 + (c >> 2)) * S::kVRowBytes + 8 * (c & 3);
       const unsigned char* r1 = r0 + 16 * S::kVRowBytes;

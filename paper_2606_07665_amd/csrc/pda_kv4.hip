@@ -510,12 +510,22 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
         load_pids(token_of(k + S::kRing + 1), pa, pb);
         // V rows that no query of the sequence sees (only where some key is
         // masked): zeros, never NaN * 0
+        unsigned apart = 0;  // tokens of the step that add_row_apart takes
         if (edge) {
 #pragma unroll
           for (int i = 0; i < S::kVLoads; ++i) {
             const int tok = t + 16 * vtile(i) + c;
             const bool live = (tok < Lw) & ((tok >= lo_seq) | (tok < pinned));
             r.vs[i] = live ? r.vs[i] : 0;  // (2^-127 times codes that are finite, times a probability of zero)
+            // (from a unit of 2^126 on a value may be an infinity, 255 is NaN)
+            const bool all = (tok < hi_min) & ((tok >= lo_max) | (tok < sinks));
+            uint64_t odd = __ballot((r.vs[i] >= 253) & !all);
+            if (odd) {
+              odd |= odd >> 16;
+              if constexpr (D != 64) odd |= odd >> 32;
+              apart |= (static_cast<unsigned>(odd) & 0xFFFF) << (D == 64 ? 0 : 16 * vtile(i));
+              if constexpr (D == 64) apart |= static_cast<unsigned>(odd >> 32) << 16;
+            }
           }
         }
         lds_order();  // the previous step's reads of the tile are done
@@ -580,6 +590,13 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
         l_acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pop, l_acc, 0, 0, 0);
         l_acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pop_lo, l_acc, 0, 0, 0);
         lds_order();
+        while (apart) {
+          const int row = __builtin_ctz(apart), tok = t + row;
+          apart &= apart - 1;
+          add_row_apart<D, S::kRowBytes>(acc, __builtin_bit_cast(u32x4, pop), __builtin_bit_cast(u32x4, pop_lo), tile, row,
+                                         (tok < hi_c) & ((tok >= lo_c) | (tok < sinks)));
+          lds_order();
+        }
         const unsigned char* r0 = tile + (4 * g4 + (c >> 2)) * S::kRowBytes + 8 * (c & 3);
         const unsigned char* r1 = r0 + 16 * S::kRowBytes;
 #pragma unroll

@@ -1,11 +1,16 @@
 """The cache operators at the borders of their forms: page updates on both sides of the one-launch
-placement's limits."""
+placement's limits, and values that are not finite and that only some queries of a sequence see."""
 import numpy as np
 import pytest
 
-from _gpu import log
+import oracle
+from _cache import build, torch_any, torch_bf16
+from _gpu import check, log
 from oracle import cache as C
+from test_gpu_kv4 import quantised
+from test_gpu_kv4 import run as run_kv4
 from test_gpu_pages import same, state, update
+from test_gpu_sink import run as run_sink
 
 pytestmark = pytest.mark.gpu
 
@@ -36,3 +41,83 @@ def test_update_of_nothing(lib):
     none = np.zeros(0, np.int32)
     got = update(lib, np.zeros((0, 4), np.int32), none, None, none, np.array([0, 2, 0, 1], np.int32), 16)
     assert got[1].tolist() == [0, 2, 0, 1] and got[4].tolist() == [0, 0]
+
+
+# (head_dim, Hq, Hkv, page, lengths, query tokens, window, sinks): the last tokens of a sequence, the far
+# end of a window and the sinks lie in different steps, in one step, in a sequence shorter than its queries
+SHAPES = [
+    (128, 32, 8, 16, [500, 66, 2, 3001], 4, 100, 5),
+    (128, 8, 1, 32, [64, 33, 4000], 2, 20, 3),
+    (64, 16, 4, 16, [200, 40, 5], 3, 37, 2),
+    (256, 12, 4, 16, [300, 31, 1], 5, 64, 4),
+    (128, 32, 8, 16, [300, 7], 4, 0, 0),
+    (64, 4, 2, 64, [129, 3], 8, 0, 0),
+]
+
+
+def partly_seen(n, tq, window, sinks):
+    """The tokens that some, but not all, of a sequence's queries see."""
+    seen = [set(C.visible_keys(n, tq, j, window, sinks).tolist()) for j in range(tq)]
+    return sorted(set().union(*seen) - set.intersection(*seen))
+
+
+def compare(got, want, what):
+    finite = np.isfinite(want)
+    assert not finite.all() and np.array_equal(np.isnan(got), np.isnan(want)), what
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)]), what
+    check(np.where(finite, got, 0), np.where(finite, want, 0), what)
+
+
+IDS = [f"D{c[0]}-{c[1]}:{c[2]}-T{c[5]}-W{c[6]}-S{c[7]}" for c in SHAPES]
+
+
+@pytest.mark.parametrize("pick", [0, 1, -1, None])
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_kv4_values_reach_only_the_queries_that_see_them(lib, shape, pick):
+    d, hq, hkv, page, lens, tq, window, sinks = shape
+    w = build(lens, hq, hkv, d, page, seed=sum(lens), num_queries=tq, window=window, sinks=sinks)
+    kc, ks, vc, vs = (t.copy() for t in quantised(w))
+    for b, n in enumerate(lens):
+        part = partly_seen(n, tq, window, sinks)
+        for i, t in enumerate(part if pick is None else part[pick:][:1]):
+            at = int(w.block_table[b, t // page])
+            if (b + i) % 2:
+                vs[at, :, 0, t % page] = 255                  # NaN
+            else:
+                vs[at, :, 1, t % page] = 254                  # an infinity among zeros
+                vc[at, :, 1, t % page] = 0
+                vc[at, :, 1, t % page, 3] = 0x70 if i % 4 else 0x0F
+    cache = (kc, ks, vc, vs)
+    want = C.attend(w.q, C.kv4_tokens(kc, ks), C.kv4_tokens(vc, vs), w.block_table, w.context_lens, w.scale, window, sinks)
+    log(f"kv4 partly seen {shape} {pick}")
+    compare(run_kv4(lib, w, cache, window, sinks), want, "kv4")
+
+
+@pytest.mark.parametrize("pick", [0, 1, -1, None])
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s[6]] + [(128, 16, 4, 4, [200, 40, 5], 3, 37, 2), (64, 4, 2, 1, [90, 3], 2, 20, 6)])
+def test_bf16_values_reach_only_the_queries_that_see_them(lib, shape, pick):
+    d, hq, hkv, page, lens, tq, window, sinks = shape
+    w = build(lens, hq, hkv, d, page, seed=sum(lens), num_queries=tq, window=window, sinks=sinks)
+    for b, n in enumerate(lens):
+        part = partly_seen(n, tq, window, sinks)
+        for i, t in enumerate(part if pick is None else part[pick:][:1]):
+            row = w.v_cache[int(w.block_table[b, t // page]), t % page]
+            row[:, (7 * b + 11 * i + np.arange(hkv)) % d] = (0x7FC0, 0x7F80, 0xFF80)[(b + i) % 3]
+    want = C.attend(w.q, oracle.bf16_to_f64(w.k_cache), oracle.bf16_to_f64(w.v_cache), w.block_table, w.context_lens, w.scale,
+                    window, sinks)
+    log(f"bf16 partly seen {shape} {pick}")
+    compare(run_sink(lib, w, window, sinks), want, "sink")
+
+
+def test_keys_that_are_not_finite_reach_only_the_queries_that_see_them(lib):
+    lens, tq, window, sinks = [500, 66], 3, 100, 5
+    w = build(lens, 32, 8, 128, 16, seed=5, num_queries=tq, window=window, sinks=sinks)
+    for b, n in enumerate(lens):
+        for t in partly_seen(n, tq, window, sinks)[-1:]:
+            w.k_cache[int(w.block_table[b, t // 16]), t % 16, ::2, 9] = 0x7FC0
+    cache = quantised(w)
+    want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, w.scale, window, sinks)
+    compare(run_kv4(lib, w, cache, window, sinks), want, "kv4 keys")
+    want = C.attend(w.q, oracle.bf16_to_f64(w.k_cache), oracle.bf16_to_f64(w.v_cache), w.block_table, w.context_lens, w.scale,
+                    window, sinks)
+    compare(run_sink(lib, w, window, sinks), want, "sink keys")
