@@ -37,15 +37,11 @@ struct Row {
   int lo;        // first token its queries see under the window
 };
 
-__device__ __forceinline__ Row row_of(const PagesUpdateArgs& a, int r) {
-  const int most = a.maxp << a.page_shift;
-  const int b = a.parents ? a.parents[r] : r;
-  const bool has = static_cast<unsigned>(b) < static_cast<unsigned>(a.batch);
+__device__ __forceinline__ Row row_with(const PagesUpdateArgs& a, int parent, int kept, int total) {
   Row w;
-  w.from = a.table + static_cast<int64_t>(has ? b : 0) * a.maxp;
-  w.total = clamp_to(a.new_lens[r], most);
-  const int len = has ? clamp_to(a.lens[b], most) : 0;
-  w.kept = len < w.total ? len : w.total;
+  w.from = a.table + static_cast<int64_t>(parent) * a.maxp;
+  w.total = total;
+  w.kept = kept;
   const int page = 1 << a.page_shift;
   w.full = w.kept >> a.page_shift;
   w.first = (w.kept + page - 1) >> a.page_shift;
@@ -56,12 +52,40 @@ __device__ __forceinline__ Row row_of(const PagesUpdateArgs& a, int r) {
   return w;
 }
 
+// The numbers that decide it: the parent (0 where there is none), its tokens
+// that are kept, and those of the row.
+struct RowInts {
+  int parent, kept, total;
+};
+
+__device__ __forceinline__ RowInts row_ints(const PagesUpdateArgs& a, int r) {
+  const int most = a.maxp << a.page_shift;
+  const int b = a.parents ? a.parents[r] : r;
+  const bool has = static_cast<unsigned>(b) < static_cast<unsigned>(a.batch);
+  const int total = clamp_to(a.new_lens[r], most);
+  const int len = has ? clamp_to(a.lens[b], most) : 0;
+  return {has ? b : 0, len < total ? len : total, total};
+}
+
+__device__ __forceinline__ Row row_of(const PagesUpdateArgs& a, int r) {
+  const RowInts n = row_ints(a, r);
+  return row_with(a, n.parent, n.kept, n.total);
+}
+
+__device__ __forceinline__ int pages_of(const PagesUpdateArgs& a, int b) {
+  const int page = 1 << a.page_shift;
+  return (clamp_to(a.lens[b], a.maxp << a.page_shift) + page - 1) >> a.page_shift;
+}
+
 // Page j of a row, j < first: the parent's, or -1 where it holds none or no
 // query of the row sees any of its tokens (past the sinks and before the
 // window; a page with tokens yet to come is kept).
-__device__ __forceinline__ int kept_page(const PagesUpdateArgs& a, const Row& w, int j) {
+__device__ __forceinline__ bool released(const PagesUpdateArgs& a, const Row& w, int j) {
   const int64_t t = static_cast<int64_t>(j) << a.page_shift;
-  return j < w.full && t >= a.sinks && t + (1 << a.page_shift) <= w.lo ? -1 : page_of(w.from[j], a.num_pages);
+  return j < w.full && t >= a.sinks && t + (1 << a.page_shift) <= w.lo;
+}
+__device__ __forceinline__ int kept_page(const PagesUpdateArgs& a, const Row& w, int j) {
+  return released(a, w, j) ? -1 : page_of(w.from[j], a.num_pages);
 }
 
 constexpr int kNoPage = -2;         // `written` of a row that writes into no page that it shares (-1: into none that it has)
@@ -81,9 +105,7 @@ __global__ __launch_bounds__(kThreads) void update_count_kernel(PagesUpdateArgs 
   const int j = blockIdx.x * kThreads + threadIdx.x;
   if (static_cast<int>(blockIdx.y) < a.batch) {
     const int b = blockIdx.y;
-    const int page = 1 << a.page_shift;
-    const int pages = (clamp_to(a.lens[b], a.maxp << a.page_shift) + page - 1) >> a.page_shift;
-    if (j >= pages) return;
+    if (j >= pages_of(a, b)) return;
     const int id = page_of(a.table[static_cast<int64_t>(b) * a.maxp + j], a.num_pages);
     if (id >= 0) atomicSub(a.cnt + id, 1);
     return;
@@ -196,19 +218,17 @@ __global__ __launch_bounds__(kScanThreads) void update_place_kernel(PagesUpdateA
   }
 }
 
-// Entry (r, j) of the new table; kCounts: and the counts of the pages that the
-// row takes or keeps.
+// Entry (r, j) of the new table; `from`: the parent's page there, -1 for j >=
+// w.first.  kCounts: and the counts of the pages that the row takes or keeps.
 template <bool kCounts>
-__device__ __forceinline__ void write_entry(const PagesUpdateArgs& a, int r, int j, int start_of_row, const int32_t* fresh, int have) {
-  const Row w = row_of(a, r);
+__device__ __forceinline__ void write_entry(const PagesUpdateArgs& a, const Row& w, int r, int j, int from, int start_of_row,
+                                            const int32_t* fresh, int have) {
   const bool copies = start_of_row < 0;
   const int start = start_of_row & 0x7FFFFFFF;
-  int id = -1;
+  int id = from;
   if (j < w.first) {
-    id = kept_page(a, w, j);
     if (j == w.full && w.writes) {
       if (copies) {
-        const int from = id;
         id = start < have ? fresh[start] : -1;
         a.src[r] = id >= 0 ? from : -1;
         a.dst[r] = from >= 0 ? id : -1;
@@ -226,7 +246,9 @@ __device__ __forceinline__ void write_entry(const PagesUpdateArgs& a, int r, int
 
 __global__ __launch_bounds__(kThreads) void update_table_kernel(PagesUpdateArgs a) {
   const int j = blockIdx.x * kThreads + threadIdx.x;
-  if (j < a.maxp) write_entry<true>(a, blockIdx.y, j, a.start[blockIdx.y], a.fresh, a.info[0]);
+  if (j >= a.maxp) return;
+  const Row w = row_of(a, blockIdx.y);
+  write_entry<true>(a, w, blockIdx.y, j, j < w.first ? kept_page(a, w, j) : -1, a.start[blockIdx.y], a.fresh, a.info[0]);
 }
 
 // The same where every workgroup finds the places for itself, in LDS, instead of
@@ -249,7 +271,115 @@ __global__ __launch_bounds__(kScanThreads) void update_place_table_kernel(PagesU
     a.info[0] = have;
     a.info[1] = lacking;
   }
-  if (r < a.rows) write_entry<false>(a, r, static_cast<int>(e - static_cast<unsigned>(r) * a.maxp), start[r], lds, have);
+  if (r >= a.rows) return;
+  const int j = static_cast<int>(e - static_cast<unsigned>(r) * a.maxp);
+  const Row w = row_of(a, r);
+  write_entry<false>(a, w, r, j, j < w.first ? kept_page(a, w, j) : -1, start[r], lds, have);
+}
+
+// The whole update in one launch, for fewer still: every workgroup counts the
+// references for itself, too, in LDS, where a thread can ask for all its entries
+// of the two tables together (rows as wide as a power of two).  Update and copy,
+// 31 sequences of 11 pages as 48 rows 12.4 -> 9.4 us, 6 of 124 as 42 rows 13.5 ->
+// 11.6; with three such rounds (42 rows of up to 512) it is 14.2 -> 16.5, so not
+// there.
+constexpr int kOneLaunchEach = 8;
+constexpr int kOneLaunchEntries = kOneLaunchEach * kScanThreads;
+inline int log2_up(int x) {  // x up to 2^30
+  int s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
+}
+inline int64_t one_launch_lds(const PagesUpdateArgs& a) {
+  return 4 * (2 * static_cast<int64_t>(a.num_pages) + 9 * static_cast<int64_t>(a.rows) + 3 * static_cast<int64_t>(a.batch));
+}
+__global__ __launch_bounds__(kScanThreads) void update_one_kernel(PagesUpdateArgs a, int width_log2) {
+  extern __shared__ int32_t lds[];
+  __shared__ int part[kScanThreads / 64];
+  PagesUpdateArgs l = a;
+  l.cnt = lds;  // and, once the counts have been read, the fresh pages: a free page's rank is at most its number
+  l.writer = l.cnt + a.num_pages;
+  l.start = l.writer + a.num_pages;
+  l.written = l.start + a.rows;
+  l.grows = l.written + a.rows;
+  int32_t* parent = l.grows + a.rows;
+  int32_t* kept = parent + a.rows;
+  int32_t* total = kept + a.rows;
+  // the sequences, then the rows: where their entries lie, how many they are,
+  // and the one that is written into (-1: none)
+  const int jobs = a.batch + a.rows;
+  int32_t* at = total + a.rows;
+  int32_t* many = at + jobs;
+  int32_t* into = many + jobs;
+  const int tid = threadIdx.x;
+  for (int i = tid; i < jobs; i += kScanThreads) {
+    const int r = i - a.batch;
+    if (r < 0) {
+      at[i] = i * a.maxp;
+      many[i] = pages_of(a, i);
+      into[i] = -1;
+      continue;
+    }
+    const RowInts n = row_ints(a, r);
+    parent[r] = n.parent;
+    kept[r] = n.kept;
+    total[r] = n.total;
+    const Row w = row_with(a, n.parent, n.kept, n.total);
+    at[i] = n.parent * a.maxp;
+    many[i] = w.first;
+    into[i] = w.writes ? w.full : -1;
+    l.grows[r] = w.pages - w.first;
+    l.written[r] = kNoPage;
+  }
+  for (int p = tid; p < a.num_pages; p += kScanThreads) {
+    l.cnt[p] = a.refcount[p];
+    l.writer[p] = kNoRow;
+  }
+  const unsigned mine = blockIdx.x * kScanThreads + tid;
+  const int my_row = static_cast<int>(mine / static_cast<unsigned>(a.maxp));
+  const int my_j = static_cast<int>(mine - static_cast<unsigned>(my_row) * a.maxp);
+  __syncthreads();
+  // this thread's own entry, needed at the end
+  Row w = {};
+  int from = -1;
+  if (my_row < a.rows) {
+    w = row_with(a, parent[my_row], kept[my_row], total[my_row]);
+    if (my_j < w.first) from = kept_page(a, w, my_j);
+  }
+  // a thread's entries are asked for together, then counted
+  const int all = jobs << width_log2;
+  int id[kOneLaunchEach];
+#pragma unroll
+  for (int i = 0; i < kOneLaunchEach; ++i) {
+    const int e = tid + i * kScanThreads, job = e >> width_log2, j = e - (job << width_log2);
+    id[i] = -1;
+    if (e < all && j < many[job]) id[i] = page_of(a.table[at[job] + j], a.num_pages);
+    if (a.window > 0 && id[i] >= 0 && job >= a.batch) {
+      const int r = job - a.batch;
+      if (released(a, row_with(a, parent[r], kept[r], total[r]), j)) id[i] = -1;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kOneLaunchEach; ++i) {
+    const int e = tid + i * kScanThreads, job = e >> width_log2, j = e - (job << width_log2);
+    if (e >= all) break;
+    const bool writes = into[job] == j;
+    if (writes) l.written[job - a.batch] = id[i];
+    if (id[i] < 0) continue;
+    if (writes)
+      atomicMin(l.writer + id[i], job - a.batch);
+    else
+      atomicAdd(l.cnt + id[i], job < a.batch ? -1 : 1);
+  }
+  __syncthreads();
+  int lacking;
+  const int have = place_rows(l, l.start, l.cnt, part, &lacking, blockIdx.x == 0);
+  __syncthreads();
+  if (blockIdx.x == 0 && tid == 0) {
+    a.info[0] = have;
+    a.info[1] = lacking;
+  }
+  if (my_row < a.rows) write_entry<false>(a, w, my_row, my_j, from, l.start[my_row], l.cnt, have);
 }
 
 // ------------------------------------------------------------------ compact
@@ -366,6 +496,112 @@ __global__ __launch_bounds__(kThreads) void compact_table_kernel(PagesCompactArg
   a.table_out[e] = id;
 }
 
+// The same in one launch, for pools that every workgroup can go through for
+// itself: a bit per page says which are live, and with the live pages before
+// every 64 of them the rank of a page is one word, the k-th live page or hole a
+// search.  Where a wave can ask for all its pages together, and with no more
+// workgroups than run at once: compaction and copy, a pool of 71 pages 12.8 ->
+// 8.5 us, of 7462 12.7 -> 9.4; with three such rounds (24672 pages) it is 117.5
+// -> 123, so not there.
+constexpr int kOneLaunchEachWave = 8;
+constexpr int kOneLaunchWords = kOneLaunchEachWave * kScanThreads / 64;  // of 64 pages
+constexpr int64_t kOneLaunchCompact = 256 * kScanThreads;               // pages and table entries
+
+// The k-th set bit of x.
+__device__ __forceinline__ int bit_of(uint64_t x, int k) {
+  int at = 0;
+#pragma unroll
+  for (int half = 32; half > 0; half >>= 1) {
+    const int n = __popcll(x & ((uint64_t{1} << half) - 1));
+    if (k >= n) {
+      k -= n;
+      at += half;
+      x >>= half;
+    }
+  }
+  return at;
+}
+
+__global__ __launch_bounds__(kScanThreads) void compact_one_kernel(PagesCompactArgs a) {
+  __shared__ uint64_t word[kOneLaunchWords + 1];
+  __shared__ int before[kOneLaunchWords + 1];  // live pages before each word
+  __shared__ int part[kScanThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int words = (a.num_pages + 63) / 64;
+  // what this thread decides at the end: a page's count, or a table entry
+  const int64_t e = static_cast<int64_t>(blockIdx.x) * kScanThreads + tid;
+  const int64_t entry = e - a.num_pages;
+  const bool in_table = entry >= 0 && entry < static_cast<int64_t>(a.batch) * a.maxp;
+  const int b = in_table ? static_cast<int>(static_cast<unsigned>(entry) / static_cast<unsigned>(a.maxp)) : 0;
+  const int j = static_cast<int>(entry - static_cast<int64_t>(b) * a.maxp);
+  int own_count = 0, id = -1, len = 0;
+  if (entry < 0) own_count = a.refcount[e];
+  if (in_table) {
+    id = a.table[entry];
+    len = a.lens[b];
+  }
+  constexpr int kWaves = kScanThreads / 64;
+  int c[kOneLaunchEachWave];
+#pragma unroll
+  for (int i = 0; i < kOneLaunchEachWave; ++i) {
+    const int p = 64 * ((tid >> 6) + i * kWaves) + lane;
+    c[i] = p < a.num_pages ? a.refcount[p] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kOneLaunchEachWave; ++i) {
+    const uint64_t bits = __ballot(c[i] > 0);
+    if (lane == 0) word[(tid >> 6) + i * kWaves] = bits;
+  }
+  __syncthreads();
+  const int own = tid < words ? __popcll(word[tid]) : 0;
+  int live;
+  const int upto = scan_sum(own, part, live);
+  if (tid < words) before[tid] = upto - own;
+  if (tid == 0) {  // (a rank may be asked for just past the last word)
+    if (words == kOneLaunchWords) word[words] = 0;
+    before[words] = live;
+  }
+  __syncthreads();
+  auto rank = [&](int p) { return before[p >> 6] + __popcll(word[p >> 6] & ((uint64_t{1} << (p & 63)) - 1)); };
+  // the k-th live page, the k-th hole: the last word with at most k before it holds it
+  auto kth = [&](int k, bool hole) {
+    int lo = 0, hi = words - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((hole ? 64 * mid - before[mid] : before[mid]) <= k) lo = mid; else hi = mid - 1;
+    }
+    return 64 * lo + bit_of(hole ? ~word[lo] : word[lo], k - (hole ? 64 * lo - before[lo] : before[lo]));
+  };
+  const int stay = rank(live), moves = live - stay;  // live pages that keep their number
+  if (blockIdx.x == 0 && tid == 0) {
+    a.info[0] = live;
+    a.info[1] = moves;
+  }
+  if (entry < 0) {
+    const int at = static_cast<int>(e);
+    const bool is_live = own_count > 0;
+    const int r = rank(at);
+    if (at >= moves) a.src[at] = a.dst[at] = -1;
+    if (is_live == (at < live)) {  // it stays, live or free
+      a.map[at] = is_live ? at : -1;
+      a.refcount_out[at] = is_live ? own_count : 0;
+    } else {  // the i-th page that moves and the i-th hole
+      const int i = is_live ? r - stay : at - r;
+      const int other = kth(is_live ? i : stay + i, is_live);
+      (is_live ? a.src : a.dst)[i] = at;
+      a.map[at] = is_live ? other : -1;
+      a.refcount_out[at] = is_live ? 0 : a.refcount[other];
+    }
+    return;
+  }
+  if (!in_table) return;
+  const int page = 1 << a.page_shift;
+  const int pages = (clamp_to(len, a.maxp << a.page_shift) + page - 1) >> a.page_shift;
+  id = j < pages ? page_of(id, a.num_pages) : -1;
+  if (id >= 0) id = !(word[id >> 6] >> (id & 63) & 1) ? -1 : id < live ? id : kth(rank(id) - stay, true);
+  a.table_out[entry] = id;
+}
+
 // --------------------------------------------------------------------- copy
 // A workgroup takes 16 KB of one page of one pool at a time: four 16-byte
 // loads in flight per thread, then their stores.
@@ -408,6 +644,13 @@ hipError_t launch_pages_update(const PagesUpdateArgs& args, hipStream_t st) {
   const bool own_place = a.rows > 0 && a.rows <= kOwnPlaceRows && entries <= kOwnPlaceBlocks * kScanThreads &&
                          4 * (static_cast<int64_t>(a.num_pages) + a.rows) <= kOwnPlaceLds;
   if (!own_place) a.cnt = a.refcount_out;
+  const int width_log2 = own_place ? log2_up(a.maxp) : 0;
+  if (own_place && (static_cast<int64_t>(a.batch + a.rows) << width_log2) <= kOneLaunchEntries &&
+      one_launch_lds(a) <= kOwnPlaceLds) {
+    hipLaunchKernelGGL(update_one_kernel, dim3(static_cast<unsigned>((entries + kScanThreads - 1) / kScanThreads)),
+                       dim3(kScanThreads), static_cast<size_t>(one_launch_lds(a)), st, a, width_log2);
+    return hipGetLastError();
+  }
   const unsigned over_pages = (a.num_pages + kThreads - 1) / kThreads, over_row = (a.maxp + kThreads - 1) / kThreads;
   hipLaunchKernelGGL(update_start_kernel, dim3(over_pages), dim3(kThreads), 0, st, a);
   if (a.batch + a.rows > 0)
@@ -423,6 +666,12 @@ hipError_t launch_pages_update(const PagesUpdateArgs& args, hipStream_t st) {
 }
 
 hipError_t launch_pages_compact(const PagesCompactArgs& a, hipStream_t st) {
+  const int64_t threads = a.num_pages + static_cast<int64_t>(a.batch) * a.maxp;
+  if (a.num_pages <= 64 * kOneLaunchWords && threads <= kOneLaunchCompact) {
+    hipLaunchKernelGGL(compact_one_kernel, dim3(static_cast<unsigned>((threads + kScanThreads - 1) / kScanThreads)),
+                       dim3(kScanThreads), 0, st, a);
+    return hipGetLastError();
+  }
   const unsigned blocks = (a.num_pages + kCompactPages - 1) / kCompactPages;
   const unsigned list = (a.num_pages + kThreads - 1) / kThreads;
   const unsigned table = static_cast<unsigned>((static_cast<int64_t>(a.batch) * a.maxp + kThreads - 1) / kThreads);

@@ -43,6 +43,30 @@ def test_update_of_nothing(lib):
     assert got[1].tolist() == [0, 2, 0, 1] and got[4].tolist() == [0, 0]
 
 
+# the update in one launch: 60 KB of counts, writers and rows, 8192 entries of both tables
+@pytest.mark.parametrize("rows,m,pages", [(32, 40, 7506), (32, 40, 7507), (44, 128, 900), (45, 128, 900), (44, 129, 900),
+                                          (44, 100, 900), (480, 16, 3600), (492, 16, 3600), (493, 16, 3600), (1, 16, 300)])
+def test_update_at_the_borders_of_one_launch(lib, rows, m, pages):
+    test_update_at_the_borders_of_the_one_launch_placement(lib, rows, m, pages)
+
+
+# compaction in one launch: 8192 pages, 262144 pages and entries
+@pytest.mark.parametrize("pages,batch,m", [(8191, 20, 16), (8192, 20, 16), (8193, 20, 16), (70000, 20, 16), (4096, 16, 16128),
+                                           (4096, 16, 16129), (63, 3, 16), (64, 3, 16), (65, 3, 16)])
+@pytest.mark.parametrize("live", [0.1, 0.9, 1.0])
+def test_compact_at_the_borders_of_one_launch(lib, pages, batch, m, live):
+    import torch
+    rng = np.random.default_rng(pages + m)
+    count = (rng.random(pages) < live).astype(np.int32) * rng.integers(1, 4, pages).astype(np.int32)
+    lens = rng.integers(0, 16 * min(m, 40), batch).astype(np.int32)
+    table = rng.integers(-2, pages + 2, (batch, m)).astype(np.int32)
+    out = [torch.full(s, 77, dtype=torch.int32, device="cuda") for s in (table.shape, (pages,), (pages,), (pages,), (pages,), (2,))]
+    log(f"compact pages={pages} batch={batch} width={m} live={live}")
+    lib.pages_compact(torch_any(table), torch_any(lens), torch_any(count), *out, page_size=16)
+    for name, a, b in zip(("table", "refcount", "map", "src", "dst", "info"), out, C.pages_compact(table, lens, count, 16)):
+        assert np.array_equal(a.cpu().numpy(), b), name
+
+
 # (head_dim, Hq, Hkv, page, lengths, query tokens, window, sinks): the last tokens of a sequence, the far
 # end of a window and the sinks lie in different steps, in one step, in a sequence shorter than its queries
 SHAPES = [
