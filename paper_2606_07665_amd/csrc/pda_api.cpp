@@ -208,7 +208,7 @@ struct Form {
   int per_cu;           // workgroups of a compute unit that run together
   int64_t token_bytes;  // K and V of a token and kv head
   bool options;         // the compute path and the fused merge apply
-  bool light;           // 4-bit steps: small calls by small_plan_light
+  bool light;           // 4-bit steps: small calls by small_plan_light, whole sequences by plan_whole_light
 };
 Form bf16_form(int d, bool sinks = false) { return {pda::max_waves(d), 1, static_cast<int64_t>(d) * 4, !sinks, false}; }
 // Workgroups of 4 waves, as many as fill a CU's registers, where their LDS (the
@@ -326,28 +326,36 @@ constexpr int64_t kSmallCallBytes = int64_t{128} << 20;
 constexpr int64_t kSmallCallPieces = 32;
 constexpr int kDefaultMinSteps = 2;
 
-// Small calls over a 4-bit cache, whose steps are a quarter of the bytes: a wave
-// takes four of them before another is worth its partials and its place in the
-// merge (two where the call has fewer than 2048 in all; below 1024 the bf16
-// rule stands, which a 2048-token window of 1 sequence at 32:8 needs: 8.9 us, 9.8
-// by this one), and a workgroup the
-// fewest kv heads with which the fixed split still applies, its waves as step
-// phases that are joined in LDS.  Replayed from a graph over three caches, the
-// bf16 rules -> these: 8 x 2048 tokens at 32:8 heads 14.5 -> 12.0 us, 1 x 32768
-// at 64:8 20.7 -> 17.3, 2 x 16384 at 32:2 16.6 -> 12.1, 4 x 8192 at 8:2, D = 64
-// 10.8 -> 9.1, 16 sequences at 12:4, D = 256, under a 4096-token window 26.3 ->
-// 23.2; 1 x 4096 at 32:8 10.0 -> 9.9.
-constexpr int64_t kLightSteps = 1024;
+// Small calls over a 4-bit cache, whose steps are a quarter of the bytes.  A
+// workgroup takes the fewest kv heads with which the fixed split still applies,
+// its waves as step phases that are joined in LDS.  A wave takes as many steps as
+// leave a workgroup a CU, up to four, since another workgroup costs its partials
+// and its place in the merge; and as many, up to four too, as leave the merge of
+// a sequence 64 pieces (32 at head size 256, which are as wide).  us per call with
+// 1, 2, 3, 4 steps, the taken one in brackets: 1 x 4096 tokens at 32:8 heads
+// [9.0] 9.8 10.5 11.4, 1 x 8192 12.2 [10.1] 10.8 11.4, 1 x 12000 15.1 12.9 [11.0]
+// 11.6, 1 x 16384 15.6 13.9 15.0 [11.8], 1 x 32768 19.0 19.0 19.0 [16.5]; for the
+// merge: 1 x 12000 at 32:2 12.1 [10.7] 10.7 11.4, 1 x 32768 21.3 14.7 13.7 [13.2].
+// Where a workgroup a step and group of heads fit the CUs and leave the merge no
+// more than 32 pieces there is nothing to join in LDS: 1 x 1024 tokens at 32:8
+// 8.6 -> 8.0, two sequences of 40 to 614 at 12:4, D = 256 10.3 -> 9.4.
+constexpr int kLightMostSteps = 4;
 Plan small_plan_light(const Form& form, const Plan& dflt, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq,
                       int num_cus, int cols, int cap, int ms_opt) {
   const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu;
-  const int64_t steps = static_cast<int64_t>(batch) * hkv * steps_seq;
-  const int ms = ms_opt > 0 ? ms_opt : steps < 2 * kLightSteps ? 2 : 4;
   int h = dflt.hgs;
+  if (ms_opt == 0 && steps_seq <= 32 && steps_seq * batch * (hkv / h) <= num_cus)
+    return plan_for(form, h, batch, hkv, d, steps_seq, num_cus, cols, 1);
   if (cap == 0)
     for (h = 1; h < dflt.hgs; ++h)
       if (hkv % h == 0 && 2 * static_cast<int64_t>(batch) * (hkv / h) <= target) break;
-  return plan_for(form, h, batch, hkv, d, steps_seq, num_cus, cols, ms);
+  const int phases = form.max_waves / h;
+  auto per_wave = [&](int64_t steps, int64_t workgroups) {
+    const int64_t n = workgroups * phases;
+    return static_cast<int>(std::min<int64_t>(kLightMostSteps, (steps + n - 1) / n));
+  };
+  const int ms = std::max({1, per_wave(steps_seq * batch * (hkv / h), num_cus), per_wave(steps_seq, d == 256 ? 32 : 64)});
+  return plan_for(form, h, batch, hkv, d, steps_seq, num_cus, cols, ms_opt > 0 ? ms_opt : ms);
 }
 
 Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq, int num_cus, int cols) {
@@ -382,7 +390,7 @@ Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, in
   //    11.4 us by events, 16.7 -> 11.9 us per call replayed from a graph).
   const int64_t kv_bytes = static_cast<int64_t>(batch) * steps_seq * pda::kStep * hkv * form.token_bytes;
   const bool small = kv_bytes <= kSmallCallBytes;
-  if (small && form.light && batch * hkv * steps_seq >= kLightSteps) {
+  if (small && form.light) {
     dflt = small_plan_light(form, dflt, batch, hkv, d, steps_seq, num_cus, cols, cap, ms_opt);
   } else if (small) {
     if (ms_opt == 0 && dflt.grid > 1 && dflt.grid < static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu)
@@ -431,6 +439,17 @@ Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, in
   return dflt;
 }
 
+// A workgroup for h kv heads of each sequence.
+Plan whole_of(const Form& form, Plan pl, int h, int32_t batch, int32_t hkv, int64_t steps_seq) {
+  pl.hgs = h;
+  pl.waves = h * (form.max_waves / h);
+  pl.grid = static_cast<int>(static_cast<int64_t>(batch) * (hkv / h));
+  pl.chunks = 1;
+  pl.chunk_steps = static_cast<int>(steps_seq);
+  pl.fused = false;
+  return pl;  // (the split plan's workspace, unused, is kept: the same calls fit the same scratch)
+}
+
 // Whole sequences, one workgroup per (sequence, kv-head group) and nothing to
 // merge, for calls whose sequences are all short: the fewest kv heads a
 // workgroup that give every pair a CU of its own.  It is the fixed split with
@@ -453,15 +472,33 @@ Plan plan_whole(const Form& form, const Plan& split, int32_t batch, int32_t hkv,
   for (int h = 1; h <= max_waves; ++h) {
     if (hkv % h || static_cast<int64_t>(batch) * (hkv / h) > num_cus) continue;
     if (steps_seq * pda::kStep * h * form.token_bytes > most_kb * 1024) break;
-    pl.hgs = h;
-    pl.waves = h * (max_waves / h);
-    pl.grid = static_cast<int>(static_cast<int64_t>(batch) * (hkv / h));
-    pl.chunks = 1;
-    pl.chunk_steps = static_cast<int>(steps_seq);
-    pl.fused = false;
-    return pl;  // (the split plan's workspace, unused, is kept: the same calls fit the same scratch)
+    return whole_of(form, split, h, batch, hkv, steps_seq);
   }
   return pl;
+}
+
+// The same over a 4-bit cache, by the steps of a wave: up to four (two at head
+// size 256) where the device has room for a split, up to eight where the heads of
+// the batch alone are three in eight of its CUs (more than half at head size 256);
+// a workgroup a CU if that holds them, else as many as run together.  us per call, split -> whole: 1 x 256
+// tokens at 32:8 heads 8.2 -> 6.4, 1 x 512 8.1 -> 8.1, 1 x 1024 8.6 -> 11.4;
+// 64 x 512 15.1 -> 12.0, 64 x 1024 21.9 -> 18.1, 150 x 500 25.8 -> 21.9, 256 x 256
+// 29.1 -> 16.4; 12:4, D = 256, 16 x 256 10.4 -> 9.2, 16 x 512 10.8 -> 12.0, 24 x
+// 1000 14.6 -> 17.2, 64 x 1024 22.9 -> 18.7.
+Plan plan_whole_light(const Form& form, const Plan& split, int32_t batch, int32_t hkv, int32_t d, int64_t steps_seq,
+                      int num_cus) {
+  const int64_t pairs = static_cast<int64_t>(batch) * hkv;
+  const bool many = d == 256 ? 2 * pairs > num_cus : 8 * pairs >= 3 * static_cast<int64_t>(num_cus);
+  const int most = many ? 8 : d == 256 ? 2 : 4;
+  for (const int64_t room : {static_cast<int64_t>(num_cus), static_cast<int64_t>(num_cus) * form.per_cu})
+    for (int h = 1; h <= form.max_waves; ++h) {
+      if (hkv % h || pairs / h > room) continue;
+      if (steps_seq > most * (form.max_waves / h)) break;
+      return whole_of(form, split, h, batch, hkv, steps_seq);
+    }
+  Plan none = split;
+  none.grid = 0;
+  return none;
 }
 
 // The plan of a call: the split plan, or whole sequences where that is
@@ -471,7 +508,8 @@ Plan make_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, int64_t 
   if (split.chunks == 1 || !fixed_split() || (form.options && (compute_path() != 0 || fused_merge())) || kv_group_cap() ||
       min_steps_option() || blocks_per_cu() != 1)
     return split;
-  const Plan whole = plan_whole(form, split, batch, hkv, steps_seq, num_cus);
+  const Plan whole = form.light ? plan_whole_light(form, split, batch, hkv, d, steps_seq, num_cus)
+                                : plan_whole(form, split, batch, hkv, steps_seq, num_cus);
   return whole.grid > 0 ? whole : split;
 }
 

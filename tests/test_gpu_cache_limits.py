@@ -145,3 +145,24 @@ def test_keys_that_are_not_finite_reach_only_the_queries_that_see_them(lib):
     want = C.attend(w.q, oracle.bf16_to_f64(w.k_cache), oracle.bf16_to_f64(w.v_cache), w.block_table, w.context_lens, w.scale,
                     window, sinks)
     compare(run_sink(lib, w, window, sinks), want, "sink keys")
+
+
+# (head_dim, Hq, Hkv, page, batch, longest): each side of the rules for whole sequences and for the steps
+# of a wave
+PLANS = [(128, 32, 8, 16, 1, 512), (128, 32, 8, 16, 1, 528), (128, 8, 2, 16, 70, 1024), (128, 8, 2, 16, 70, 1040),
+         (128, 8, 8, 16, 100, 512), (128, 8, 8, 16, 100, 528), (128, 3, 3, 16, 90, 300), (256, 4, 4, 16, 16, 256),
+         (256, 4, 4, 16, 16, 272), (256, 4, 4, 16, 32, 1000), (256, 4, 4, 16, 64, 1024), (128, 4, 4, 16, 24, 1000), (128, 4, 4, 16, 23, 1000),
+         (256, 4, 4, 16, 140, 130), (64, 2, 2, 16, 200, 500),
+         (64, 2, 2, 16, 1, 8208), (128, 4, 2, 16, 1, 12000), (128, 8, 8, 16, 1, 8192), (256, 3, 1, 16, 1, 12000)]
+
+
+@pytest.mark.parametrize("d,hq,hkv,page,batch,longest", PLANS)
+def test_kv4_at_the_borders_of_its_plans(lib, d, hq, hkv, page, batch, longest):
+    rng = np.random.default_rng(batch + longest)
+    lens = rng.integers(0, 120, batch)
+    lens[batch // 2] = longest
+    w = build(lens.tolist(), hq, hkv, d, page, seed=batch + longest)
+    cache = quantised(w)
+    want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, w.scale)
+    log(f"kv4 plan D={d} {hq}:{hkv} B={batch} longest={longest}")
+    check(run_kv4(lib, w, cache), want, "plan")
