@@ -166,3 +166,37 @@ def test_kv4_at_the_borders_of_its_plans(lib, d, hq, hkv, page, batch, longest):
     want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, w.scale)
     log(f"kv4 plan D={d} {hq}:{hkv} B={batch} longest={longest}")
     check(run_kv4(lib, w, cache), want, "plan")
+
+
+@pytest.mark.parametrize("d,hq,hkv,page,batch,longest", PLANS[::2] + [(128, 32, 8, 16, 40, 3000), (128, 8, 8, 16, 3, 40000)])
+def test_a_reserve_covers_every_plan_of_its_sizes(lib, d, hq, hkv, page, batch, longest):
+    import torch
+    rng = np.random.default_rng(longest)
+    lens = rng.integers(0, 120, batch)
+    lens[0] = longest
+    w = build(lens.tolist(), hq, hkv, d, page, seed=longest, poison=False)
+    cache = [torch_any(t) for t in quantised(w)]
+    table, lens = torch_any(w.block_table), torch_any(w.context_lens)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    lib.release_workspaces()
+    lib.kv4_workspace_reserve(batch, hq, hkv, d, page, table.shape[1], stream=s)
+    most = 16 // (hq // hkv)
+    calls = [(tq, window, sinks) for tq in sorted({1, most}) for window, sinks in ((0, 0), (100, 4), (1000, 300))]
+    qs = [torch.randn((batch, tq, hq, d), device="cuda").bfloat16() for tq, _, _ in calls]
+    outs = [torch.zeros_like(q) for q in qs]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        for (_, window, sinks), q, out in zip(calls, qs, outs):
+            lib.paged_decode_attention_kv4(q, *cache, table, lens, out, float(w.scale), window=window, sinks=sinks)
+    for rep in range(3):
+        for out in outs:
+            out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for (_, window, sinks), q, out in zip(calls, qs, outs):
+            eager = torch.zeros_like(q)
+            lib.paged_decode_attention_kv4(q, *cache, table, lens, eager, float(w.scale), window=window, sinks=sinks)
+            torch.cuda.synchronize()
+            assert torch.equal(out, eager), (rep, window, sinks)
