@@ -365,8 +365,11 @@ Plan make_split_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, in
   // covers; with more than 8 columns (several query tokens) those writes
   // cost more than the longer token rows save, so at most 4 kv heads go
   // together (multiq: 191.4 -> 188.3 us per call; long70b and ragged, at 8
-  // columns or fewer, run slower with 4).
-  const int dflt_most = cols > 8 ? std::min(4, form.max_waves) : form.max_waves;
+  // columns or fewer, run slower with 4).  Over a 4-bit cache, whose steps are
+  // shorter beside the same partials, at most 2 (101 Zipf sequences with three
+  // queries at 40:8 heads 124.5 -> 119.3, 64 x U[128, 8192] with four at 32:8 71.2
+  // -> 70.2; at 4 columns 60.4 -> 63.3).
+  const int dflt_most = cols > 8 ? std::min(form.light ? 2 : 4, form.max_waves) : form.max_waves;
   const int most = cap > 0 && cap < form.max_waves ? cap : dflt_most;
   const int together = form.max_waves > 8 ? heads_of_waves(hkv, form.max_waves, most) : heads_per_group(hkv, most);
   Plan dflt = plan_for(form, together, batch, hkv, d, steps_seq, num_cus, cols, ms_opt > 0 ? ms_opt : kDefaultMinSteps);
