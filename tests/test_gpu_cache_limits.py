@@ -150,10 +150,10 @@ def test_keys_that_are_not_finite_reach_only_the_queries_that_see_them(lib):
 # (head_dim, Hq, Hkv, page, batch, longest): each side of the rules for whole sequences and for the steps
 # of a wave
 PLANS = [(128, 32, 8, 16, 1, 512), (128, 32, 8, 16, 1, 528), (128, 8, 2, 16, 70, 1024), (128, 8, 2, 16, 70, 1040),
-         (128, 8, 8, 16, 100, 512), (128, 8, 8, 16, 100, 528), (128, 3, 3, 16, 90, 300), (256, 4, 4, 16, 16, 256),
-         (256, 4, 4, 16, 16, 272), (256, 4, 4, 16, 32, 1000), (256, 4, 4, 16, 64, 1024), (128, 4, 4, 16, 24, 1000), (128, 4, 4, 16, 23, 1000),
-         (256, 4, 4, 16, 140, 130), (64, 2, 2, 16, 200, 500),
-         (64, 2, 2, 16, 1, 8208), (128, 4, 2, 16, 1, 12000), (128, 8, 8, 16, 1, 8192), (256, 3, 1, 16, 1, 12000)]
+         (128, 8, 8, 16, 100, 512), (128, 8, 8, 16, 100, 528), (128, 3, 3, 16, 90, 300), (128, 4, 4, 16, 24, 1000),
+         (128, 4, 4, 16, 23, 1000), (256, 4, 4, 16, 16, 256), (256, 4, 4, 16, 16, 272), (256, 4, 4, 16, 32, 1000),
+         (256, 4, 4, 16, 64, 1024), (256, 4, 4, 16, 140, 130), (64, 2, 2, 16, 200, 500), (64, 2, 2, 16, 1, 8208),
+         (128, 4, 2, 16, 1, 12000), (128, 8, 8, 16, 1, 8192), (256, 3, 1, 16, 1, 12000)]
 
 
 @pytest.mark.parametrize("d,hq,hkv,page,batch,longest", PLANS)
@@ -200,3 +200,19 @@ def test_a_reserve_covers_every_plan_of_its_sizes(lib, d, hq, hkv, page, batch, 
             lib.paged_decode_attention_kv4(q, *cache, table, lens, eager, float(w.scale), window=window, sinks=sinks)
             torch.cuda.synchronize()
             assert torch.equal(out, eager), (rep, window, sinks)
+
+
+# Batches whose prefix leaves LDS for one workgroup a CU only, of 12, 8 or 4 waves, with a sequence that is
+# split.
+@pytest.mark.parametrize("d,hq,hkv,batch,longest,tq,window", [(128, 8, 2, 3000, 2000, 1, 0), (128, 4, 1, 8192, 40, 1, 0),
+                                                              (128, 4, 4, 2500, 5000, 2, 60), (64, 4, 2, 5000, 3000, 1, 0),
+                                                              (256, 2, 1, 4000, 1500, 1, 0), (128, 3, 3, 3500, 700, 1, 0)])
+def test_kv4_very_large_batches(lib, d, hq, hkv, batch, longest, tq, window):
+    rng = np.random.default_rng(batch)
+    lens = rng.integers(0, 20, batch)
+    lens[batch // 3] = longest
+    w = build(lens.tolist(), hq, hkv, d, 16, seed=batch, num_queries=tq, window=window, sinks=4)
+    cache = quantised(w)
+    want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, w.scale, window, 4)
+    log(f"kv4 batch={batch} D={d} {hq}:{hkv} longest={longest}")
+    check(run_kv4(lib, w, cache, window, 4), want, "batch")
