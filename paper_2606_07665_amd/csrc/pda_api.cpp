@@ -1040,6 +1040,11 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
   if (window < 0) return fail(PDA_ERR_SHAPE, "window must be >= 0 (got %d)", window);
   if (sinks < 0) return fail(PDA_ERR_SHAPE, "num_sinks must be >= 0 (got %d)", sinks);
   if (window == 0) sinks = 0;  // every key is visible
+  // A window as long as the table hides nothing and no query sees more sinks than it holds; the kernels subtract a
+  // window from positions that go down to 1 - num_queries, in 32 bits.
+  const int32_t most_tokens = max_pages_per_seq * page_size;  // at most 2^30 (check_shape)
+  window = std::min(window, most_tokens);
+  sinks = std::min(sinks, most_tokens);
   if (num_queries > pda::kMaxCols || num_queries * (num_q_heads / num_kv_heads) > pda::kMaxCols)
     return fail(PDA_ERR_UNSUPPORTED, "num_queries %d x query group %d exceeds %d", num_queries,
                 num_q_heads / num_kv_heads, pda::kMaxCols);

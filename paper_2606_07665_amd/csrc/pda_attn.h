@@ -34,7 +34,8 @@ __device__ __forceinline__ int clamp_len(int L, int max_ctx) {
 // 32-token steps from the one holding seq_start to the end.  With S > 0 sinks
 // (a window only) every query sees the keys t < S as well: the sequence then
 // has the sink_steps steps that hold them ahead of the window's, those before
-// the window's first step.
+// the window's first step.  (window and sinks are at most the tokens of a
+// table, 2^30: nothing here passes 32 bits.)
 __device__ __forceinline__ int seq_start(int L, int nq, int window) {
   if (window <= 0) return 0;
   const int s = L - nq + 1 - window;

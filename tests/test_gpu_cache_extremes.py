@@ -1,0 +1,62 @@
+"""The cache operators at the ends of what their arguments can hold, against the fp64 reference."""
+import numpy as np
+import pytest
+
+import oracle
+from _cache import build, torch_any, torch_bf16
+from _gpu import check, log
+from oracle import cache as C
+from test_gpu_kv4 import quantised
+from test_gpu_kv4 import run as run_kv4
+from test_gpu_sink import run as run_sink
+
+pytestmark = pytest.mark.gpu
+
+INT_MAX = 2 ** 31 - 1
+
+
+@pytest.fixture(scope="module")
+def lib(gpu_lib):
+    return gpu_lib
+
+
+def run_ext(lib, w, window):
+    import torch
+    q = torch_bf16(w.q)
+    out = torch.full(tuple(q.shape), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lib.paged_decode_attention_ext(q, torch_bf16(w.k_cache), torch_bf16(w.v_cache), torch_any(w.block_table),
+                                   torch_any(w.context_lens), out, float(w.scale), window=window)
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy().astype(np.float64)
+
+
+# ------------------------------------------------------------ window and sinks
+# (head_dim, Hq, Hkv, page, lengths, query tokens): sequences shorter than their queries, idle slots alone and
+# beside others
+SHORT = [(128, 32, 8, 16, [0, 1, 2, 5, 33, 700], 4), (128, 8, 8, 16, [0, 13, 15, 3000], 16), (64, 6, 2, 32, [0, 0, 0], 5),
+         (256, 12, 4, 16, [0, 1, 64, 500], 3), (64, 4, 2, 64, [1], 8)]
+
+
+@pytest.mark.parametrize("fixed", [0, 1])
+@pytest.mark.parametrize("window", [INT_MAX, INT_MAX - 1, INT_MAX - 14, 1 << 30])
+@pytest.mark.parametrize("d,hq,hkv,page,lens,tq", SHORT, ids=[f"D{c[0]}-{c[1]}:{c[2]}-T{c[5]}" for c in SHORT])
+def test_a_window_past_every_position_hides_nothing(lib, d, hq, hkv, page, lens, tq, window, fixed):
+    w = build(lens, hq, hkv, d, page, seed=sum(lens) + tq, num_queries=tq)
+    cache = quantised(w)
+    log(f"window {window} D={d} {hq}:{hkv} lens={lens} Tq={tq} fixed={fixed}")
+    lib.set_option(lib.OPT_FIXED_SPLIT, fixed)
+    try:
+        bf16 = C.attend(w.q, oracle.bf16_to_f64(w.k_cache), oracle.bf16_to_f64(w.v_cache), w.block_table, w.context_lens, w.scale)
+        check(run_ext(lib, w, window), bf16, "ext")
+        kv4 = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, w.scale)
+        for sinks in (0, 4, INT_MAX):
+            check(run_sink(lib, w, window, sinks), bf16, f"sink {sinks}")
+            check(run_kv4(lib, w, cache, window, sinks), kv4, f"kv4 {sinks}")
+    finally:
+        lib.set_option(lib.OPT_FIXED_SPLIT, 1)
+
+
+def test_sinks_past_every_position_leave_nothing_hidden(lib):
+    w = build([0, 3, 700], 32, 8, 128, 16, seed=31, num_queries=4)
+    want = C.attend(w.q, oracle.bf16_to_f64(w.k_cache), oracle.bf16_to_f64(w.v_cache), w.block_table, w.context_lens, w.scale)
+    check(run_sink(lib, w, 7, INT_MAX), want, "sink")
