@@ -258,13 +258,15 @@ int paged_decode_attention_sink(const void* q, const void* k_cache, const void* 
  * among its elements, so its largest element lies in [4, 8) units of
  * 2^(s - 127); elements are rounded to the nearest code, ties to the even one,
  * and those past 6 units become 6.  A group with an infinity or a NaN gets
- * s = 255.  Only the slots of these tokens change.
+ * s = 255.  Only the slots of these tokens change; a token whose table entry is
+ * outside [0, num_pages) writes nothing.
  *
  * pda_kv4_read -- the last num_tokens tokens of each sequence as the bf16
  * values they stand for (exact: a code times a power of two; only the scales
  * 253 and 254, which pda_kv4_append never writes, reach past bf16's range, to
- * infinities), as chunked prefill attends to them: k_out, v_out bf16 [batch, num_tokens, num_kv_heads,
- * head_dim]; positions below 0 give zeros.
+ * infinities), as chunked prefill attends to them: k_out, v_out bf16
+ * [batch, num_tokens, num_kv_heads, head_dim]; positions below 0 and table
+ * entries outside [0, num_pages) give zeros.
  *
  * Both: asynchronous on `stream`, no workspace, no allocation.
  */

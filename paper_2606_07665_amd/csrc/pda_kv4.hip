@@ -53,8 +53,8 @@ struct Kv4Lane {
   int t;          // position in the sequence
   int j;          // token of the call
   int g, grp;     // kv head, group
-  int64_t chunk;  // index of the group's 16 bytes of codes, and of its scale
-  bool in;        // the call has this token (chunk is valid only where t >= 0)
+  int64_t chunk;  // index of the group's 16 bytes of codes, and of its scale; -1: its token has no page
+  bool in;        // the call has this token
 };
 
 template <int D, int kTile>
@@ -75,11 +75,14 @@ __device__ __forceinline__ Kv4Lane kv4_lane(const Kv4Args& a) {
   p.in = p.j >= 0 && p.j < a.tokens;
   p.g = hp / kPairs;
   p.grp = (hp % kPairs) * 2 + ((threadIdx.x & 7) >> 2);
-  p.chunk = 0;
+  p.chunk = -1;
   if (p.in && p.t >= 0) {
+    // an entry outside the pool (a page that was lacking, or was released) is no
+    // page: clamped into the pool it would be another sequence's
     const unsigned raw = static_cast<unsigned>(a.bt[static_cast<int64_t>(b) * a.maxp + (p.t >> a.page_shift)]);
-    const int64_t page = raw < static_cast<unsigned>(a.num_pages) ? raw : a.num_pages - 1;
-    p.chunk = (((page * a.hkv + p.g) * kGroups + p.grp) << a.page_shift) + (p.t & ((1 << a.page_shift) - 1));
+    const int64_t page = raw;
+    if (raw < static_cast<unsigned>(a.num_pages))
+      p.chunk = (((page * a.hkv + p.g) * kGroups + p.grp) << a.page_shift) + (p.t & ((1 << a.page_shift) - 1));
   }
   return p;
 }
@@ -94,9 +97,9 @@ template <int D, int kTile>
 __global__ __launch_bounds__(kKv4Threads) void kv4_append_kernel(Kv4Args a, const uint16_t* __restrict__ k_new,
                                                                  const uint16_t* __restrict__ v_new) {
   const Kv4Lane p = kv4_lane<D, kTile>(a);
-  // (a run past the last token, or a lane before the first: its four lanes
-  // stay together for the exchange below, as they are of one token)
-  if (!p.in || p.t < 0) return;
+  // (a run past the last token, a lane before the first, or no page: the four
+  // lanes of the exchange below stay together, as they are of one token)
+  if (p.chunk < 0) return;
   const u32x4 x = ld16((blockIdx.z ? v_new : k_new) + kv4_row<D>(a, p));
   // the group's largest biased exponent: of 8 elements in the lane, then of
   // its 4 lanes
@@ -127,7 +130,7 @@ __global__ __launch_bounds__(kKv4Threads) void kv4_read_kernel(Kv4Args a, uint16
   const Kv4Lane p = kv4_lane<D, kTile>(a);
   if (!p.in) return;
   bf16x8 y = {};
-  if (p.t >= 0) {
+  if (p.chunk >= 0) {
     const unsigned w = reinterpret_cast<const unsigned*>((blockIdx.z ? a.v : a.k) + 16 * p.chunk)[threadIdx.x & 3];
     y = decode8(w, scale_of((blockIdx.z ? a.vs : a.ks)[p.chunk]));
   }

@@ -60,3 +60,45 @@ def test_sinks_past_every_position_leave_nothing_hidden(lib):
     w = build([0, 3, 700], 32, 8, 128, 16, seed=31, num_queries=4)
     want = C.attend(w.q, oracle.bf16_to_f64(w.k_cache), oracle.bf16_to_f64(w.v_cache), w.block_table, w.context_lens, w.scale)
     check(run_sink(lib, w, 7, INT_MAX), want, "sink")
+
+
+# ------------------------------------------------------- tokens without a page
+# (head_dim, kv heads, page, tokens, length): single tokens and runs of eight
+NOWHERE = [(128, 8, 16, 1, 40), (64, 2, 16, 5, 40), (256, 2, 32, 40, 100), (128, 3, 16, 33, 70)]
+
+
+@pytest.mark.parametrize("entry", [-1, -7, 2 ** 31 - 1, None])  # None: the first number past the pool
+@pytest.mark.parametrize("d,hkv,page,tokens,length", NOWHERE)
+def test_kv4_tokens_without_a_page_go_nowhere(lib, d, hkv, page, tokens, length, entry):
+    import torch
+    rng = np.random.default_rng(d + tokens)
+    pages = 30
+    codes = rng.integers(0, 256, (2, pages, hkv, d // 32, page, 16), np.uint8)
+    scales = rng.integers(0, 255, (2, pages, hkv, d // 32, page), np.uint8)
+    used = -(-length // page)
+    table = np.full((2, used), -1, np.int32)
+    table[0] = rng.choice(pages - 1, used, replace=False)  # the last page is nobody's
+    table[1] = pages if entry is None else entry            # the second sequence has no page at all
+    table[0, -2] = table[1, 0]                              # the first lacks its last page but one
+    lens = np.array([length, length - 1], np.int32)
+    new = [rng.integers(0, 0x7F80, (2, tokens, hkv, d)).astype(np.uint16) for _ in range(2)]
+    dev = [torch_any(x) for x in (codes[0], scales[0], codes[1], scales[1])]
+    bt, cl = torch_any(table), torch_any(lens)
+    log(f"kv4 without a page D={d} P={page} T={tokens} entry={entry}")
+    lib.kv4_append(torch_bf16(new[0]), torch_bf16(new[1]), *dev, bt, cl)
+    back = [torch.full((2, tokens, hkv, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lib.kv4_read(*back, *dev, bt, cl)
+    torch.cuda.synchronize()
+    t = lens[0] - tokens + np.arange(tokens)  # the first sequence's tokens, those with a page
+    here = [j for j in range(tokens) if t[j] >= 0 and t[j] // page != used - 2]
+    for i in range(2):
+        c, s = codes[i].copy(), scales[i].copy()
+        for j in here:
+            qc, qs = C.kv4_quantise(new[i][0, j])
+            c[table[0, t[j] // page], :, :, t[j] % page] = qc
+            s[table[0, t[j] // page], :, :, t[j] % page] = qs
+        assert np.array_equal(dev[2 * i].cpu().numpy(), c) and np.array_equal(dev[2 * i + 1].cpu().numpy(), s)
+        got = back[i].float().cpu().numpy()
+        assert (got[1] == 0).all() and (np.delete(got[0], here, axis=0) == 0).all()
+        want = C.kv4_values(*C.kv4_quantise(new[i][0, here])).reshape(len(here), hkv, d)
+        assert np.array_equal(got[0, here], want.astype(np.float32))
