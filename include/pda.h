@@ -44,7 +44,8 @@
  * thread-local message readable with pda_last_error().  Argument checks run
  * before any HIP call; on an argument error nothing is launched and `out` is
  * untouched.  Device-resident contents are not validated: page ids outside
- * [0, num_pages) are clamped into range and lengths are clamped to
+ * [0, num_pages) are clamped into range where a cache is read (a call that
+ * writes one drops the token) and lengths are clamped to
  * [0, max_pages_per_seq * page_size], so bad contents give unspecified
  * values but never an out-of-bounds access.
  */
@@ -392,7 +393,8 @@ int pda_pages_workspace_reserve(int32_t rows, int32_t num_pages, void* stream);
  *   context_lens  int32 [batch] on the device, already counting the new token:
  *                 sequence b's vectors go to position L_b - 1, i.e. page
  *                 block_table[b, (L_b-1) / page_size], slot (L_b-1) % page_size,
- *                 every kv head.  L_b = 0 writes nothing.
+ *                 every kv head.  L_b = 0 writes nothing, and so does a token
+ *                 whose block_table entry is outside [0, num_pages).
  * Only those slots change.  Two sequences whose page tables send their new
  * token to the same slot race (the page table must not do that).
  * Asynchronous on `stream`; no workspace, no allocation (graph-capturable).
@@ -698,7 +700,8 @@ int pda_attention_prelude(const void* x, const void* w_packed, const void* bias,
  * position context_lens[b] - 1, as pda_kv_append would, and q to q_out.
  * k_cache, v_cache, block_table, page_size, num_pages and max_pages_per_seq
  * as for paged_decode_attention (caches written in place, only those slots);
- * sequences with length 0 append nothing.  Other arguments and errors as
+ * sequences with length 0, or whose block_table entry there is outside
+ * [0, num_pages), append nothing.  Other arguments and errors as
  * for pda_attention_prelude.
  */
 int pda_attention_prelude_append(const void* x, const void* w_packed, const void* bias,

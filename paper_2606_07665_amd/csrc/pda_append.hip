@@ -13,9 +13,10 @@
 // thread per 16-byte chunk, so each (sequence, kv head) row of D bf16 is
 // moved by D/8 consecutive lanes with 16-byte accesses.
 //
-// Page ids and lengths read from device memory are clamped into range (a
-// length into [0, maxp*P], a page id into [0, num_pages)), so bad device
-// contents cannot address outside the pool.
+// Lengths read from device memory are clamped into [0, maxp*P], and a token
+// whose page id lies outside [0, num_pages) is dropped (clamped it would land
+// in what may be another sequence's page), so bad device contents cannot
+// address outside the pool.
 #include "pda_append.h"
 
 namespace pda {
@@ -46,7 +47,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(
   const int t = L - tokens + j;                     // this token's position
   if (t < 0) return;
   const unsigned raw = static_cast<unsigned>(bt[static_cast<int64_t>(b) * maxp + (t >> page_shift)]);
-  const int64_t page = raw < static_cast<unsigned>(num_pages) ? raw : num_pages - 1;
+  if (raw >= static_cast<unsigned>(num_pages)) return;
+  const int64_t page = raw;
   const int slot = t & ((1 << page_shift) - 1);
 
   const int64_t dst = (((page << page_shift) + slot) * hkv + g) * D + 8 * chunk;

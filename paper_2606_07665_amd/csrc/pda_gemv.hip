@@ -542,8 +542,9 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
         uint16_t* out = is_k ? e.k_out : e.v_out;
         if (out) dst = out + (b * e.hkv + g) * e.d;
         const int at = clamped(pos[t], e.maxp << e.page_shift) - 1;
-        if (e.k_cache && at >= 0) {  // length 0: no token in this slot, nothing to append
-          const int64_t page = page_id[t] < static_cast<uint32_t>(e.num_pages) ? page_id[t] : e.num_pages - 1;
+        // length 0: no token in this slot, nothing to append; nor to an entry that is no page
+        if (e.k_cache && at >= 0 && page_id[t] < static_cast<uint32_t>(e.num_pages)) {
+          const int64_t page = page_id[t];
           const int64_t row = (page << e.page_shift) + (at & ((1 << e.page_shift) - 1));
           uint16_t* cache = (is_k ? e.k_cache : e.v_cache) + (row * e.hkv + g) * e.d;
           store_bf16<kRows>(cache + eA, v[0]);
@@ -716,7 +717,8 @@ __global__ __launch_bounds__(64) void prelude_epilogue(PreludeArgs a) {
     } else {
       const int t = Lc - 1;
       const unsigned raw = static_cast<unsigned>(a.bt[static_cast<int64_t>(b) * a.maxp + (t >> a.page_shift)]);
-      const int64_t page = raw < static_cast<unsigned>(a.num_pages) ? raw : a.num_pages - 1;
+      const int64_t page = raw;
+      if (raw >= static_cast<unsigned>(a.num_pages)) cache = nullptr;  // the entry is no page
       row = (((page << a.page_shift) + (t & ((1 << a.page_shift) - 1))) * a.hkv + g) * D;
     }
   }

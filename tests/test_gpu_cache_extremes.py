@@ -102,3 +102,72 @@ def test_kv4_tokens_without_a_page_go_nowhere(lib, d, hkv, page, tokens, length,
         assert (got[1] == 0).all() and (np.delete(got[0], here, axis=0) == 0).all()
         want = C.kv4_values(*C.kv4_quantise(new[i][0, here])).reshape(len(here), hkv, d)
         assert np.array_equal(got[0, here], want.astype(np.float32))
+
+
+@pytest.mark.parametrize("entry", [-1, 2 ** 31 - 1, None])
+@pytest.mark.parametrize("d,hkv,page,tokens,length", NOWHERE + [(128, 2, 1, 7, 20), (64, 4, 4, 1, 9)])
+def test_bf16_tokens_without_a_page_go_nowhere(lib, d, hkv, page, tokens, length, entry):
+    import torch
+    rng = np.random.default_rng(d + tokens)
+    used = -(-length // page)
+    pages = 3 * used
+    pools = rng.integers(0, 0x7F80, (2, pages, page, hkv, d)).astype(np.uint16)
+    table = np.full((2, used), -1, np.int32)
+    table[0] = rng.choice(pages - 1, used, replace=False)
+    table[1] = pages if entry is None else entry
+    table[0, -2] = table[1, 0]
+    lens = np.array([length, length - 1], np.int32)
+    new = rng.integers(0, 0x7F80, (2, 2, tokens, hkv, d)).astype(np.uint16)
+    dev = [torch_bf16(p) for p in pools]
+    log(f"bf16 without a page D={d} P={page} T={tokens} entry={entry}")
+    lib.kv_append_n(torch_bf16(new[0]), torch_bf16(new[1]), *dev, torch_any(table), torch_any(lens))
+    torch.cuda.synchronize()
+    for i in range(2):
+        want = pools[i].copy()
+        for j in range(tokens):
+            t = length - tokens + j
+            if t >= 0 and t // page != used - 2:
+                want[table[0, t // page], t % page] = new[i][0, j]
+        assert np.array_equal(dev[i].view(torch.int16).cpu().numpy().view(np.uint16), want)
+
+
+# (batch, hidden, Hq, Hkv, D, q/k norm): without a norm the projection's workgroups finish the prelude, with one
+# a second kernel does
+@pytest.mark.parametrize("entry", [-1, None])
+@pytest.mark.parametrize("b,hidden,hq,hkv,d,norm", [
+    (1, 2560, 32, 8, 128, False), (6, 512, 8, 2, 128, True), (8, 4096, 32, 2, 128, False), (64, 1024, 8, 2, 128, False),
+    (100, 512, 4, 2, 128, True), (256, 512, 8, 2, 128, False), (16, 768, 12, 4, 256, True), (16, 768, 12, 4, 256, False),
+    (3, 1024, 4, 2, 64, True)])
+def test_a_prelude_appends_nothing_without_a_page(lib, b, hidden, hq, hkv, d, norm, entry):
+    import torch
+    rng = np.random.default_rng(b + hidden)
+    plan = lib.prelude_plan(lib.prelude_dims(b, hidden, hq, hkv, d, d, False, 1e5, 1e-6), norm)
+    assert bool(plan.fused) == (not norm)
+    page, used = 16, 3
+    lens = rng.integers(1, page * used + 1, b).astype(np.int32)
+    pages = used * b + 5
+    table = rng.permutation(pages - 1)[:used * b].reshape(b, used).astype(np.int32)  # the last page is nobody's
+    lost = [r for r in range(b) if r % 2 == 0]
+    for r in lost:
+        table[r, (lens[r] - 1) // page] = pages if entry is None else entry
+    pools = [rng.integers(0, 0x7F80, (pages, page, hkv, d)).astype(np.uint16) for _ in range(2)]
+    x = torch.randn((b, hidden), device="cuda").bfloat16()
+    wp = lib.pack_weights((torch.randn(((hq + 2 * hkv) * d, hidden), device="cuda") * hidden ** -0.5).bfloat16())
+    norms = dict(q_norm=torch.ones(d, dtype=torch.bfloat16, device="cuda"),
+                 k_norm=torch.ones(d, dtype=torch.bfloat16, device="cuda")) if norm else {}
+    shape = dict(num_q_heads=hq, num_kv_heads=hkv, head_dim=d, rope_theta=1e5, **norms)
+    q, q2 = (torch.empty((b, hq, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k, v = (torch.empty((b, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cl, dev = torch_any(lens), [torch_bf16(p) for p in pools]
+    log(f"prelude without a page B={b} {hq}:{hkv} D={d} norm={norm} entry={entry}")
+    lib.attention_prelude(x, wp, cl, q, k, v, **shape)
+    lib.attention_prelude_append(x, wp, cl, q2, *dev, torch_any(table), **shape)
+    torch.cuda.synchronize()
+    assert torch.equal(q, q2)
+    for pool, new, got in zip(pools, (k, v), dev):
+        want, rows = pool.copy(), new.view(torch.int16).cpu().numpy().view(np.uint16)
+        for r in range(b):
+            if r not in lost:
+                t = lens[r] - 1
+                want[table[r, t // page], t % page] = rows[r]
+        assert np.array_equal(got.view(torch.int16).cpu().numpy().view(np.uint16), want)
