@@ -509,8 +509,11 @@ int pda_release_workspaces(void);
  * Returns PDA_OK, or PDA_ERR_SHAPE naming the first bad entry.  The kernels
  * never trust these device contents (out-of-range values are clamped, so a
  * bad table gives wrong numbers but no fault); with PDA_DEBUG_VALIDATE=1 in
- * the environment, every attention and append call runs this check first
- * (synchronising; skipped while the stream is being captured).
+ * the environment, every attention and append call, and a 4-bit cache's read
+ * back, runs this check first (synchronising; skipped while the stream is being
+ * captured), on the pages of the tokens that the call touches: those that its
+ * queries see under a window with sinks, or the last num_tokens.  The others
+ * may have been released.
  */
 int pda_validate_paging(const int32_t* block_table, const int32_t* context_lens, int32_t batch,
                         int32_t max_pages_per_seq, int32_t page_size, int32_t num_pages, void* stream);

@@ -713,10 +713,24 @@ int prof_read(int kind, double* first_ms, double* second_ms, int64_t* calls) {
 }
 
 // ---------------------------------------------------------------- validation
+// The tokens of a sequence that a call touches: all of them, what its queries
+// see under a window with sinks, or the last so many (an append, a read back).
+struct Touched {
+  int32_t num_queries = 1, window = 0, sinks = 0;
+  int32_t tokens = 0;  // > 0: the last so many
+  // Of a sequence of `len` tokens: [0, pinned) and [first, len).
+  void of(int64_t len, int64_t* pinned, int64_t* first) const {
+    const int64_t before = tokens > 0 ? len - tokens : window > 0 ? len - num_queries + 1 - window : 0;
+    *first = std::max<int64_t>(before, 0);
+    *pinned = tokens > 0 ? 0 : std::min<int64_t>(sinks, *first);
+  }
+};
+
 // Host-side check of the device page tables and lengths (debugging aid):
-// synchronises the stream and copies both to the host.
+// synchronises the stream and copies both to the host.  Pages without a
+// touched token may have been released: any entry.
 int validate_paging(const int32_t* block_table, const int32_t* context_lens, int32_t batch, int32_t maxp,
-                    int32_t page_size, int32_t num_pages, hipStream_t st) {
+                    int32_t page_size, int32_t num_pages, const Touched& touched, hipStream_t st) {
   std::vector<int32_t> lens(batch), bt(static_cast<size_t>(batch) * maxp);
   hipError_t e = hipMemcpyAsync(lens.data(), context_lens, lens.size() * 4, hipMemcpyDeviceToHost, st);
   if (e == hipSuccess)
@@ -728,8 +742,12 @@ int validate_paging(const int32_t* block_table, const int32_t* context_lens, int
     if (lens[b] < 0 || lens[b] > max_ctx)
       return fail(PDA_ERR_SHAPE, "context_lens[%d] = %d outside [0, %lld]", b, lens[b],
                   static_cast<long long>(max_ctx));
+    int64_t pinned, first;
+    touched.of(lens[b], &pinned, &first);
     const int32_t pages = (lens[b] + page_size - 1) / page_size;
     for (int32_t j = 0; j < pages; ++j) {
+      const int64_t t = static_cast<int64_t>(j) * page_size;
+      if (t >= pinned && t + page_size <= first) continue;
       const int32_t id = bt[static_cast<size_t>(b) * maxp + j];
       if (id < 0 || id >= num_pages)
         return fail(PDA_ERR_SHAPE, "block_table[%d][%d] = %d outside [0, %d)", b, j, id, num_pages);
@@ -746,13 +764,18 @@ bool debug_validate() {
 }
 
 int maybe_validate(const int32_t* block_table, const int32_t* context_lens, int32_t batch, int32_t maxp,
-                   int32_t page_size, int32_t num_pages, hipStream_t st) {
+                   int32_t page_size, int32_t num_pages, const Touched& touched, hipStream_t st) {
   if (!debug_validate()) return PDA_OK;
   hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(st, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) return PDA_OK;
-  return validate_paging(block_table, context_lens, batch, maxp, page_size, num_pages, st);
+  return validate_paging(block_table, context_lens, batch, maxp, page_size, num_pages, touched, st);
 }
 
+Touched last_tokens(int32_t n) {
+  Touched t;
+  t.tokens = n;
+  return t;
+}
 
 // ---------------------------------------------------------------- descriptors
 const char* dtype_name(int32_t dt) {
@@ -1001,7 +1024,7 @@ int check_kv4_tokens(pda::Kv4Args* c, const void* k, const void* v, const void* 
     return fail(PDA_ERR_ALIGN, "keys, values and codes must be 16-byte aligned");
   if (misaligned(block_table, 4) || misaligned(context_lens, 4))
     return fail(PDA_ERR_ALIGN, "block_table and context_lens must be 4-byte aligned");
-  if ((rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages,
+  if ((rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages, last_tokens(num_tokens),
                            static_cast<hipStream_t>(stream))))
     return rc;
   c->k = static_cast<uint8_t*>(const_cast<void*>(k_codes));
@@ -1060,8 +1083,8 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
     return fail(PDA_ERR_ALIGN, "q, %s and out must be 16-byte aligned", kv4 ? "k_codes, v_codes" : "k_cache, v_cache");
   if (misaligned(block_table, 4) || misaligned(context_lens, 4))
     return fail(PDA_ERR_ALIGN, "block_table and context_lens must be 4-byte aligned");
-  if (!noalloc && (rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size,
-                                       num_pages, static_cast<hipStream_t>(stream))))
+  if (!noalloc && (rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages,
+                                       Touched{num_queries, window, sinks, 0}, static_cast<hipStream_t>(stream))))
     return rc;
 
   int dev = 0;
@@ -1385,7 +1408,7 @@ int pda_kv_append_n(const void* k_new, const void* v_new, void* k_cache, void* v
     return fail(PDA_ERR_ALIGN, "k_new, v_new, k_cache and v_cache must be 16-byte aligned");
   if (misaligned(block_table, 4) || misaligned(context_lens, 4))
     return fail(PDA_ERR_ALIGN, "block_table and context_lens must be 4-byte aligned");
-  if ((rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages,
+  if ((rc = maybe_validate(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages, last_tokens(num_tokens),
                            static_cast<hipStream_t>(stream))))
     return rc;
   pda::AppendArgs a;
@@ -1687,7 +1710,7 @@ int pda_validate_paging(const int32_t* block_table, const int32_t* context_lens,
   if (!block_table || !context_lens) return fail(PDA_ERR_NULL, "a tensor pointer is NULL");
   if (static_cast<int64_t>(batch) * max_pages_per_seq > (int64_t{1} << 31))
     return fail(PDA_ERR_SHAPE, "block_table too large to validate");
-  return validate_paging(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages,
+  return validate_paging(block_table, context_lens, batch, max_pages_per_seq, page_size, num_pages, Touched{},
                          static_cast<hipStream_t>(stream));
 }
 

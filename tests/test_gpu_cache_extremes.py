@@ -171,3 +171,69 @@ def test_a_prelude_appends_nothing_without_a_page(lib, b, hidden, hq, hkv, d, no
                 t = lens[r] - 1
                 want[table[r, t // page], t % page] = rows[r]
         assert np.array_equal(got.view(torch.int16).cpu().numpy().view(np.uint16), want)
+
+
+# --------------------------------------------------- the checks of a debugging run
+VALIDATED = """
+import sys, torch
+sys.path.insert(0, '.')
+from paper_2606_07665_amd import binding as B
+dev = dict(dtype=torch.int32, device='cuda')
+N, P, M, HQ, HKV, D, W, S, T = 80, 16, 40, 8, 2, 128, 50, 20, 3
+table, lens = torch.arange(80, **dev).reshape(2, M), torch.tensor([400, 600], **dev)
+ref = (torch.arange(80, device='cuda') < 25).int() + ((torch.arange(80, device='cuda') >= 40) & (torch.arange(80, device='cuda') < 78)).int()
+new = torch.tensor([403, 603], **dev)
+t2, r2, src, dst, info = torch.empty_like(table), torch.empty_like(ref), torch.empty(2, **dev), torch.empty(2, **dev), torch.empty(2, **dev)
+B.pages_update(table, lens, None, new, ref, t2, r2, src, dst, info, page_size=P, window=W, sinks=S, num_queries=T)
+held = (t2 >= 0).sum(dim=1).tolist()
+assert held[0] < 10 and held[1] < 10, held          # most pages are released
+k, v = (torch.randn((N, P, HKV, D), device='cuda').bfloat16() for _ in range(2))
+c4 = [*B.kv4_cache(N, P, HKV, D), *B.kv4_cache(N, P, HKV, D)]
+q = torch.randn((2, T, HQ, D), device='cuda').bfloat16()
+out, kn = torch.zeros_like(q), torch.randn((2, T, HKV, D), device='cuda').bfloat16()
+calls = dict(
+    sink=lambda t: B.paged_decode_attention_sink(q, k, v, t, new, out, 0.1, window=W, sinks=S),
+    kv4=lambda t: B.paged_decode_attention_kv4(q, *c4, t, new, out, 0.1, window=W, sinks=S),
+    append=lambda t: B.kv4_append(kn, kn, *c4, t, new),
+    read=lambda t: B.kv4_read(kn, kn.clone(), *c4, t, new),
+    bf16=lambda t: B.kv_append_n(kn, kn, k, v, t, new))
+ext = lambda t: B.paged_decode_attention_ext(q, k, v, t, new, out, 0.1, window=W)
+
+def refused(call, t):
+    try:
+        call(t)
+        return ''
+    except B.PdaError as e:
+        return str(e)
+
+for name, call in calls.items():
+    assert not refused(call, t2), name
+    last = t2.clone()
+    last[1, 602 // P] = -1
+    assert 'block_table[1][37]' in refused(call, last), name
+    bad = t2.clone()
+    bad[0, 1] = N + 3                                # the sinks' second page: attention sees it, the others do not
+    assert ('block_table[0][1]' in refused(call, bad)) == (name in ('sink', 'kv4')), name
+gone = t2.clone()
+gone[:, :2] = -1
+assert not refused(ext, gone) and 'block_table[0][0]' in refused(calls['sink'], gone)
+first = (403 - T + 1 - W) // P                       # the window's first page, and the one before it
+edge = t2.clone()
+edge[0, first - 1] = N
+assert not refused(ext, edge) and not refused(calls['kv4'], edge)
+edge[0, first] = N
+assert f'block_table[0][{first}]' in refused(ext, edge) and f'block_table[0][{first}]' in refused(calls['kv4'], edge)
+plain = lambda t: B.paged_decode_attention_ext(q, k, v, t, new, out, 0.1)
+assert 'block_table' in refused(plain, t2)           # without a window every page is seen
+print('AS IT SHOULD')
+"""
+
+
+def test_a_debugging_run_checks_the_pages_that_a_call_touches():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", VALIDATED], cwd=root, env=dict(os.environ, PDA_DEBUG_VALIDATE="1"),
+                       capture_output=True, text=True, timeout=110)
+    assert r.returncode == 0 and "AS IT SHOULD" in r.stdout, r.stdout + r.stderr[-2000:]
