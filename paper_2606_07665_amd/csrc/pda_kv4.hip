@@ -169,6 +169,9 @@ struct Attn4 {
 };
 
 constexpr float kLazy = 8.f;  // see the online softmax
+// The largest scale of a value under which a probability of 2^kLazy leaves room
+// for the sum of a table's 2^30 tokens in fp32: 30 + 8 + log2(6) + 214 - 127 < 128.
+constexpr unsigned kLazyScale = 214;
 
 // One pass over the cache with the split, the columns and the partials of the
 // bf16 kernel (pda_kernels.hip): a wave takes 32-token steps of one kv head,
@@ -383,6 +386,7 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
 #pragma unroll
     for (int dt = 0; dt < S::kDT; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -__builtin_inff();
+    float seen = -__builtin_inff();  // the largest score of this lane's tokens, unscaled
     f32x4 l_acc = {0.f, 0.f, 0.f, 0.f};  // the column's sum of probabilities, in every row
 
     // first token of the wave's k-th step (clamped to its last)
@@ -540,12 +544,18 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
           for (int j = 0; j < 4; ++j)
             *reinterpret_cast<u32x4*>(row + 16 * j) = __builtin_bit_cast(u32x4, decode8(r.vw[i][j], unit));
         }
+        unsigned top = r.vs[0];
+#pragma unroll
+        for (int i = 1; i < S::kVLoads; ++i) top = max(top, r.vs[i]);
+        const bool large = top > kLazyScale;
         load_v(at, only, r);
         // Online softmax in log2 units, against a reference m_run of each column
         // that follows its maximum only when a score passes it by 2^kLazy: the
         // probabilities are then at most 2^kLazy, which costs fp32 and the hi +
         // lo pairs nothing, and most steps neither reduce a maximum across
-        // lanes nor rescale the accumulator.
+        // lanes nor rescale the accumulator.  Where the step has values so large
+        // that 2^kLazy of them could leave fp32 (`large`) the reference is the
+        // maximum itself, as in the bf16 kernel.
         if (edge) {
 #pragma unroll
           for (int T = 0; T < 2; ++T)
@@ -558,11 +568,11 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
         }
         const float mx0 = fmaxf(fmaxf(sacc[0][0], sacc[0][1]), fmaxf(sacc[0][2], sacc[0][3]));
         const float mx1 = fmaxf(fmaxf(sacc[1][0], sacc[1][1]), fmaxf(sacc[1][2], sacc[1][3]));
-        float mx = fmaxf(mx0, mx1);
-        if (__any(mx * p.scale > m_run + kLazy)) {  // (no key yet: m_run = -inf)
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
-          const float m_new = fmaxf(m_run, mx * p.scale);
+        seen = fmaxf(seen, fmaxf(mx0, mx1));
+        if (__any((seen * p.scale > m_run + kLazy) | large)) {  // (no key yet: m_run = -inf)
+          seen = fmaxf(seen, __shfl_xor(seen, 16));
+          seen = fmaxf(seen, __shfl_xor(seen, 32));
+          const float m_new = fmaxf(m_run, seen * p.scale);
           // (a column that has still seen no key keeps 0 in its place)
           const float alpha = m_run == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
           m_run = m_new;

@@ -237,3 +237,58 @@ def test_a_debugging_run_checks_the_pages_that_a_call_touches():
     r = subprocess.run([sys.executable, "-c", VALIDATED], cwd=root, env=dict(os.environ, PDA_DEBUG_VALIDATE="1"),
                        capture_output=True, text=True, timeout=110)
     assert r.returncode == 0 and "AS IT SHOULD" in r.stdout, r.stdout + r.stderr[-2000:]
+
+
+# ------------------------------------------------------------ the largest values
+# Scores are 0 but for a few tokens at 7.9 in log2 units, which a softmax whose reference lags by up to 8 takes
+# as probabilities of 2^7.9.  "one": such a token has values up to the format's largest, 1.5 * 2^127.  "after":
+# 128 tokens with a score of 0 have values up to 2^126.6, behind one such token of each wave: their sum stays in
+# fp32 relative to the largest probability, which holds only in waves that see both.
+@pytest.mark.parametrize("kind,min_steps", [("one", 0), ("one", 1 << 20), ("after", 1 << 20)])  # waves of a step or two, of many
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("d,hq,hkv,batch", [(128, 8, 2, 3), (64, 4, 4, 3), (256, 4, 1, 2), (128, 16, 8, 10)])
+def test_kv4_values_near_the_top_of_the_range(lib, d, hq, hkv, batch, kind, sign, min_steps):
+    rng = np.random.default_rng(d + batch)
+    n, page = 1500, 16
+    w = build([n] * batch, hq, hkv, d, page, seed=d, poison=False)
+    kc, ks, vc, vs = (t.copy() for t in quantised(w))
+    kc[:], ks[:], vc[:], vs[:] = 0, 127, 0, 100
+    w.q[:] = 0
+    w.q[..., 0] = 0x3F80  # 1.0: a score is element 0 of the key
+    scale = sign * 7.9 / 6 * np.log(2.0)
+
+    def slot(b, t):
+        return int(w.block_table[b, t // page]), t % page
+
+    for b in range(batch):
+        for t in ([700] if kind == "one" else [32 * s + 5 for s in range(4, 8)]):
+            at, s = slot(b, t)
+            kc[at, :, 0, s, 0] = 0x07 if sign > 0 else 0x0F  # 6 or -6
+        for t in ([700] if kind == "one" else range(256, 384)):
+            at, s = slot(b, t)
+            vs[at, :, :, s] = 252 if kind == "one" else 251
+            vc[at, :, :, s] = rng.integers(0, 256, vc[at, :, :, s].shape)
+    cache = (kc, ks, vc, vs)
+    lib.set_option(lib.OPT_MIN_STEPS, min_steps)
+    lib.set_option(lib.OPT_FIXED_SPLIT, int(min_steps == 0))
+    try:
+        log(f"large values D={d} {hq}:{hkv} B={batch} {kind} sign={sign} min_steps={min_steps}")
+        got = run_kv4(lib, w, cache, scale=scale)
+        w.k_cache, w.v_cache = (np.asarray(bits_of(C.kv4_tokens(*cache[2 * i:2 * i + 2]))) for i in range(2))
+        w.scale = scale
+        bf16 = run_sink(lib, w, 0, 0)
+    finally:
+        lib.set_option(lib.OPT_MIN_STEPS, 0)
+        lib.set_option(lib.OPT_FIXED_SPLIT, 1)
+    want = C.attend(w.q, C.kv4_tokens(kc, ks), C.kv4_tokens(vc, vs), w.block_table, w.context_lens, scale)
+    assert np.isfinite(bf16).all() and np.isfinite(got).all()
+    # (sums of large values of both signs: fp32's error relative to the largest, beside half a bf16 spacing)
+    most = np.abs(want).max()
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -15 * most).all()
+
+
+def bits_of(x):
+    """float64 values that bf16 holds exactly, as its bits."""
+    f = x.astype(np.float32)
+    assert np.array_equal(f.astype(np.float64), x)
+    return (f.view(np.uint32) >> 16).astype(np.uint16)
