@@ -138,6 +138,14 @@ __global__ __launch_bounds__(kKv4Threads) void kv4_read_kernel(Kv4Args a, uint16
 }
 
 // --------------------------------------------------------------- attention
+// Eight bf16 values times zero: a NaN where they are not finite.
+__device__ __forceinline__ u32x4 times_zero(u32x4 x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    x[i] = ((x[i] & 0x7F80u) == 0x7F80u ? 0x7FC0u : 0u) | ((x[i] & 0x7F800000u) == 0x7F800000u ? 0x7FC00000u : 0u);
+  return x;
+}
+
 typedef const __attribute__((address_space(1))) uint8_t global_u8;
 typedef const __attribute__((address_space(1))) u32x4 global_u32x4;
 
@@ -163,9 +171,10 @@ __host__ __device__ constexpr int pref_offset4(int waves) { return ml_offset4<D>
 struct Attn4 {
   int batch, hq, hkv, group, hgs, page_shift, num_pages, maxp, min_steps, nq, window, sinks, chunks, chunk_steps;
   float scale;  // in log2 units, > 0
-  // q as the products take it: its bits and `keep`, then exclusive or `flip`:
-  // the signs turned for a negative scale, zeros (and a scale of 1) for a zero
-  unsigned keep, flip;
+  // q as the products take it: its bits exclusive or `flip`, the signs turned for
+  // a negative scale; for a zero one (`zero`) times_zero of them, and a scale of 1
+  unsigned flip;
+  int zero;
 };
 
 constexpr float kLazy = 8.f;  // see the online softmax
@@ -492,8 +501,10 @@ __global__ __launch_bounds__(64 * kv4_max_waves(D), kv4_max_waves(D) / 4) void a
     // q as the B operand: column c, elements 8 j .. +7 of the lane's part of d
     bf16x8 qop[S::kQK];
 #pragma unroll
-    for (int i = 0; i < S::kQK; ++i)
-      qop[i] = __builtin_bit_cast(bf16x8, c < ncols ? (qraw[i] & p.keep) ^ p.flip : u32x4{0u, 0u, 0u, 0u});
+    for (int i = 0; i < S::kQK; ++i) {
+      const u32x4 x = p.zero ? times_zero(qraw[i]) : qraw[i] ^ p.flip;
+      qop[i] = __builtin_bit_cast(bf16x8, c < ncols ? x : u32x4{0u, 0u, 0u, 0u});
+    }
     {
       auto step = [&](int k, Set& r) {
         const int t = token_of(k);
@@ -726,7 +737,7 @@ hipError_t launch_attn4(const LaunchArgs& a, const Kv4Args& c, hipStream_t st) {
   p.chunk_steps = a.chunk_steps;
   const float s = a.scale * kLog2e;
   p.scale = s == 0.f ? 1.f : s < 0.f ? -s : s;
-  p.keep = s == 0.f ? 0u : ~0u;
+  p.zero = s == 0.f;
   p.flip = s < 0.f ? 0x80008000u : 0u;
   hipLaunchKernelGGL((attn4_kernel<D, kFixed>), dim3(a.grid), dim3(64 * a.waves), kv4_attn_lds_bytes(D, a.batch, a.waves),
                      st, a.q, c.k, c.ks, c.v, c.vs, a.bt, a.lens, a.out, a.ws_acc, a.ws_ml, a.ws_pref, p);

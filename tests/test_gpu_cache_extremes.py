@@ -6,6 +6,7 @@ import oracle
 from _cache import build, torch_any, torch_bf16
 from _gpu import check, log
 from oracle import cache as C
+from test_gpu_cache_limits import compare
 from test_gpu_kv4 import quantised
 from test_gpu_kv4 import run as run_kv4
 from test_gpu_sink import run as run_sink
@@ -292,3 +293,19 @@ def bits_of(x):
     f = x.astype(np.float32)
     assert np.array_equal(f.astype(np.float64), x)
     return (f.view(np.uint32) >> 16).astype(np.uint16)
+
+
+# -------------------------------------------------------- a scale of zero
+@pytest.mark.parametrize("scale", [0.0, -0.0])
+@pytest.mark.parametrize("d,hq,hkv,lens,tq", [(128, 32, 8, [700, 33, 0], 1), (64, 8, 4, [100, 5000], 3), (256, 12, 4, [3, 400], 2)])
+def test_kv4_queries_that_are_not_finite(lib, d, hq, hkv, lens, tq, scale):
+    w = build(lens, hq, hkv, d, 16, seed=d + tq, num_queries=tq)
+    cache = quantised(w)
+    rng = np.random.default_rng(d)
+    rows = [(b, j, int(h)) for b in range(len(lens)) for j in range(tq) for h in rng.choice(hq, 3, replace=False)]
+    for i, (b, j, h) in enumerate(rows):
+        w.q[b, j, h, (37 * i + 1) % d] = (0x7FC0, 0x7F80, 0xFF80, 0xFFC1)[i % 4]
+    with np.errstate(invalid="ignore"):
+        want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, scale)
+    log(f"queries not finite D={d} {hq}:{hkv} T={tq} scale={scale}")
+    compare(run_kv4(lib, w, cache, scale=scale), want, f"scale {scale}")
