@@ -217,11 +217,13 @@ int paged_decode_attention_ext(const void* q, const void* k_cache, const void* v
  * t < num_sinks.
  *   window        as for paged_decode_attention_ext; 0 (no window) makes every
  *                 key visible, whatever num_sinks is.
- *   num_sinks     >= 0; 0 is paged_decode_attention_ext.
+ *   num_sinks     >= 0; 0, or window 0 with one query, is
+ *                 paged_decode_attention_ext.
  * A page none of whose tokens any query of the sequence sees -- wholly past
  * the sinks and wholly before the window -- is never read and may have been
- * released (any block_table entry).  The calls run on the matrix cores with
- * the merge kernel, whatever PDA_OPT_COMPUTE_PATH and PDA_OPT_FUSED_MERGE say.
+ * released (any block_table entry).  The other calls run on the matrix cores
+ * with the merge kernel, whatever PDA_OPT_COMPUTE_PATH and PDA_OPT_FUSED_MERGE
+ * say.
  * An infinity or a NaN among a token's values reaches only the queries that see
  * the token (with num_sinks 0, as in paged_decode_attention_ext, it can reach
  * the other queries of its sequence as a NaN).

@@ -1062,7 +1062,9 @@ int attention_call(const void* q, const void* k_cache, const void* v_cache, cons
   if (num_queries < 1) return fail(PDA_ERR_SHAPE, "num_queries must be >= 1 (got %d)", num_queries);
   if (window < 0) return fail(PDA_ERR_SHAPE, "window must be >= 0 (got %d)", window);
   if (sinks < 0) return fail(PDA_ERR_SHAPE, "num_sinks must be >= 0 (got %d)", sinks);
-  if (window == 0) sinks = 0;  // every key is visible
+  // Every key is visible without a window; with several queries the kernel for sinks still is the one that keeps what
+  // is not finite from those that do not see it.
+  if (window == 0 && num_queries == 1) sinks = 0;
   // A window as long as the table hides nothing and no query sees more sinks than it holds; the kernels subtract a
   // window from positions that go down to 1 - num_queries, in 32 bits.
   const int32_t most_tokens = max_pages_per_seq * page_size;  // at most 2^30 (check_shape)

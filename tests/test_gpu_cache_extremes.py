@@ -6,7 +6,7 @@ import oracle
 from _cache import build, torch_any, torch_bf16
 from _gpu import check, log
 from oracle import cache as C
-from test_gpu_cache_limits import compare
+from test_gpu_cache_limits import compare, partly_seen
 from test_gpu_kv4 import quantised
 from test_gpu_kv4 import run as run_kv4
 from test_gpu_sink import run as run_sink
@@ -309,3 +309,30 @@ def test_kv4_queries_that_are_not_finite(lib, d, hq, hkv, lens, tq, scale):
         want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, scale)
     log(f"queries not finite D={d} {hq}:{hkv} T={tq} scale={scale}")
     compare(run_kv4(lib, w, cache, scale=scale), want, f"scale {scale}")
+
+
+# ------------------------------------------------------ sinks without a window
+@pytest.mark.parametrize("pick", [0, -1, None])
+@pytest.mark.parametrize("d,hq,hkv,page,lens,tq", [(128, 32, 8, 16, [300, 7, 2, 4000], 4), (64, 4, 2, 64, [129, 3], 8),
+                                                   (256, 12, 4, 4, [100, 33], 3), (128, 8, 8, 1, [70, 15], 16)])
+def test_bf16_values_reach_only_the_queries_that_see_them_without_a_window(lib, d, hq, hkv, page, lens, tq, pick):
+    w = build(lens, hq, hkv, d, page, seed=sum(lens), num_queries=tq)
+    for b, n in enumerate(lens):
+        part = partly_seen(n, tq, 0, 4)
+        for i, t in enumerate(part if pick is None else part[pick:][:1]):
+            row = w.v_cache[int(w.block_table[b, t // page]), t % page]
+            row[:, (7 * b + 11 * i + np.arange(hkv)) % d] = (0x7FC0, 0x7F80, 0xFF80)[(b + i) % 3]
+    want = C.attend(w.q, oracle.bf16_to_f64(w.k_cache), oracle.bf16_to_f64(w.v_cache), w.block_table, w.context_lens, w.scale)
+    log(f"bf16 partly seen, no window D={d} {hq}:{hkv} lens={lens} {pick}")
+    compare(run_sink(lib, w, 0, 4), want, "sink")
+
+
+@pytest.mark.parametrize("option", ["OPT_COMPUTE_PATH", "OPT_FUSED_MERGE"])
+def test_options_leave_sinks_without_a_window_alone(lib, option):
+    w = build([33, 700, 3000], 32, 8, 128, 16, seed=22, num_queries=2)
+    want = run_sink(lib, w, 0, 4)
+    lib.set_option(getattr(lib, option), 1)
+    try:
+        assert np.array_equal(run_sink(lib, w, 0, 4), want)
+    finally:
+        lib.set_option(getattr(lib, option), 0)
