@@ -290,6 +290,14 @@ def _stream_ptr(stream, device=None):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _i32(name, x):
+    """x as the C calls take it (ctypes would cut it to its low 32 bits)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must be a 32-bit integer, got {x}")
+    return x
+
+
 @functools.lru_cache(maxsize=None)
 def _parsed_dims(dims):
     """dims string -> tuple of (kind, value): 0 any, 1 number, 2 symbol."""
@@ -486,7 +494,7 @@ def paged_decode_attention_ext(q, k_cache, v_cache, block_table, context_lens, o
                     ("out", out, torch.bfloat16, "B T Hq D")])
     _check(load().paged_decode_attention_ext(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
-        out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"], sz["N"], sz["M"], sz["T"], int(window),
+        out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"], sz["N"], sz["M"], sz["T"], _i32("window", window),
         ctypes.c_float(float(scale)), _stream_ptr(stream)))
     return out
 
@@ -507,8 +515,8 @@ def paged_decode_attention_sink(q, k_cache, v_cache, block_table, context_lens, 
                     ("out", out, torch.bfloat16, "B T Hq D")])
     _check(load().paged_decode_attention_sink(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
-        out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"], sz["N"], sz["M"], sz["T"], int(window), int(sinks),
-        ctypes.c_float(float(scale)), _stream_ptr(stream)))
+        out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"], sz["N"], sz["M"], sz["T"], _i32("window", window),
+        _i32("sinks", sinks), ctypes.c_float(float(scale)), _stream_ptr(stream)))
     return out
 
 
@@ -581,7 +589,8 @@ def paged_decode_attention_kv4(q, k_codes, k_scales, v_codes, v_scales, block_ta
     _kv4_groups(sz)
     _check(load().paged_decode_attention_kv4(
         q.data_ptr(), *(t.data_ptr() for t in cache), out.data_ptr(), sz["B"], sz["Hq"], sz["Hkv"], sz["D"], sz["P"],
-        sz["N"], sz["M"], sz["T"], int(window), int(sinks), ctypes.c_float(float(scale)), _stream_ptr(stream)))
+        sz["N"], sz["M"], sz["T"], _i32("window", window), _i32("sinks", sinks), ctypes.c_float(float(scale)),
+        _stream_ptr(stream)))
     return out
 
 
@@ -613,8 +622,8 @@ def pages_update(block_table, context_lens, parents, new_lens, refcount, table_o
     _check(load().pda_pages_update(
         block_table.data_ptr(), context_lens.data_ptr(), _ptr(parents), new_lens.data_ptr(), refcount.data_ptr(),
         table_out.data_ptr(), refcount_out.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), info.data_ptr(), sz["B"],
-        sz["R"], int(page_size), sz["N"], sz["M"], int(num_queries), int(window), int(sinks),
-        _stream_ptr(stream)))
+        sz["R"], _i32("page_size", page_size), sz["N"], sz["M"], _i32("num_queries", num_queries), _i32("window", window),
+        _i32("sinks", sinks), _stream_ptr(stream)))
 
 
 def pages_compact(block_table, context_lens, refcount, table_out, refcount_out, page_map, copy_src, copy_dst, info, page_size,
@@ -635,8 +644,8 @@ def pages_compact(block_table, context_lens, refcount, table_out, refcount_out, 
                     ("copy_src", copy_src, i32, "N"), ("copy_dst", copy_dst, i32, "N"), ("info", info, i32, "2")])
     _check(load().pda_pages_compact(
         block_table.data_ptr(), context_lens.data_ptr(), refcount.data_ptr(), table_out.data_ptr(), refcount_out.data_ptr(),
-        page_map.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), info.data_ptr(), sz["B"], int(page_size), sz["N"],
-        sz["M"], _stream_ptr(stream)))
+        page_map.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), info.data_ptr(), sz["B"], _i32("page_size", page_size),
+        sz["N"], sz["M"], _stream_ptr(stream)))
 
 
 def pages_copy(pools, copy_src, copy_dst, count=None, stream=None):

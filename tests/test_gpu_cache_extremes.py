@@ -336,3 +336,33 @@ def test_options_leave_sinks_without_a_window_alone(lib, option):
         assert np.array_equal(run_sink(lib, w, 0, 4), want)
     finally:
         lib.set_option(getattr(lib, option), 0)
+
+
+# ----------------------------------------------- numbers past 32 bits
+@pytest.mark.parametrize("big", [2 ** 31, 2 ** 32 + 16, -2 ** 32 + 16, 2 ** 64])
+def test_numbers_past_32_bits_are_refused(lib, big):
+    import torch
+    w = build([100, 700], 8, 2, 128, 16, seed=1, poison=False)
+    q, k, v = torch_bf16(w.q), torch_bf16(w.k_cache), torch_bf16(w.v_cache)
+    table, lens, cache = torch_any(w.block_table), torch_any(w.context_lens), [torch_any(t) for t in quantised(w)]
+    out = torch.zeros_like(q)
+    for kw in (dict(window=big), dict(window=5, sinks=big)):
+        name = "sinks" if "sinks" in kw else "window"
+        with pytest.raises(ValueError, match=name):
+            lib.paged_decode_attention_kv4(q, *cache, table, lens, out, 0.1, **kw)
+        with pytest.raises(ValueError, match=name):
+            lib.paged_decode_attention_sink(q, k, v, table, lens, out, 0.1, **kw)
+    with pytest.raises(ValueError, match="window"):
+        lib.paged_decode_attention_ext(q, k, v, table, lens, out, 0.1, window=big)
+    n, dev = w.k_cache.shape[0], dict(dtype=torch.int32, device="cuda")
+    ref = torch.ones(n, **dev)
+    outs = [torch.full(s, 77, **dev) for s in (tuple(table.shape), (n,), (2,), (2,), (2,))]
+    for kw in (dict(page_size=big), dict(page_size=16, window=big), dict(page_size=16, window=9, sinks=big),
+               dict(page_size=16, num_queries=big)):
+        with pytest.raises(ValueError, match="32-bit"):
+            lib.pages_update(table, lens, None, lens, ref, *outs, **kw)
+    outs = [torch.full(s, 77, **dev) for s in (tuple(table.shape), (n,), (n,), (n,), (n,), (2,))]
+    with pytest.raises(ValueError, match="32-bit"):
+        lib.pages_compact(table, lens, ref, *outs, page_size=big)
+    torch.cuda.synchronize()
+    assert (out == 0).all() and all((o == 77).all() for o in outs)
