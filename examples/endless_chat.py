@@ -116,6 +116,9 @@ class Pages:
 def run(cache="kv4", conversations=4, prompt=300, forks=3, steps=400, window=256, sinks=4, page=16, layers=2, seed=0,
         log=print):
     """The loop above; returns the last step's tensors and what compaction left unchanged."""
+    for name, n in (("conversations", conversations), ("prompt", prompt), ("forks", forks), ("steps", steps), ("layers", layers)):
+        if n < 1:
+            raise ValueError(f"{name} must be at least 1, got {n}")
     pda.load()
     gen = torch.Generator(device="cuda").manual_seed(seed)
     rows = conversations * forks
