@@ -366,3 +366,34 @@ def test_numbers_past_32_bits_are_refused(lib, big):
         lib.pages_compact(table, lens, ref, *outs, page_size=big)
     torch.cuda.synchronize()
     assert (out == 0).all() and all((o == 77).all() for o in outs)
+
+
+# ---------------------------------------- each side of the 4-bit call's forms
+# (head_dim, Hq, Hkv, batch): three, or at head size 256 two, workgroups of 4 waves a CU up to the first batch of
+# each pair, one of 12 (8) waves from the second on; then 12 and 8 waves, 8 and 4
+@pytest.mark.parametrize("d,hq,hkv,batch", [(128, 4, 4, 2154), (128, 4, 4, 2155), (64, 4, 2, 4202), (64, 4, 2, 4203),
+                                            (256, 2, 1, 1471), (256, 2, 1, 1472), (128, 4, 2, 6463), (128, 4, 2, 6464),
+                                            (256, 2, 2, 2943), (256, 2, 2, 2944)])
+def test_kv4_on_each_side_of_its_workgroups(lib, d, hq, hkv, batch):
+    rng = np.random.default_rng(batch)
+    lens = rng.integers(0, 6, batch)
+    lens[batch // 2] = 1500
+    w = build(lens.tolist(), hq, hkv, d, 16, seed=batch)
+    cache = quantised(w)
+    want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, w.scale)
+    log(f"kv4 workgroups D={d} {hq}:{hkv} B={batch}")
+    check(run_kv4(lib, w, cache), want, "workgroups")
+
+
+# (Hq, Hkv, query tokens): 8 and 9, 10 columns: up to four kv heads a workgroup, up to two
+@pytest.mark.parametrize("hq,hkv,tq", [(32, 8, 2), (24, 8, 3), (40, 8, 2), (16, 4, 2), (12, 4, 3)])
+@pytest.mark.parametrize("longest", [4000, 9000])
+def test_kv4_on_each_side_of_eight_columns(lib, hq, hkv, tq, longest):
+    rng = np.random.default_rng(hq + tq)
+    lens = rng.integers(0, 100, 64)
+    lens[20] = longest
+    w = build(lens.tolist(), hq, hkv, 128, 16, seed=hq + tq, num_queries=tq)
+    cache = quantised(w)
+    want = C.attend(w.q, C.kv4_tokens(*cache[:2]), C.kv4_tokens(*cache[2:]), w.block_table, w.context_lens, w.scale)
+    log(f"kv4 columns {hq}:{hkv} T={tq} longest={longest}")
+    check(run_kv4(lib, w, cache), want, "columns")
