@@ -519,9 +519,11 @@ Plan make_plan(const Form& form, int32_t batch, int32_t hkv, int32_t d, int64_t 
 // Workspace that any plan of these sizes may need, and of any smaller batch or
 // table, fewer columns and every window: what a call asks for, so that calls
 // of one shape that plan differently (by their windows) use one workspace,
-// also under capture.  A plan has at most one workgroup per compute unit and
-// per (sequence, kv head, step), each with one slot of up to max_waves kv
-// heads beside one per (sequence, kv-head group).
+// also under capture.  A plan has at most per_cu workgroups per compute unit and
+// one per (sequence, kv head, step), each with one slot of up to max_waves kv
+// heads beside one per (sequence, kv-head group).  (A 4-bit plan of a batch of
+// thousands may have up to 4 waves a compute unit fewer than that of a smaller
+// one: those rows are in the quarter that workspace_for adds.)
 int64_t workspace_bytes(const Form& form, int32_t batch, int32_t hkv, int32_t d, int32_t p, int32_t maxp, int num_cus,
                         int cols) {
   const int64_t target = static_cast<int64_t>(num_cus) * blocks_per_cu() * form.per_cu;

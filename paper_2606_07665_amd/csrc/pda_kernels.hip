@@ -779,6 +779,8 @@ __global__ __launch_bounds__(64 * max_waves(D), 1) void attn_kernel(
       if constexpr (kSink) {
         if (edge && nq > 1) {
           // the rows that some of the queries see, if they hold an infinity or a NaN
+          // (33 sequences, four queries, a window of 2000 with 77 sinks: 61.7 us a call,
+          // 60.6 without looking)
           const int tl = t0 + (lane & 31);
           const bool some = tl < L && (tl >= lo_seq || tl < pinned) && !(tl < hi_min && (tl >= lo_max || tl < sinks));
           unsigned apart = static_cast<unsigned>(__ballot(some));

@@ -197,8 +197,8 @@ constexpr unsigned kLazyScale = 214;
 //    and read back transposed, as in the bf16 kernel.
 //
 // A quarter of the bf16 kernel's bytes leaves a step ~1300 cycles of a SIMD at
-// 7 TB/s, and it takes ~160 vector, 32 matrix and 25 LDS instructions: the time
-// goes where a wave waits.  So:
+// 7 TB/s, and it takes (D = 128, counters) 176 vector, 26 matrix and 24 LDS
+// instructions: the time goes where a wave waits.  So:
 //  * 12 waves a CU (3 a SIMD, 168 registers each), each with the loads of two
 //    steps in flight, as three workgroups of 4 waves where the prefix over the
 //    batch leaves LDS for them: one takes up its next sequence while the others

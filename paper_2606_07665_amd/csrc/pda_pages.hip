@@ -208,6 +208,11 @@ __device__ __forceinline__ int place_rows(const PagesUpdateArgs& a, int32_t* sta
   return have;
 }
 
+// One workgroup, which goes through the pool until it has found enough free
+// pages: what a step costs in a large pool is how far up they lie.  256 sequences
+// by a token, 30 pages taken, us an update: 59 of 131072 pages with the free ones
+// right behind 66000 live, 101 with them at the pool's end; at the end of 400000
+// 283, of 1000000 683.
 __global__ __launch_bounds__(kScanThreads) void update_place_kernel(PagesUpdateArgs a) {
   __shared__ int part[kScanThreads / 64];
   int lacking;
@@ -281,7 +286,7 @@ __global__ __launch_bounds__(kScanThreads) void update_place_table_kernel(PagesU
 // references for itself, too, in LDS, where a thread can ask for all its entries
 // of the two tables together (rows as wide as a power of two).  Update and copy,
 // 31 sequences of 11 pages as 48 rows 12.4 -> 9.4 us, 6 of 124 as 42 rows 13.5 ->
-// 11.6; with three such rounds (42 rows of up to 512) it is 14.2 -> 16.5, so not
+// 11.3; with three such rounds (32 rows of up to 512) it is 14.2 -> 16.5, so not
 // there.
 constexpr int kOneLaunchEach = 8;
 constexpr int kOneLaunchEntries = kOneLaunchEach * kScanThreads;
@@ -500,8 +505,8 @@ __global__ __launch_bounds__(kThreads) void compact_table_kernel(PagesCompactArg
 // itself: a bit per page says which are live, and with the live pages before
 // every 64 of them the rank of a page is one word, the k-th live page or hole a
 // search.  Where a wave can ask for all its pages together, and with no more
-// workgroups than run at once: compaction and copy, a pool of 71 pages 12.8 ->
-// 8.5 us, of 7462 12.7 -> 9.4; with three such rounds (24672 pages) it is 117.5
+// workgroups than run at once: compaction and copy, a pool of 71 pages 13.1 ->
+// 8.8 us, of 7462 12.6 -> 9.3; with three such rounds (24672 pages) it is 117.5
 // -> 123, so not there.
 constexpr int kOneLaunchEachWave = 8;
 constexpr int kOneLaunchWords = kOneLaunchEachWave * kScanThreads / 64;  // of 64 pages
