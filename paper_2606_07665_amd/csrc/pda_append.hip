@@ -46,16 +46,17 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(
   L = L < 0 ? 0 : (L > max_ctx ? max_ctx : L);
   const int t = L - tokens + j;                     // this token's position
   if (t < 0) return;
+  // The values are asked for together with the page id, and their place is worked
+  // out before the branch on it: neither waits behind it.
   const unsigned raw = static_cast<unsigned>(bt[static_cast<int64_t>(b) * maxp + (t >> page_shift)]);
-  if (raw >= static_cast<unsigned>(num_pages)) return;
+  const int64_t src = (bj * hkv + g) * D + 8 * chunk;
+  u32x4 x = *reinterpret_cast<const u32x4*>((which ? v_new : k_new) + src);
   const int64_t page = raw;
   const int slot = t & ((1 << page_shift) - 1);
-
-  const int64_t dst = (((page << page_shift) + slot) * hkv + g) * D + 8 * chunk;
-  const int64_t src = (bj * hkv + g) * D + 8 * chunk;
-  const uint16_t* from = which ? v_new : k_new;
-  uint16_t* to = which ? vc : kc;
-  *reinterpret_cast<u32x4*>(to + dst) = *reinterpret_cast<const u32x4*>(from + src);
+  int64_t dst = (((page << page_shift) + slot) * hkv + g) * D + 8 * chunk;
+  asm volatile("" : "+v"(dst), "+v"(x) : "s"(kc), "s"(vc));
+  if (raw >= static_cast<unsigned>(num_pages)) return;
+  *reinterpret_cast<u32x4*>((which ? vc : kc) + dst) = x;
 }
 
 }  // namespace

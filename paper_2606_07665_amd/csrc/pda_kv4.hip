@@ -53,7 +53,7 @@ struct Kv4Lane {
   int t;          // position in the sequence
   int j;          // token of the call
   int g, grp;     // kv head, group
-  int64_t chunk;  // index of the group's 16 bytes of codes, and of its scale; -1: its token has no page
+  unsigned page;  // its token's page; one outside the pool: none
   bool in;        // the call has this token
 };
 
@@ -75,16 +75,22 @@ __device__ __forceinline__ Kv4Lane kv4_lane(const Kv4Args& a) {
   p.in = p.j >= 0 && p.j < a.tokens;
   p.g = hp / kPairs;
   p.grp = (hp % kPairs) * 2 + ((threadIdx.x & 7) >> 2);
-  p.chunk = -1;
-  if (p.in && p.t >= 0) {
-    // an entry outside the pool (a page that was lacking, or was released) is no
-    // page: clamped into the pool it would be another sequence's
-    const unsigned raw = static_cast<unsigned>(a.bt[static_cast<int64_t>(b) * a.maxp + (p.t >> a.page_shift)]);
-    const int64_t page = raw;
-    if (raw < static_cast<unsigned>(a.num_pages))
-      p.chunk = (((page * a.hkv + p.g) * kGroups + p.grp) << a.page_shift) + (p.t & ((1 << a.page_shift) - 1));
-  }
+  p.page = ~0u;
+  if (p.in && p.t >= 0) p.page = static_cast<unsigned>(a.bt[static_cast<int64_t>(b) * a.maxp + (p.t >> a.page_shift)]);
   return p;
+}
+
+// Whether there is a page: an entry outside the pool (a page that was lacking, or
+// was released) is none; clamped into the pool it would be another sequence's.
+__device__ __forceinline__ bool kv4_paged(const Kv4Args& a, const Kv4Lane& p) {
+  return p.page < static_cast<unsigned>(a.num_pages);
+}
+
+// Index of the group's 16 bytes of codes, and of its scale.
+template <int D>
+__device__ __forceinline__ int64_t kv4_chunk(const Kv4Args& a, const Kv4Lane& p) {
+  const int64_t group = (static_cast<int64_t>(p.page) * a.hkv + p.g) * (D / kKv4Group) + p.grp;
+  return (group << a.page_shift) + (p.t & ((1 << a.page_shift) - 1));
 }
 
 // The bf16 row of a lane: element index of its 8 elements.
@@ -98,9 +104,13 @@ __global__ __launch_bounds__(kKv4Threads) void kv4_append_kernel(Kv4Args a, cons
                                                                  const uint16_t* __restrict__ v_new) {
   const Kv4Lane p = kv4_lane<D, kTile>(a);
   // (a run past the last token, a lane before the first, or no page: the four
-  // lanes of the exchange below stay together, as they are of one token)
-  if (p.chunk < 0) return;
-  const u32x4 x = ld16((blockIdx.z ? v_new : k_new) + kv4_row<D>(a, p));
+  // lanes of the exchange below stay together, as they are of one token; the
+  // values are asked for together with the page id, not behind the branch on it)
+  if (!p.in || p.t < 0) return;
+  u32x4 x = ld16((blockIdx.z ? v_new : k_new) + kv4_row<D>(a, p));
+  asm volatile("" : "+v"(x) : "s"(a.k), "s"(a.ks), "s"(a.v), "s"(a.vs));
+  if (!kv4_paged(a, p)) return;
+  const int64_t chunk = kv4_chunk<D>(a, p);
   // the group's largest biased exponent: of 8 elements in the lane, then of
   // its 4 lanes
   unsigned e = 0;
@@ -120,8 +130,8 @@ __global__ __launch_bounds__(kKv4Threads) void kv4_append_kernel(Kv4Args a, cons
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x2), unit, 2);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x3), unit, 3);
   if (s == 255) w = 0;
-  reinterpret_cast<unsigned*>((blockIdx.z ? a.v : a.k) + 16 * p.chunk)[threadIdx.x & 3] = w;
-  if ((threadIdx.x & 3) == 0) (blockIdx.z ? a.vs : a.ks)[p.chunk] = static_cast<uint8_t>(s);
+  reinterpret_cast<unsigned*>((blockIdx.z ? a.v : a.k) + 16 * chunk)[threadIdx.x & 3] = w;
+  if ((threadIdx.x & 3) == 0) (blockIdx.z ? a.vs : a.ks)[chunk] = static_cast<uint8_t>(s);
 }
 
 template <int D, int kTile>
@@ -130,9 +140,10 @@ __global__ __launch_bounds__(kKv4Threads) void kv4_read_kernel(Kv4Args a, uint16
   const Kv4Lane p = kv4_lane<D, kTile>(a);
   if (!p.in) return;
   bf16x8 y = {};
-  if (p.chunk >= 0) {
-    const unsigned w = reinterpret_cast<const unsigned*>((blockIdx.z ? a.v : a.k) + 16 * p.chunk)[threadIdx.x & 3];
-    y = decode8(w, scale_of((blockIdx.z ? a.vs : a.ks)[p.chunk]));
+  if (kv4_paged(a, p)) {
+    const int64_t chunk = kv4_chunk<D>(a, p);
+    const unsigned w = reinterpret_cast<const unsigned*>((blockIdx.z ? a.v : a.k) + 16 * chunk)[threadIdx.x & 3];
+    y = decode8(w, scale_of((blockIdx.z ? a.vs : a.ks)[chunk]));
   }
   *reinterpret_cast<u32x4*>((blockIdx.z ? v_out : k_out) + kv4_row<D>(a, p)) = __builtin_bit_cast(u32x4, y);
 }
