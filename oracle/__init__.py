@@ -255,7 +255,8 @@ def kv_append(k_cache, v_cache, k_new, v_new, block_table, context_lens):
 
     With several new tokens per sequence (``k_new``: [B, T, Hkv, D]), the
     lengths count all of them and token j lands at position L_b - T + j;
-    positions below 0 (L_b < T) write nothing.
+    positions below 0 (L_b < T) write nothing, and neither do tokens whose
+    page is not one of the pool.
     Returns new (k_cache, v_cache) arrays; the inputs are not modified.
     """
     k = np.array(k_cache, copy=True)
@@ -273,6 +274,8 @@ def kv_append(k_cache, v_cache, k_new, v_new, block_table, context_lens):
             if t < 0:
                 continue
             page = int(block_table[b][t // page_size])
+            if not 0 <= page < len(k):
+                continue
             k[page, t % page_size] = kn[b, j]
             v[page, t % page_size] = vn[b, j]
     return k, v

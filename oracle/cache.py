@@ -79,7 +79,7 @@ def kv4_tokens(codes, scales):
 
 def kv4_append(codes, scales, new, block_table, context_lens):
     """Copies of one pool's codes and scales with new bf16 rows [B, T, Hkv, D]
-    at positions L_b - T + j."""
+    at positions L_b - T + j; a token without a page in the pool goes nowhere."""
     codes, scales = codes.copy(), scales.copy()
     page = codes.shape[3]
     c, s = kv4_quantise(new)
@@ -88,19 +88,22 @@ def kv4_append(codes, scales, new, block_table, context_lens):
             t = int(context_lens[b]) - new.shape[1] + j
             if t >= 0:
                 n = int(block_table[b][t // page])
+                if not 0 <= n < len(codes):
+                    continue
                 codes[n, :, :, t % page] = c[b, j]
                 scales[n, :, :, t % page] = s[b, j]
     return codes, scales
 
 
 def kv4_read(codes, scales, tokens, block_table, context_lens):
-    """The last ``tokens`` tokens of each sequence, float64 [B, T, Hkv, D]; zeros before the first."""
+    """The last ``tokens`` tokens of each sequence, float64 [B, T, Hkv, D];
+    zeros before the first, and where there is no page in the pool."""
     x = kv4_tokens(codes, scales)
     out = np.zeros((len(context_lens), tokens, *x.shape[2:]))
     for b, n in enumerate(context_lens):
         for j in range(tokens):
             t = int(n) - tokens + j
-            if t >= 0:
+            if t >= 0 and 0 <= block_table[b][t // x.shape[1]] < len(x):
                 out[b, j] = x[int(block_table[b][t // x.shape[1]]), t % x.shape[1]]
     return out
 
