@@ -751,9 +751,149 @@ int pda_o_proj_residual_norm(const void* attn, const void* w_packed, const void*
 int pda_o_proj_workspace_reserve(int32_t batch, int32_t in_features, int32_t hidden, void* stream);
 
 /*
- * pda_prelude_plan, pda_o_proj_plan [library interface] -- host-only dry runs
- * of the planner of the projection y = x W^T in a prelude (qk_norm: with norm
- * weights) and in an output projection, as pda_plan for attention.  No HIP
+ * ---------------------------------------------------------------------------
+ * The feed-forward half of a decode layer [library interface]: what follows
+ * pda_o_proj_residual_norm up to the next layer's prelude.  Weights are packed
+ * by pda_pack_weights; every call is asynchronous on `stream`.
+ *
+ * pda_linear -- a product with its epilogue:
+ *   y = act(x W^T + bias) + residual, or gated
+ *   y = act(x Wg^T + bias_g) * (x Wu^T + bias_u) + residual
+ *   x         bf16 [batch, in_features], 16-byte aligned.
+ *   w_packed  packed bf16 [out_features, in_features], 16-byte aligned; gated
+ *             [2 out_features, in_features], the rows of Wg, then those of Wu.
+ *   bias      bf16, one a row of W, or NULL.
+ *   residual  bf16 [batch, out_features] or NULL.
+ *   out       bf16 [batch, out_features], or fp32 with out_f32 (a router's
+ *             logits); in bf16 it may be residual itself, otherwise it lies
+ *             apart from everything that is read.
+ * Sums and the epilogue are fp32; y is rounded once.  Uses the (device,
+ * stream) workspace where the product is split along in_features
+ * (pda_linear_workspace_reserve before graph capture).
+ *
+ * Activations: none, silu(x) = x / (1 + exp(-x)), gelu(x) = x (1 + erf(x /
+ * sqrt 2)) / 2, its tanh form, and max(x, 0).
+ */
+typedef enum {
+  PDA_ACT_NONE = 0,
+  PDA_ACT_SILU = 1,
+  PDA_ACT_GELU = 2,
+  PDA_ACT_GELU_TANH = 3,
+  PDA_ACT_RELU = 4
+} pda_activation;
+typedef struct {
+  int32_t batch;         /* rows of x, 0 .. 256                                    */
+  int32_t in_features;   /* a positive multiple of 32, at most 65536               */
+  int32_t out_features;  /* a positive multiple of 16, at most 262144; gated, at
+                            most 1000000000 / in_features                          */
+  int32_t activation;    /* pda_activation                                         */
+  int32_t gated;         /* 0 or 1                                                 */
+  int32_t out_f32;       /* 0 or 1                                                 */
+} pda_linear_dims;
+int pda_linear(const void* x, const void* w_packed, const void* bias, const void* residual, void* out,
+               const pda_linear_dims* dims, void* stream);
+/* Grow the (current device, stream) workspace for a product of these dims, and
+   of every smaller batch. */
+int pda_linear_workspace_reserve(const pda_linear_dims* dims, void* stream);
+
+/*
+ * pda_moe_route -- each token's experts, from the router's logits l:
+ *   s_e = softmax(l)_e or, with sigmoid, 1 / (1 + exp(-l_e));
+ *   the top_k experts by s_e + select_bias_e, the best first, of equal ones the
+ *   lowest; weight = s_e, divided by the sum of the chosen ones' with
+ *   renormalise, times scale.
+ *   logits         fp32 [tokens, num_experts], rows logit_stride elements apart
+ *                  (a router product padded to a multiple of 16 rows is read in
+ *                  place).
+ *   select_bias    fp32 [num_experts], finite, or NULL: it decides who is chosen
+ *                  and is no part of the weight.
+ *   expert_ids     int32 [tokens, top_k]; expert_weights fp32 [tokens, top_k].
+ * A logit of -infinity or NaN is an expert that may not be chosen: it comes last,
+ * with weight 0 (all weights are 0 where every logit is); +infinity counts as
+ * the largest finite number.  Without a bias the order is that of the logits,
+ * with one that of the sums in fp64.  No workspace.
+ */
+typedef struct {
+  int32_t tokens;        /* 0 .. 1048576                                           */
+  int32_t num_experts;   /* 1 .. 1024                                              */
+  int32_t top_k;         /* 1 .. 16, at most num_experts                           */
+  int32_t logit_stride;  /* at least num_experts                                   */
+  int32_t sigmoid;       /* 0: softmax, 1: sigmoid                                 */
+  int32_t renormalise;   /* 0 or 1                                                 */
+  float scale;           /* of the weights, finite                                 */
+} pda_route_dims;
+int pda_moe_route(const float* logits, const float* select_bias, int32_t* expert_ids, float* expert_weights,
+                  const pda_route_dims* dims, void* stream);
+
+/*
+ * pda_moe_experts -- the experts' gated products for a few tokens:
+ *   out_t = residual_t + sum_j w_tj D_e (act(G_e x_t) * (U_e x_t)),  e = expert_ids[t, j]
+ *   x               bf16 [tokens, hidden], 16-byte aligned.
+ *   expert_ids      int32 [tokens, top_k] on the device; an id outside
+ *                   [0, num_experts) adds nothing (an idle slot, an expert of
+ *                   another GPU), one that comes twice counts twice.
+ *   expert_weights  fp32 [tokens, top_k].
+ *   w_gate_up       packed bf16 [num_experts * 2 inter, hidden]: each expert's
+ *                   rows of G, then those of U; 16-byte aligned.
+ *   w_down          packed bf16 [num_experts * hidden, inter]: each expert's D;
+ *                   16-byte aligned.
+ *   residual        bf16 [tokens, hidden] or NULL.
+ *   out             bf16 [tokens, hidden]; may be residual or x itself, otherwise
+ *                   it lies apart from everything that is read.
+ * Sums are fp32; act(G x) * (U x) is rounded to bf16 between the two products
+ * (the matrix cores' operand) and out once.  Only the experts that are asked for are
+ * read.  What is not finite in a token reaches that token alone.  Uses the
+ * (device, stream) workspace, tokens * top_k * (2 inter + 4 hidden) bytes
+ * (pda_moe_workspace_reserve before graph capture).
+ */
+typedef struct {
+  int32_t tokens;        /* 0 .. 256                                               */
+  int32_t hidden;        /* a positive multiple of 32, at most 32768               */
+  int32_t inter;         /* rows of G and of U: a positive multiple of 32, at most
+                            65536                                                  */
+  int32_t num_experts;   /* 1 .. 1024; num_experts * 2 inter and num_experts *
+                            hidden below 2^31                                      */
+  int32_t top_k;         /* 1 .. 16                                                */
+  int32_t activation;    /* pda_activation                                         */
+} pda_moe_dims;
+int pda_moe_experts(const void* x, const int32_t* expert_ids, const float* expert_weights, const void* w_gate_up,
+                    const void* w_down, const void* residual, void* out, const pda_moe_dims* dims, void* stream);
+/* Grow the (current device, stream) workspace for a call of these dims, and of
+   every smaller number of tokens and top_k. */
+int pda_moe_workspace_reserve(const pda_moe_dims* dims, void* stream);
+
+/*
+ * pda_block_norm -- the norms around a block's output y, with its gate and
+ * scale:
+ *   u = y / sqrt(mean(y^2) + eps) * (post_w + weight_offset), or y without post_w
+ *   z = residual + scale * gate * u              (the new residual stream)
+ *   h = z / sqrt(mean(z^2) + eps) * (pre_w + weight_offset)
+ *   y         bf16 [rows, hidden].
+ *   residual  bf16 [rows, hidden] or NULL (0).
+ *   post_w, pre_w  bf16 [hidden] or NULL; without pre_w, normed_out is NULL.
+ *   gate      bf16 [hidden], or [rows, hidden] with gate_rows, or NULL (1).
+ *   residual_out  bf16 [rows, hidden]: z rounded once; normed_out bf16
+ *             [rows, hidden]: h, from the unrounded z.  Each may be y or
+ *             residual itself (not both the same one); otherwise they lie
+ *             apart from each other and from everything that is read.
+ * No workspace.
+ */
+typedef struct {
+  int32_t rows;          /* 0 .. 16777216                                          */
+  int32_t hidden;        /* a positive multiple of 8, at most 32768                */
+  int32_t gate_rows;     /* 0 or 1                                                 */
+  float scale;           /* finite                                                 */
+  float weight_offset;   /* finite; 1 for weights kept as their difference from 1  */
+  float eps;             /* finite and >= 0                                        */
+} pda_block_norm_dims;
+int pda_block_norm(const void* y, const void* residual, const void* post_w, const void* pre_w, const void* gate,
+                   void* residual_out, void* normed_out, const pda_block_norm_dims* dims, void* stream);
+
+/*
+ * pda_prelude_plan, pda_o_proj_plan, pda_linear_plan [library interface] --
+ * host-only dry runs of the planner of the projection y = x W^T in a prelude
+ * (qk_norm: with norm weights), in an output projection and in a product with
+ * its epilogue, as pda_plan for attention.  No HIP
  * call.  (A prelude whose outputs lie over x or the weights runs unfused,
  * whatever the plan says.)  Errors as for the calls' arguments; batch 0 gives
  * all zeros.
@@ -763,7 +903,8 @@ typedef struct {
   int32_t wide;                 /* 1: 32 x 32 x 16 matrix instructions             */
   int32_t col_groups;           /* workgroups that share the same rows             */
   int32_t k_splits;             /* parts of the k range                            */
-  int32_t fused;                /* 1: the prelude's epilogue runs in the kernel    */
+  int32_t fused;                /* 1: the prelude's or the product's epilogue runs
+                                   in the kernel                                   */
   int32_t workgroups;           /* with work                                       */
   int32_t ss_parts;             /* o_proj, unsplit: sums of z^2 per 16 features    */
   int64_t workspace_bytes;      /* that the call asks for: enough for every smaller
@@ -771,6 +912,7 @@ typedef struct {
 } pda_projection;
 int pda_prelude_plan(const pda_prelude_dims* dims, int32_t qk_norm, int32_t num_cus, pda_projection* out);
 int pda_o_proj_plan(int32_t batch, int32_t in_features, int32_t hidden, int32_t num_cus, pda_projection* out);
+int pda_linear_plan(const pda_linear_dims* dims, int32_t num_cus, pda_projection* out);
 
 #ifdef __cplusplus
 }

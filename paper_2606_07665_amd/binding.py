@@ -38,7 +38,8 @@ _DECLINED = -1     # its answer where the Python checks are to be run
 _NATIVE_CALLS = ("paged_decode_attention_ext", "paged_decode_attention_noalloc", "paged_decode_attention_append",
                  "pda_kv_append_n", "pda_attention_prelude", "pda_attention_prelude_append",
                  "pda_o_proj_residual_norm", "paged_decode_attention_sink", "paged_decode_attention_kv4", "pda_kv4_append",
-                 "pda_kv4_read", "pda_pages_update", "pda_pages_compact", "pda_pages_copy")
+                 "pda_kv4_read", "pda_pages_update", "pda_pages_compact", "pda_pages_copy", "pda_linear", "pda_moe_route",
+                 "pda_moe_experts", "pda_block_norm")
 
 
 class PdaError(RuntimeError):
@@ -58,6 +59,32 @@ class Projection(ctypes.Structure):
     """pda_projection of include/pda.h."""
     _fields_ = [(name, ctypes.c_int32) for name in ("row_tiles", "col_tiles", "wide", "col_groups", "k_splits", "fused",
                                                     "workgroups", "ss_parts")] + [("workspace_bytes", ctypes.c_int64)]
+
+
+class LinearDims(ctypes.Structure):
+    """pda_linear_dims of include/pda.h."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("batch", "in_features", "out_features", "activation", "gated", "out_f32")]
+
+
+class RouteDims(ctypes.Structure):
+    """pda_route_dims of include/pda.h."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("tokens", "num_experts", "top_k", "logit_stride", "sigmoid",
+                                                    "renormalise")] + [("scale", ctypes.c_float)]
+
+
+class MoeDims(ctypes.Structure):
+    """pda_moe_dims of include/pda.h."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("tokens", "hidden", "inter", "num_experts", "top_k", "activation")]
+
+
+class BlockNormDims(ctypes.Structure):
+    """pda_block_norm_dims of include/pda.h."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("rows", "hidden", "gate_rows")] + \
+               [(name, ctypes.c_float) for name in ("scale", "weight_offset", "eps")]
+
+
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3, "relu": 4}  # pda_activation
+SCORINGS = {"softmax": 0, "sigmoid": 1}
 
 
 class Pool(ctypes.Structure):
@@ -151,6 +178,16 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.pda_prelude_plan.restype = ctypes.c_int
     lib.pda_o_proj_plan.argtypes = [i32, i32, i32, i32, ctypes.POINTER(Projection)]
     lib.pda_o_proj_plan.restype = ctypes.c_int
+    lib.pda_linear.argtypes = [vp] * 5 + [ctypes.POINTER(LinearDims), vp]
+    lib.pda_linear_workspace_reserve.argtypes = [ctypes.POINTER(LinearDims), vp]
+    lib.pda_linear_plan.argtypes = [ctypes.POINTER(LinearDims), i32, ctypes.POINTER(Projection)]
+    lib.pda_moe_route.argtypes = [vp] * 4 + [ctypes.POINTER(RouteDims), vp]
+    lib.pda_moe_experts.argtypes = [vp] * 7 + [ctypes.POINTER(MoeDims), vp]
+    lib.pda_moe_workspace_reserve.argtypes = [ctypes.POINTER(MoeDims), vp]
+    lib.pda_block_norm.argtypes = [vp] * 7 + [ctypes.POINTER(BlockNormDims), vp]
+    for fn in (lib.pda_linear, lib.pda_linear_workspace_reserve, lib.pda_linear_plan, lib.pda_moe_route,
+               lib.pda_moe_experts, lib.pda_moe_workspace_reserve, lib.pda_block_norm):
+        fn.restype = ctypes.c_int
     lib.pda_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
     lib.pda_kv_append_n.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]
     lib.pda_kv_append_n.restype = ctypes.c_int
@@ -210,6 +247,7 @@ class _Declining:
 
     attention = kv_append = attention_append = prelude = o_proj = _decline
     attention_sink = attention_kv4 = kv4_tokens = pages_update = pages_compact = pages_copy = _decline
+    linear = moe_route = moe_experts = block_norm = _decline
 
 
 def _built_for() -> str:
@@ -937,3 +975,170 @@ def validate_paging(block_table, context_lens, num_pages, page_size, stream=None
     _validate([("block_table", block_table, torch.int32, "B M"), ("context_lens", context_lens, torch.int32, "B")])
     _check(load().pda_validate_paging(block_table.data_ptr(), context_lens.data_ptr(), block_table.shape[0],
                                       block_table.shape[1], page_size, num_pages, _stream_ptr(stream)))
+
+
+def _current(dev):
+    """The tensors' GPU as the current one (the library launches there), for calls that the native module left."""
+    import torch
+    return torch.cuda.device(dev)
+
+
+def _choice(name, value, choices):
+    if value not in choices:
+        raise ValueError(f"{name} must be one of {', '.join(choices)}, got {value!r}")
+    return choices[value]
+
+
+def linear(x, w_packed, out, *, bias=None, residual=None, activation="none", gated=False, stream=None):
+    """out = activation(x W^T + bias) + residual, or with ``gated`` W and bias
+    holding the gate's rows and then as many others, out = activation(x Wg^T +
+    bias_g) * (x Wu^T + bias_u) + residual.
+
+    x: bf16 [B, K]; w_packed: bf16 [N, K] from :func:`pack_weights` (gated:
+    [2 N, K]); bias: bf16 [N] (gated: [2 N]) or None; residual: bf16 [B, N] or
+    None; out: bf16 or fp32 [B, N], in bf16 possibly residual itself;
+    activation: "none", "silu", "gelu", "gelu_tanh" or "relu".  Returns out."""
+    act = _choice("activation", activation, ACTIVATIONS)
+    rc = (_nat or _load_native()).linear(x, w_packed, out, bias, residual, act, gated, stream)
+    if rc == PDA_OK:
+        return out
+    if rc != _DECLINED:
+        _check(rc)
+    import torch
+    bf = torch.bfloat16
+    if out.dtype not in (bf, torch.float32):
+        raise TypeError(f"out must be {bf} or {torch.float32}, got {out.dtype}")
+    sz = _validate([("x", x, bf, "B K"), ("out", out, out.dtype, "B N"), ("residual", residual, bf, "B N")])
+    _validate([("x", x, bf, "B K"), ("w_packed", w_packed, bf, "R K"), ("bias", bias, bf, "R")],
+              dict(sz, R=sz["N"] * (2 if gated else 1)))
+    dims = linear_dims(sz["B"], sz["K"], sz["N"], activation, gated, out.dtype is torch.float32)
+    with _current(x.device):
+        _check(load().pda_linear(x.data_ptr(), w_packed.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(),
+                                 ctypes.byref(dims), _stream_ptr(stream)))
+    return out
+
+
+def linear_dims(batch, in_features, out_features, activation="none", gated=False, out_f32=False) -> LinearDims:
+    return LinearDims(_i32("batch", batch), _i32("in_features", in_features), _i32("out_features", out_features),
+                      _choice("activation", activation, ACTIVATIONS), int(bool(gated)), int(bool(out_f32)))
+
+
+def linear_workspace_reserve(dims: LinearDims, stream=None) -> None:
+    _check(load().pda_linear_workspace_reserve(ctypes.byref(dims), _stream_ptr(stream)))
+
+
+def linear_plan(dims: LinearDims, num_cus: int = 256) -> Projection:
+    """How a linear product of these dims is split (no HIP call)."""
+    p = Projection()
+    _check(load().pda_linear_plan(ctypes.byref(dims), num_cus, ctypes.byref(p)))
+    return p
+
+
+def moe_route(logits, expert_ids, expert_weights, *, scoring="softmax", renormalise=True, select_bias=None, scale=1.0,
+              stream=None):
+    """Each token's top_k experts and their weights from the router's logits:
+    the best by score (softmax or sigmoid of the logits) plus select_bias, of
+    equal ones the lowest; weights are the scores, divided by the chosen ones'
+    sum with ``renormalise``, times ``scale``.
+
+    logits: fp32 [T, E], its rows contiguous but possibly further apart (a
+    slice of a wider product); expert_ids: int32 [T, top_k]; expert_weights:
+    fp32 [T, top_k]; select_bias: fp32 [E] or None.  Returns the two."""
+    sig = _choice("scoring", scoring, SCORINGS)
+    rc = (_nat or _load_native()).moe_route(logits, expert_ids, expert_weights, select_bias, sig, renormalise, scale, stream)
+    if rc == PDA_OK:
+        return expert_ids, expert_weights
+    if rc != _DECLINED:
+        _check(rc)
+    import torch
+    f32 = torch.float32
+    sz = _validate([("expert_ids", expert_ids, torch.int32, "T J"), ("expert_weights", expert_weights, f32, "T J"),
+                    ("select_bias", select_bias, f32, "E")])
+    if logits.dim() != 2 or logits.shape[0] != sz["T"] or logits.shape[1] != sz.get("E", logits.shape[1]):
+        raise ValueError(f"logits must be [T, E] with T = {sz['T']}" + (f", E = {sz['E']}" if "E" in sz else "") +
+                         f", got shape {tuple(logits.shape)}")
+    if logits.dtype != f32:
+        raise TypeError(f"logits must be {f32}, got {logits.dtype}")
+    if logits.device != expert_ids.device:
+        raise ValueError("all tensors must be on one GPU")
+    t, e = logits.shape
+    stride = logits.stride(0) if t > 1 else max(e, 1)
+    if (e > 1 and logits.stride(1) != 1) or stride < e:
+        raise ValueError("the rows of logits must be contiguous and apart")
+    dims = RouteDims(_i32("tokens", t), _i32("num_experts", e), _i32("top_k", sz["J"]), _i32("logit_stride", stride), sig,
+                     int(bool(renormalise)), float(scale))
+    with _current(logits.device):
+        _check(load().pda_moe_route(logits.data_ptr(), _ptr(select_bias), expert_ids.data_ptr(), expert_weights.data_ptr(),
+                                    ctypes.byref(dims), _stream_ptr(stream)))
+    return expert_ids, expert_weights
+
+
+def moe_experts(x, expert_ids, expert_weights, w_gate_up, w_down, out, *, residual=None, activation="silu", stream=None):
+    """out[t] = residual[t] + sum_j expert_weights[t, j] * D_e(activation(G_e
+    x[t]) * (U_e x[t])) with e = expert_ids[t, j]; an id outside [0, E) adds
+    nothing.
+
+    x, residual, out: bf16 [T, H] (out may be either of the others);
+    expert_ids: int32 [T, top_k]; expert_weights: fp32 [T, top_k]; w_gate_up:
+    bf16 [E, 2 F, H], each expert's rows of G and then of U, and w_down: bf16
+    [E, H, F], packed by :func:`pack_weights` as one matrix of all the experts'
+    rows (``pack_weights(w.flatten(0, 1)).view(w.shape)``).  Returns out."""
+    act = _choice("activation", activation, ACTIVATIONS)
+    rc = (_nat or _load_native()).moe_experts(x, expert_ids, expert_weights, w_gate_up, w_down, out, residual, act, stream)
+    if rc == PDA_OK:
+        return out
+    if rc != _DECLINED:
+        _check(rc)
+    import torch
+    bf = torch.bfloat16
+    sz = _validate([("x", x, bf, "T H"), ("expert_ids", expert_ids, torch.int32, "T J"),
+                    ("expert_weights", expert_weights, torch.float32, "T J"), ("w_down", w_down, bf, "E H F"),
+                    ("out", out, bf, "T H"), ("residual", residual, bf, "T H")])
+    _validate([("x", x, bf, "T H"), ("w_gate_up", w_gate_up, bf, "E R H")], dict(sz, R=2 * sz["F"]))
+    dims = moe_dims(sz["T"], sz["H"], sz["F"], sz["E"], sz["J"], activation)
+    with _current(x.device):
+        _check(load().pda_moe_experts(x.data_ptr(), expert_ids.data_ptr(), expert_weights.data_ptr(), w_gate_up.data_ptr(),
+                                      w_down.data_ptr(), _ptr(residual), out.data_ptr(), ctypes.byref(dims),
+                                      _stream_ptr(stream)))
+    return out
+
+
+def moe_dims(tokens, hidden, inter, num_experts, top_k, activation="silu") -> MoeDims:
+    return MoeDims(_i32("tokens", tokens), _i32("hidden", hidden), _i32("inter", inter), _i32("num_experts", num_experts),
+                   _i32("top_k", top_k), _choice("activation", activation, ACTIVATIONS))
+
+
+def moe_workspace_reserve(dims: MoeDims, stream=None) -> None:
+    _check(load().pda_moe_workspace_reserve(ctypes.byref(dims), _stream_ptr(stream)))
+
+
+def block_norm(y, residual, residual_out, normed_out=None, *, post_w=None, pre_w=None, gate=None, scale=1.0,
+               weight_offset=0.0, eps=1e-5, stream=None):
+    """The norms around a block's output y: with u = RMSNorm(y) * (post_w +
+    weight_offset), or y where post_w is None, residual_out = z = residual +
+    scale * gate * u, and with pre_w normed_out = RMSNorm(z) * (pre_w +
+    weight_offset).
+
+    y, residual, residual_out, normed_out: bf16 [R, H] (residual may be None:
+    0; each output may be y or residual itself); post_w, pre_w: bf16 [H] or
+    None; gate: bf16 [H] or [R, H] or None.  Returns residual_out,
+    normed_out."""
+    rc = (_nat or _load_native()).block_norm(y, residual, residual_out, normed_out, post_w, pre_w, gate, scale,
+                                             weight_offset, eps, stream)
+    if rc == PDA_OK:
+        return residual_out, normed_out
+    if rc != _DECLINED:
+        _check(rc)
+    import torch
+    if (pre_w is None) != (normed_out is None):
+        raise ValueError("pre_w and normed_out must both be given or both be None")
+    bf = torch.bfloat16
+    sz = _validate([("y", y, bf, "R H"), ("residual", residual, bf, "R H"), ("residual_out", residual_out, bf, "R H"),
+                    ("normed_out", normed_out, bf, "R H"), ("post_w", post_w, bf, "H"), ("pre_w", pre_w, bf, "H"),
+                    ("gate", gate, bf, "H" if gate is not None and gate.dim() == 1 else "R H")])
+    dims = BlockNormDims(_i32("rows", sz["R"]), _i32("hidden", sz["H"]), int(gate is not None and gate.dim() == 2),
+                         float(scale), float(weight_offset), float(eps))
+    with _current(y.device):
+        _check(load().pda_block_norm(y.data_ptr(), _ptr(residual), _ptr(post_w), _ptr(pre_w), _ptr(gate),
+                                     residual_out.data_ptr(), _ptr(normed_out), ctypes.byref(dims), _stream_ptr(stream)))
+    return residual_out, normed_out

@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -19,6 +20,7 @@
 
 #include "pda.h"
 #include "pda_append.h"
+#include "pda_ffn.h"
 #include "pda_probe.h"
 #include "pda_gemv.h"
 #include "pda_internal.h"
@@ -855,6 +857,10 @@ int check_prelude(const pda_prelude_dims* dm) {
   return PDA_OK;
 }
 
+pda::Fusable prelude_fusable(bool qk_norm, bool interleaved, int rotary_dim) {
+  return pda::prelude_fusable(qk_norm, interleaved, rotary_dim) ? pda::Fusable::kPairs : pda::Fusable::kNo;
+}
+
 int64_t prelude_rows(const pda_prelude_dims& d) {
   return static_cast<int64_t>(d.num_q_heads + 2 * d.num_kv_heads) * d.head_dim;
 }
@@ -863,6 +869,77 @@ bool overlaps(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a && b && x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
 }
+
+// An output that is not one of the arrays it may replace lies apart from all
+// that is read.
+struct Extent {
+  const char* name;
+  const void* p;
+  int64_t bytes;
+};
+int check_apart(const Extent& out, std::initializer_list<Extent> others) {
+  for (const Extent& o : others)
+    if (overlaps(out.p, out.bytes, o.p, o.bytes)) return fail(PDA_ERR_LAYOUT, "%s overlaps %s", out.name, o.name);
+  return PDA_OK;
+}
+
+// ------------------------------------------------------------ feed-forward
+int check_linear(const pda_linear_dims* dm) {
+  if (!dm) return fail(PDA_ERR_NULL, "dims is NULL");
+  const pda_linear_dims& d = *dm;
+  if (d.batch < 0) return fail(PDA_ERR_SHAPE, "batch must be >= 0 (got %d)", d.batch);
+  if (d.batch > pda::kMaxGemvBatch) return fail(PDA_ERR_UNSUPPORTED, "batch %d exceeds %d", d.batch, pda::kMaxGemvBatch);
+  if (d.in_features <= 0 || d.out_features <= 0) return fail(PDA_ERR_SHAPE, "in_features and out_features must be positive");
+  if (d.in_features % pda::kTileK || d.in_features > 65536)
+    return fail(PDA_ERR_UNSUPPORTED, "in_features %d (supported: multiples of 32 up to 65536)", d.in_features);
+  if (d.out_features % pda::kTileRows || d.out_features > pda::kMaxLinearFeatures)
+    return fail(PDA_ERR_UNSUPPORTED, "out_features %d (supported: multiples of 16 up to %d)", d.out_features,
+                pda::kMaxLinearFeatures);
+  if (d.activation < PDA_ACT_NONE || d.activation > PDA_ACT_RELU)
+    return fail(PDA_ERR_UNSUPPORTED, "activation %d is not a pda_activation", d.activation);
+  if ((d.gated != 0 && d.gated != 1) || (d.out_f32 != 0 && d.out_f32 != 1))
+    return fail(PDA_ERR_SHAPE, "gated and out_f32 must be 0 or 1");
+  if (d.gated && static_cast<int64_t>(d.in_features) * d.out_features > pda::kMaxGatedElements)
+    return fail(PDA_ERR_UNSUPPORTED, "a gated product takes in_features * out_features up to %lld",
+                static_cast<long long>(pda::kMaxGatedElements));
+  return PDA_OK;
+}
+
+int linear_rows(const pda_linear_dims& d) { return d.gated ? 2 * d.out_features : d.out_features; }
+
+pda::RowsPlan linear_plan(const pda_linear_dims& d, int cus) {
+  return pda::plan_rows(d.batch, linear_rows(d), d.in_features, cus, d.gated ? pda::Fusable::kPairs : pda::Fusable::kAny,
+                        pda::kMaxRowsSplits);
+}
+
+int64_t linear_ws_bytes(const pda_linear_dims& d, int cus) {
+  return align256(pda::rows_most_floats(d.batch, linear_rows(d), cus, pda::kMaxRowsSplits) * 4);
+}
+
+int check_moe(const pda_moe_dims* dm) {
+  if (!dm) return fail(PDA_ERR_NULL, "dims is NULL");
+  const pda_moe_dims& d = *dm;
+  if (d.tokens < 0) return fail(PDA_ERR_SHAPE, "tokens must be >= 0 (got %d)", d.tokens);
+  if (d.tokens > pda::kMaxMoeTokens) return fail(PDA_ERR_UNSUPPORTED, "tokens %d exceeds %d", d.tokens, pda::kMaxMoeTokens);
+  if (d.hidden <= 0 || d.inter <= 0 || d.num_experts <= 0 || d.top_k <= 0)
+    return fail(PDA_ERR_SHAPE, "hidden, inter, num_experts and top_k must be positive");
+  if (d.hidden % pda::kTileK || d.hidden > 32768)
+    return fail(PDA_ERR_UNSUPPORTED, "hidden %d (supported: multiples of 32 up to 32768)", d.hidden);
+  if (d.inter % pda::kTileK || d.inter > 65536)
+    return fail(PDA_ERR_UNSUPPORTED, "inter %d (supported: multiples of 32 up to 65536)", d.inter);
+  if (d.num_experts > pda::kMaxExperts || d.top_k > pda::kMaxTopK)
+    return fail(PDA_ERR_UNSUPPORTED, "num_experts %d, top_k %d (supported: up to %d and %d)", d.num_experts, d.top_k,
+                pda::kMaxExperts, pda::kMaxTopK);
+  if (static_cast<int64_t>(d.num_experts) * std::max(2 * d.inter, d.hidden) >= (int64_t{1} << 31))
+    return fail(PDA_ERR_UNSUPPORTED, "num_experts * 2 inter and num_experts * hidden must be below 2^31");
+  if (d.activation < PDA_ACT_NONE || d.activation > PDA_ACT_RELU)
+    return fail(PDA_ERR_UNSUPPORTED, "activation %d is not a pda_activation", d.activation);
+  return PDA_OK;
+}
+
+// h [pairs, inter] in bf16, then y [pairs, hidden] in fp32.
+int64_t moe_h_bytes(const pda_moe_dims& d) { return align256(int64_t{2} * d.tokens * d.top_k * d.inter); }
+int64_t moe_ws_bytes(const pda_moe_dims& d) { return moe_h_bytes(d) + align256(int64_t{4} * d.tokens * d.top_k * d.hidden); }
 
 // k splits of an output projection: only where the kernel that adds them
 // holds a row of z.
@@ -879,7 +956,7 @@ int64_t prelude_ws_bytes(const pda_prelude_dims& d, int cus) {
 }
 
 pda::RowsPlan oproj_plan(int batch, int in_features, int hidden, int cus) {
-  return pda::plan_rows(batch, hidden, in_features, cus, false, oproj_splits(hidden));
+  return pda::plan_rows(batch, hidden, in_features, cus, pda::Fusable::kNo, oproj_splits(hidden));
 }
 
 // o_proj workspace: z [splits, batch, hidden] in fp32, then the partial sums
@@ -975,7 +1052,8 @@ int run_prelude(const void* x, const void* w_packed, const void* bias, const voi
       fusable = fusable && !overlaps(o.p, o.bytes, x, static_cast<int64_t>(d.batch) * d.hidden * 2) &&
               !overlaps(o.p, o.bytes, w_packed, static_cast<int64_t>(g.n) * g.k * 2);
   }
-  const pda::RowsPlan plan = pda::plan_rows(g.batch, g.n, g.k, cus, fusable, pda::kMaxRowsSplits);
+  const pda::RowsPlan plan = pda::plan_rows(g.batch, g.n, g.k, cus, fusable ? pda::Fusable::kPairs : pda::Fusable::kNo,
+                                            pda::kMaxRowsSplits);
   const bool fused = plan.fused;
   void* ws = nullptr;
   const int64_t least = fused ? 0 : align256(static_cast<int64_t>(plan.splits) * g.batch * g.n * 4);
@@ -1683,6 +1761,239 @@ int pda_o_proj_plan(int32_t batch, int32_t in_features, int32_t hidden, int32_t 
   return PDA_OK;
 }
 
+int pda_linear(const void* x, const void* w_packed, const void* bias, const void* residual, void* out,
+               const pda_linear_dims* dims, void* stream) {
+  g_err.clear();
+  int rc = check_linear(dims);
+  if (rc) return rc;
+  const pda_linear_dims& d = *dims;
+  if (d.batch == 0) return PDA_OK;
+  if (!x || !w_packed || !out) return fail(PDA_ERR_NULL, "a tensor pointer is NULL");
+  if (misaligned(x, 16) || misaligned(w_packed, 16)) return fail(PDA_ERR_ALIGN, "x and w_packed must be 16-byte aligned");
+  if (misaligned(bias, 2) || misaligned(residual, 2) || misaligned(out, d.out_f32 ? 4 : 2))
+    return fail(PDA_ERR_ALIGN, "bf16 arrays must be 2-byte and an fp32 out 4-byte aligned");
+  const int rows = linear_rows(d);
+  const int64_t features = static_cast<int64_t>(d.batch) * d.out_features;
+  const Extent o{"out", out, features * (d.out_f32 ? 4 : 2)};
+  const bool in_place = out == residual && !d.out_f32;
+  if ((rc = check_apart(o, {{"x", x, int64_t{2} * d.batch * d.in_features},
+                            {"w_packed", w_packed, int64_t{2} * rows * d.in_features},
+                            {"bias", bias, int64_t{2} * rows},
+                            {"residual", in_place ? nullptr : residual, 2 * features}})))
+    return rc;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  int cus = 0;
+  if ((rc = device_cus(dev, &cus))) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const pda::RowsPlan plan = linear_plan(d, cus);
+  void* ws = nullptr;
+  const int64_t least = plan.fused ? 0 : align256(int64_t{4} * plan.splits * d.batch * rows);
+  if ((rc = workspace_for(dev, st, least, linear_ws_bytes(d, cus), &ws))) return rc;
+  pda::RowsArgs g{};
+  g.x = static_cast<const uint16_t*>(x);
+  g.wp = static_cast<const uint16_t*>(w_packed);
+  g.y = plan.fused ? nullptr : static_cast<float*>(ws);
+  g.batch = d.batch;
+  g.n = rows;
+  g.k = d.in_features;
+  pda::LinearArgs l;
+  l.bias = static_cast<const uint16_t*>(bias);
+  l.residual = static_cast<const uint16_t*>(residual);
+  l.out = out;
+  l.features = d.out_features;
+  l.activation = d.activation;
+  l.f32 = d.out_f32;
+  e = plan.fused ? pda::launch_rows_linear(g, plan, l, d.gated != 0, st) : pda::launch_rows(g, plan, st);
+  if (e != hipSuccess) return hip_fail(e, "linear kernel launch");
+  if (!plan.fused && (e = pda::launch_linear_epilogue(l, g.y, plan.splits, d.batch, d.gated != 0, st)) != hipSuccess)
+    return hip_fail(e, "linear epilogue launch");
+  return PDA_OK;
+}
+
+int pda_linear_workspace_reserve(const pda_linear_dims* dims, void* stream) {
+  g_err.clear();
+  int rc = check_linear(dims);
+  if (rc) return rc;
+  if (dims->batch == 0) return PDA_OK;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  int cus = 0;
+  if ((rc = device_cus(dev, &cus))) return rc;
+  void* ptr = nullptr;
+  const int64_t need = linear_ws_bytes(*dims, cus);
+  return workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr);
+}
+
+int pda_linear_plan(const pda_linear_dims* dims, int32_t num_cus, pda_projection* out) {
+  g_err.clear();
+  if (!out) return fail(PDA_ERR_NULL, "pda_linear_plan: NULL output pointer");
+  int rc = check_linear(dims);
+  if (rc) return rc;
+  if (num_cus <= 0) return fail(PDA_ERR_SHAPE, "num_cus must be positive");
+  *out = pda_projection{};
+  if (dims->batch == 0) return PDA_OK;
+  *out = projection(linear_plan(*dims, num_cus), linear_ws_bytes(*dims, num_cus));
+  return PDA_OK;
+}
+
+int pda_moe_route(const float* logits, const float* select_bias, int32_t* expert_ids, float* expert_weights,
+                  const pda_route_dims* dims, void* stream) {
+  g_err.clear();
+  if (!dims) return fail(PDA_ERR_NULL, "dims is NULL");
+  const pda_route_dims& d = *dims;
+  if (d.tokens < 0) return fail(PDA_ERR_SHAPE, "tokens must be >= 0 (got %d)", d.tokens);
+  if (d.tokens > pda::kMaxRouteTokens)
+    return fail(PDA_ERR_UNSUPPORTED, "tokens %d exceeds %d", d.tokens, pda::kMaxRouteTokens);
+  if (d.num_experts <= 0 || d.top_k <= 0) return fail(PDA_ERR_SHAPE, "num_experts and top_k must be positive");
+  if (d.num_experts > pda::kMaxExperts || d.top_k > pda::kMaxTopK)
+    return fail(PDA_ERR_UNSUPPORTED, "num_experts %d, top_k %d (supported: up to %d and %d)", d.num_experts, d.top_k,
+                pda::kMaxExperts, pda::kMaxTopK);
+  if (d.top_k > d.num_experts) return fail(PDA_ERR_SHAPE, "top_k %d of %d experts", d.top_k, d.num_experts);
+  if (d.logit_stride < d.num_experts)
+    return fail(PDA_ERR_LAYOUT, "logit_stride %d is below num_experts %d", d.logit_stride, d.num_experts);
+  if ((d.sigmoid != 0 && d.sigmoid != 1) || (d.renormalise != 0 && d.renormalise != 1))
+    return fail(PDA_ERR_SHAPE, "sigmoid and renormalise must be 0 or 1");
+  if (!std::isfinite(d.scale)) return fail(PDA_ERR_SCALE, "scale must be finite");
+  if (d.tokens == 0) return PDA_OK;
+  if (!logits || !expert_ids || !expert_weights) return fail(PDA_ERR_NULL, "a tensor pointer is NULL");
+  if (misaligned(logits, 4) || misaligned(select_bias, 4) || misaligned(expert_ids, 4) || misaligned(expert_weights, 4))
+    return fail(PDA_ERR_ALIGN, "logits, select_bias, expert_ids and expert_weights must be 4-byte aligned");
+  const int64_t out = int64_t{4} * d.tokens * d.top_k;
+  const Extent in{"logits", logits, int64_t{4} * ((d.tokens - 1) * static_cast<int64_t>(d.logit_stride) + d.num_experts)};
+  const Extent bias{"select_bias", select_bias, int64_t{4} * d.num_experts};
+  int rc = check_apart({"expert_ids", expert_ids, out}, {in, bias, {"expert_weights", expert_weights, out}});
+  if (rc || (rc = check_apart({"expert_weights", expert_weights, out}, {in, bias}))) return rc;
+  pda::RouteArgs a;
+  a.logits = logits;
+  a.select_bias = select_bias;
+  a.ids = expert_ids;
+  a.weights = expert_weights;
+  a.stride = d.logit_stride;
+  a.tokens = d.tokens;
+  a.experts = d.num_experts;
+  a.top_k = d.top_k;
+  a.sigmoid = d.sigmoid;
+  a.renormalise = d.renormalise;
+  a.scale = d.scale;
+  hipError_t e = pda::launch_route(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "route kernel launch");
+  return PDA_OK;
+}
+
+int pda_moe_experts(const void* x, const int32_t* expert_ids, const float* expert_weights, const void* w_gate_up,
+                    const void* w_down, const void* residual, void* out, const pda_moe_dims* dims, void* stream) {
+  g_err.clear();
+  int rc = check_moe(dims);
+  if (rc) return rc;
+  const pda_moe_dims& d = *dims;
+  if (d.tokens == 0) return PDA_OK;
+  if (!x || !expert_ids || !expert_weights || !w_gate_up || !w_down || !out)
+    return fail(PDA_ERR_NULL, "a tensor pointer is NULL");
+  if (misaligned(x, 16) || misaligned(w_gate_up, 16) || misaligned(w_down, 16))
+    return fail(PDA_ERR_ALIGN, "x, w_gate_up and w_down must be 16-byte aligned");
+  if (misaligned(expert_ids, 4) || misaligned(expert_weights, 4) || misaligned(residual, 2) || misaligned(out, 2))
+    return fail(PDA_ERR_ALIGN, "expert_ids and expert_weights must be 4-byte, residual and out 2-byte aligned");
+  const int64_t rows = int64_t{2} * d.tokens * d.hidden, pairs = static_cast<int64_t>(d.tokens) * d.top_k;
+  const int64_t matrix = int64_t{2} * d.num_experts * d.hidden * d.inter;
+  if ((rc = check_apart({"out", out, rows}, {{"x", out == x ? nullptr : x, rows},
+                                             {"residual", out == residual ? nullptr : residual, rows},
+                                             {"expert_ids", expert_ids, 4 * pairs},
+                                             {"expert_weights", expert_weights, 4 * pairs},
+                                             {"w_gate_up", w_gate_up, 2 * matrix},
+                                             {"w_down", w_down, matrix}})))
+    return rc;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  int cus = 0;
+  if ((rc = device_cus(dev, &cus))) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  void* ws = nullptr;
+  const int64_t need = moe_ws_bytes(d);
+  if ((rc = workspace_for(dev, st, need, need, &ws))) return rc;
+  pda::ExpertsArgs a;
+  a.x = static_cast<const uint16_t*>(x);
+  a.ids = expert_ids;
+  a.weights = expert_weights;
+  a.w_gate_up = static_cast<const uint16_t*>(w_gate_up);
+  a.w_down = static_cast<const uint16_t*>(w_down);
+  a.residual = static_cast<const uint16_t*>(residual);
+  a.out = static_cast<uint16_t*>(out);
+  a.h = static_cast<uint16_t*>(ws);
+  a.y = reinterpret_cast<float*>(static_cast<char*>(ws) + moe_h_bytes(d));
+  a.tokens = d.tokens;
+  a.hidden = d.hidden;
+  a.inter = d.inter;
+  a.experts = d.num_experts;
+  a.top_k = d.top_k;
+  a.activation = d.activation;
+  if ((e = pda::launch_experts(a, cus, st)) != hipSuccess) return hip_fail(e, "experts kernel launch");
+  return PDA_OK;
+}
+
+int pda_moe_workspace_reserve(const pda_moe_dims* dims, void* stream) {
+  g_err.clear();
+  int rc = check_moe(dims);
+  if (rc) return rc;
+  if (dims->tokens == 0) return PDA_OK;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  void* ptr = nullptr;
+  const int64_t need = moe_ws_bytes(*dims);
+  return workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr);
+}
+
+int pda_block_norm(const void* y, const void* residual, const void* post_w, const void* pre_w, const void* gate,
+                   void* residual_out, void* normed_out, const pda_block_norm_dims* dims, void* stream) {
+  g_err.clear();
+  if (!dims) return fail(PDA_ERR_NULL, "dims is NULL");
+  const pda_block_norm_dims& d = *dims;
+  if (d.rows < 0) return fail(PDA_ERR_SHAPE, "rows must be >= 0 (got %d)", d.rows);
+  if (d.rows > pda::kMaxNormRows) return fail(PDA_ERR_UNSUPPORTED, "rows %d exceeds %d", d.rows, pda::kMaxNormRows);
+  if (d.hidden <= 0) return fail(PDA_ERR_SHAPE, "hidden must be positive");
+  if (d.hidden % 8 || d.hidden > 32768)
+    return fail(PDA_ERR_UNSUPPORTED, "hidden %d (supported: multiples of 8 up to 32768)", d.hidden);
+  if (d.gate_rows != 0 && d.gate_rows != 1) return fail(PDA_ERR_SHAPE, "gate_rows must be 0 or 1");
+  if (!std::isfinite(d.scale) || !std::isfinite(d.weight_offset) || !std::isfinite(d.eps) || d.eps < 0.f)
+    return fail(PDA_ERR_SCALE, "scale, weight_offset and eps must be finite and eps >= 0");
+  if (d.rows == 0) return PDA_OK;
+  if ((pre_w == nullptr) != (normed_out == nullptr))
+    return fail(PDA_ERR_NULL, "pre_w and normed_out must both be given or both be NULL");
+  if (!y || !residual_out) return fail(PDA_ERR_NULL, "a tensor pointer is NULL");
+  for (const void* p : {y, residual, post_w, pre_w, gate, static_cast<const void*>(residual_out),
+                        static_cast<const void*>(normed_out)})
+    if (misaligned(p, 2)) return fail(PDA_ERR_ALIGN, "bf16 arrays must be 2-byte aligned");
+  const int64_t all = int64_t{2} * d.rows * d.hidden, one = int64_t{2} * d.hidden;
+  const Extent post{"post_w", post_w, one}, pre{"pre_w", pre_w, one}, g{"gate", gate, d.gate_rows ? all : one};
+  for (const Extent& o : {Extent{"residual_out", residual_out, all}, Extent{"normed_out", normed_out, all}}) {
+    const int rc = check_apart(o, {{"y", o.p == y ? nullptr : y, all}, {"residual", o.p == residual ? nullptr : residual, all},
+                                   post, pre, g});
+    if (rc) return rc;
+  }
+  if (overlaps(residual_out, all, normed_out, all)) return fail(PDA_ERR_LAYOUT, "normed_out overlaps residual_out");
+  pda::BlockNormArgs a;
+  a.y = static_cast<const uint16_t*>(y);
+  a.residual = static_cast<const uint16_t*>(residual);
+  a.post_w = static_cast<const uint16_t*>(post_w);
+  a.pre_w = static_cast<const uint16_t*>(pre_w);
+  a.gate = static_cast<const uint16_t*>(gate);
+  a.z = static_cast<uint16_t*>(residual_out);
+  a.h = static_cast<uint16_t*>(normed_out);
+  a.gate_stride = d.gate_rows ? d.hidden : 0;
+  a.rows = d.rows;
+  a.hidden = d.hidden;
+  a.scale = d.scale;
+  a.weight_offset = d.weight_offset;
+  a.eps = d.eps;
+  hipError_t e = pda::launch_block_norm(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "block norm kernel launch");
+  return PDA_OK;
+}
+
 int pda_prelude_plan(const pda_prelude_dims* dims, int32_t qk_norm, int32_t num_cus, pda_projection* out) {
   g_err.clear();
   if (!out) return fail(PDA_ERR_NULL, "pda_prelude_plan: NULL output pointer");
@@ -1694,7 +2005,7 @@ int pda_prelude_plan(const pda_prelude_dims* dims, int32_t qk_norm, int32_t num_
   const pda_prelude_dims& d = *dims;
   const pda::RowsPlan plan =
       pda::plan_rows(d.batch, static_cast<int>(prelude_rows(d)), d.hidden, num_cus,
-                     pda::prelude_fusable(qk_norm != 0, d.interleaved != 0, d.rotary_dim), pda::kMaxRowsSplits);
+                     prelude_fusable(qk_norm != 0, d.interleaved != 0, d.rotary_dim), pda::kMaxRowsSplits);
   *out = projection(plan, prelude_ws_bytes(d, num_cus));
   return PDA_OK;
 }

@@ -23,7 +23,7 @@ struct RowsPlan {
   int rt, bt, waves;
   int kb;          // steps per block of weights
   bool wide;       // 32 x 32 x 16 matrix-core tiles instead of 16 x 16 x 32
-  bool fused;      // the prelude epilogue runs in rows_kernel
+  bool fused;      // the epilogue runs in rows_kernel
   int row_groups, col_groups;
   int splits;      // of k (1 unless the epilogue is a kernel of its own)
   int split_grid;  // workgroups of one split
@@ -40,9 +40,11 @@ constexpr int rows_ss_parts(int rt, int bt, int waves, bool wide) {
 
 constexpr int kMaxSsParts = 4;
 
-// fusable: the prelude epilogue may run in the kernel (the plan says whether
-// it is to).  max_splits: at most kMaxRowsSplits.
-RowsPlan plan_rows(int batch, int n, int k, int num_cus, bool fusable, int max_splits);
+// fusable: whether the epilogue may run in the kernel (the plan says whether
+// it is to), in any form or only in those whose row tiles go in pairs.
+// max_splits: at most kMaxRowsSplits.
+enum class Fusable { kNo = 0, kPairs = 1, kAny = 2 };
+RowsPlan plan_rows(int batch, int n, int k, int num_cus, Fusable fusable, int max_splits);
 // Most floats of y, all splits together, that the plan of any k and any batch
 // up to `batch` has: never less for a larger batch.
 int64_t rows_most_floats(int batch, int n, int num_cus, int max_splits);
@@ -97,6 +99,23 @@ struct OProjArgs {
   float eps;
 };
 
+// What a linear product's epilogue does, in rows_kernel or in linear_epilogue:
+// out = act(y + bias) (* (y_up + bias_up) with a gate) + residual.
+constexpr int kLinearThreads = 256;
+constexpr int kMaxLinearFeatures = 262144;
+// A gated pair's up tile is reached from its gate tile's descriptor, whose bytes
+// stay below 2^31.
+constexpr int64_t kMaxGatedElements = 1000000000;
+struct LinearArgs {
+  const uint16_t* bias;      // bf16 [features], gated [2 features], or null
+  const uint16_t* residual;  // bf16 [batch, features] or null
+  void* out;                 // bf16 or (f32) fp32 [batch, features]; may be residual
+  int features;              // output features: half the rows of W with a gate
+  int activation;            // pda_activation
+  int f32;
+};
+struct GatedArgs : LinearArgs {};  // W holds the gate's rows, then as many of the other factor
+
 struct RowsArgs {
   const uint16_t* x;   // bf16 [batch, k]
   const uint16_t* wp;  // packed bf16 [n, k]
@@ -113,6 +132,9 @@ hipError_t launch_rows(const RowsArgs& a, const RowsPlan& p, hipStream_t st);
 hipError_t launch_rows_prelude(const RowsArgs& a, const RowsPlan& p, const PreludeArgs& e, hipStream_t st);
 // z = y + residual and the partial sums of z^2
 hipError_t launch_rows_residual(const RowsArgs& a, const RowsPlan& p, const OProjArgs& o, hipStream_t st);
+// with the whole linear epilogue (gated: a plan made with pairs)
+hipError_t launch_rows_linear(const RowsArgs& a, const RowsPlan& p, const LinearArgs& e, bool gated, hipStream_t st);
+hipError_t launch_linear_epilogue(const LinearArgs& a, const float* y, int splits, int batch, bool gated, hipStream_t st);
 hipError_t launch_prelude_epilogue(const PreludeArgs& a, hipStream_t st);
 hipError_t launch_oproj_sum(const OProjArgs& a, hipStream_t st);
 hipError_t launch_oproj_norm(const OProjArgs& a, hipStream_t st);

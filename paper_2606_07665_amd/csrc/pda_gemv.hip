@@ -28,6 +28,8 @@
 // spans all features of a sequence and is a second, small kernel.
 #include "pda_gemv.h"
 
+#include "pda_device.h"
+
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -35,25 +37,6 @@
 
 namespace pda {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kBufferDword3 = 0x00020000;  // raw 32-bit buffer format
-constexpr int kCachePolicyNT = 2;          // non-temporal: weights are read once
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, uint32_t bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(base);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a >> 32));
-  void* ub = reinterpret_cast<void*>((static_cast<uint64_t>(hi) << 32) | lo);
-  return __builtin_amdgcn_make_buffer_rsrc(ub, 0, static_cast<int>(__builtin_amdgcn_readfirstlane(bytes)),
-                                           kBufferDword3);
-}
 
 // Packed layout: tile (t, kt) of rows 16t .. 16t+15 and k 32kt .. 32kt+31 is
 // stored at element (t * (k / 32) + kt) * 512; inside it, 16-byte chunk l
@@ -71,14 +54,6 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const uint16_t* __re
   const int64_t row = t * kTileRows + (l & 15);
   const int64_t col = static_cast<int64_t>(kt) * kTileK + 8 * (l >> 4);
   *reinterpret_cast<u32x4*>(wp + chunk * 8) = *reinterpret_cast<const u32x4*>(w + row * k + col);
-}
-
-__device__ __forceinline__ float bf16_to_f32(uint16_t h) {
-  return __builtin_bit_cast(float, static_cast<uint32_t>(h) << 16);
-}
-
-__device__ __forceinline__ uint16_t f32_to_bf16(float f) {
-  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f));
 }
 
 // y[b, n] = sum_k x[b, k] W[n, k] over a packed W.  A workgroup takes RT row
@@ -120,32 +95,20 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
 // of the workgroup takes the same number of blocks with fixed wait counts.
 struct NoEpilogue {};
 
+// Four (or two) consecutive features of a linear product, from element `at` on.
+template <int N>
+__device__ __forceinline__ void store_features(const LinearArgs& e, int64_t at, const float (&v)[N]) {
+  if (e.f32)
+    __builtin_memcpy(static_cast<float*>(e.out) + at, v, 4 * N);
+  else
+    store_bf16<N>(static_cast<uint16_t*>(e.out) + at, v);
+}
+
 // waves per SIMD the register budget is set for
 constexpr int rows_min_waves(int rt, int bt, int w, int kb) { return w > 4 ? (rt * bt * kb <= 4 ? 4 : 2) : 1; }
-// s_waitcnt vmcnt(n) alone; vmcnt is split over bits 3:0 and 15:14
-constexpr int kWaitLoads = 0x0F70;
-constexpr int wait_loads(int n) { return kWaitLoads | (n & 15) | ((n >> 4) << 14); }
 __host__ __device__ constexpr int rows_lds_bytes(int rt, int bt, int w, int dx) {
   const int ring = w * dx * bt * 2048, sum = w * rt * bt * 1024;
   return ring > sum ? ring : sum;
-}
-
-// N consecutive bf16 values, packed two to a register; p need only be 2-byte
-// aligned (the memory pipeline takes any alignment).
-template <int N>
-__device__ __forceinline__ void load_bf16(const uint16_t* p, uint32_t* v) {
-  __builtin_memcpy(v, p, 2 * N);
-}
-__device__ __forceinline__ float unpack_bf16(const uint32_t* v, int j) {
-  return bf16_to_f32(static_cast<uint16_t>(v[j / 2] >> (16 * (j & 1))));
-}
-template <int N>
-__device__ __forceinline__ void store_bf16(uint16_t* p, const float (&v)[N]) {
-  uint32_t w[N / 2];
-#pragma unroll
-  for (int j = 0; j < N / 2; ++j)
-    w[j] = f32_to_bf16(v[2 * j]) | (static_cast<uint32_t>(f32_to_bf16(v[2 * j + 1])) << 16);
-  __builtin_memcpy(p, w, 2 * N);
 }
 
 // Sine and cosine of position pos at rotary pair i0 + j, j < N (i0 a multiple
@@ -178,8 +141,11 @@ template <int RT, int BT, int W, int DX, int KB, bool kWide, bool kShared, class
 __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_kernel(RowsArgs a, Epilogue e) {
   constexpr bool kPrelude = std::is_same<Epilogue, PreludeArgs>::value;
   constexpr bool kResidual = std::is_same<Epilogue, OProjArgs>::value;
+  constexpr bool kGated = std::is_same<Epilogue, GatedArgs>::value;
+  constexpr bool kLinear = kGated || std::is_same<Epilogue, LinearArgs>::value;
+  constexpr bool kPairs = kPrelude || kGated;  // an output takes rows of both tiles of a pair
   static_assert(KB % DX == 0, "a block of weights covers whole turns of the activation ring");
-  static_assert(!kPrelude || RT % 2 == 0, "the prelude's row tiles go in pairs");
+  static_assert(!kPairs || RT % 2 == 0, "these row tiles go in pairs");
   static_assert(!kWide || (RT % 2 == 0 && BT % 2 == 0), "wide tiles take row and column tiles in pairs");
   constexpr int kSlot = BT * 2048;               // one step's activations of a wave
   constexpr int kLx = 2 * BT, kLw = 2 * RT;      // vector memory instructions of a step
@@ -190,10 +156,10 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
   constexpr int kTR = kWide ? RT / 2 : RT, kTC = kWide ? BT / 2 : BT;
   constexpr int kTM = kWide ? 4 : 2, kTG = kWide ? 4 : 1;
   using Acc = typename std::conditional<kWide, f32x16, f32x4>::type;
-  // epilogue items: a group of one accumulator, or for the prelude the same
+  // epilogue items: a group of one accumulator, or with pairs the same
   // group of both row tiles of a pair; half the rows of each lane where
   // there are fewer groups than waves
-  constexpr int kUnits = kTR * kTC * kTG / (kPrelude ? 2 : 1);
+  constexpr int kUnits = kTR * kTC * kTG / (kPairs ? 2 : 1);
   constexpr int kSub = kUnits < W ? 2 : 1;
   constexpr int kRows = 4 / kSub;                // rows per lane of an item
   constexpr int kItems = kUnits * kSub;
@@ -224,8 +190,8 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
   const int b0 = bg * BT * 16;                   // first sequence
   const int tiles = a.n / kTileRows;
 
-  // Item `it`: accumulator column c; row tile r of the workgroup (with the
-  // prelude, pair r) and the lane's first row in it.
+  // Item `it`: accumulator column c; row tile r of the workgroup (or pair r)
+  // and the lane's first row in it.
   struct Item {
     int c, r, row0, acc_r, group, sub;
   };
@@ -233,12 +199,12 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
     Item m;
     const int u = it / kSub;
     m.sub = it % kSub;
-    constexpr int kG = kWide ? (kPrelude ? 2 : 4) : 1;  // groups of an accumulator taken one by one
+    constexpr int kG = kWide ? (kPairs ? 2 : 4) : 1;  // groups of an accumulator taken one by one
     m.group = u % kG;
     m.c = (u / kG) % kTC;
     const int x = u / kG / kTC;
     m.acc_r = x;
-    m.r = kWide && !kPrelude ? 2 * x + (m.group >> 1) : x;
+    m.r = kWide && !kPairs ? 2 * x + (m.group >> 1) : x;
     m.row0 = (kWide ? 8 * (m.group & 1) : 0) + 4 * kblk + m.sub * kRows;
     return m;
   };
@@ -247,9 +213,10 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
   int item_b[kPer];
   bool item_on[kPer];
   float sn[kPer][kRows], cs[kPer][kRows];
-  // residual, or bias of the pair's rows: kept as loaded and converted after
-  // the loop, so that nothing waits for them here
-  uint32_t raw[kPer][kPrelude ? kRows : kRows / 2];
+  // residual, or bias of the pair's rows (or both, the residual last): kept as
+  // loaded and converted after the loop, so that nothing waits for them here
+  constexpr int kHalf = kRows / 2;  // registers of a tile's rows
+  uint32_t raw[kPer][kPairs && kLinear ? 3 * kHalf : (kPairs || kLinear ? 2 * kHalf : kHalf)];
   int pos[kPer];
 #pragma unroll
   for (int t = 0; t < kPer; ++t) {
@@ -264,6 +231,18 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
 #pragma unroll
       for (int j = 0; j < kRows / 2; ++j) raw[t][j] = 0u;
       if (item_on[t]) load_bf16<kRows>(e.residual + static_cast<int64_t>(item_b[t]) * a.n + n, raw[t]);
+    }
+    if constexpr (kLinear) {
+      const int n = 16 * ((kGated ? tile0 >> 1 : tile0) + m.r) + m.row0;
+      item_on[t] = item_on[t] && n < e.features;
+#pragma unroll
+      for (int j = 0; j < (kGated ? 3 : 2) * kHalf; ++j) raw[t][j] = 0u;
+      if (e.bias && item_on[t]) {
+        load_bf16<kRows>(e.bias + n, raw[t]);
+        if constexpr (kGated) load_bf16<kRows>(e.bias + e.features + n, raw[t] + kHalf);
+      }
+      if (e.residual && item_on[t])
+        load_bf16<kRows>(e.residual + static_cast<int64_t>(item_b[t]) * e.features + n, raw[t] + (kGated ? 2 : 1) * kHalf);
     }
   }
 
@@ -286,6 +265,11 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
       const int h = pair / per_head, q = pair - h * per_head;
       const int half = (!e.interleaved && h < e.hq + e.hkv) ? e.rotary_dim / 32 : 0;
       t = h * 2 * per_head + (q < half ? q + (r & 1) * half : 2 * q + (r & 1));
+    }
+    if constexpr (kGated) {
+      // pair p: tile p of the gate rows and tile p of the up rows, tiles / 2 on
+      const int p = t >> 1;
+      t = p < tiles >> 1 ? p + (r & 1) * (tiles >> 1) : tiles;
     }
     return uniform(t);
   };
@@ -555,6 +539,27 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
         store_bf16<kRows>(dst + eA, v[0]);
         store_bf16<kRows>(dst + eB, v[1]);
       }
+    } else if constexpr (kLinear) {
+      const int n = 16 * ((kGated ? tile0 >> 1 : tile0) + m.r) + m.row0;
+      float v[kRows];
+      if constexpr (kGated) {
+        float up[kRows];
+        total(kWide ? m.acc_r : 2 * m.acc_r, m.c, m.group, m.sub, v);
+        total(kWide ? m.acc_r : 2 * m.acc_r + 1, m.c, kWide ? m.group + 2 : 0, m.sub, up);
+#pragma unroll
+        for (int j = 0; j < kRows; ++j)
+          v[j] = activate(v[j] + unpack_bf16(raw[t], j), e.activation) * (up[j] + unpack_bf16(raw[t] + kHalf, j));
+      } else {
+        total(m.acc_r, m.c, m.group, m.sub, v);
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) v[j] = activate(v[j] + unpack_bf16(raw[t], j), e.activation);
+      }
+      // (adding an absent residual's zeros would turn a -0 into a 0)
+      if (e.residual) {
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) v[j] += unpack_bf16(raw[t] + (kGated ? 2 : 1) * kHalf, j);
+      }
+      if (item_on[t]) store_features(e, b * e.features + n, v);
     } else {
       const int tile = tile0 + m.r;
       const int n = 16 * tile + m.row0;
@@ -684,6 +689,50 @@ __global__ __launch_bounds__(kSumThreads) void oproj_sum_kernel(OProjArgs a) {
       store_bf16<4>(a.normed_out + base + n, h);
     }
   }
+}
+
+// The epilogue of a linear product that was split along k, or whose row tiles
+// do not end in pairs: y's splits in order, bias, activation, gate, residual.
+// One thread for four features of a sequence.
+__global__ __launch_bounds__(kLinearThreads) void linear_epilogue(LinearArgs a, const float* __restrict__ y, int splits,
+                                                                  int batch, int gated) {
+  const int per = a.features / 4;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kLinearThreads + threadIdx.x;
+  if (i >= static_cast<int64_t>(batch) * per) return;
+  const int64_t b = i / per;
+  const int n = 4 * static_cast<int>(i - b * per);
+  const int rows = gated ? 2 * a.features : a.features;
+  const int64_t stride = static_cast<int64_t>(batch) * rows;
+  const float* p = y + b * rows + n;
+  uint32_t bias[2] = {0u, 0u}, bias_up[2] = {0u, 0u}, res[2] = {0u, 0u};
+  if (a.bias) {
+    load_bf16<4>(a.bias + n, bias);
+    if (gated) load_bf16<4>(a.bias + a.features + n, bias_up);
+  }
+  if (a.residual) load_bf16<4>(a.residual + b * a.features + n, res);
+  // every split is requested before any is added; those past the last re-read
+  // it and are dropped
+  f32x4 part[kMaxRowsSplits], part_up[kMaxRowsSplits];
+#pragma unroll
+  for (int s = 0; s < kMaxRowsSplits; ++s) {
+    const float* q = p + (s < splits ? s : splits - 1) * stride;
+    part[s] = *reinterpret_cast<const f32x4*>(q);
+    part_up[s] = *reinterpret_cast<const f32x4*>(q + (gated ? a.features : 0));
+  }
+  float v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float g = part[0][j], u = part_up[0][j];
+#pragma unroll
+    for (int s = 1; s < kMaxRowsSplits; ++s) {
+      g += s < splits ? part[s][j] : 0.f;
+      u += s < splits ? part_up[s][j] : 0.f;
+    }
+    v[j] = activate(g + unpack_bf16(bias, j), a.activation);
+    if (gated) v[j] *= u + unpack_bf16(bias_up, j);
+    if (a.residual) v[j] += unpack_bf16(res, j);
+  }
+  store_features(a, b * a.features + n, v);
 }
 
 // One wave per (sequence b, head h) of the projection: h < hq is a q head,
@@ -902,7 +951,7 @@ static constexpr int most_row_tiles() {
 // with 2560 to 10240 rows (190 shapes, up to 16 forms each), the form chosen is
 // on average 0.9% slower than the fastest and at most 8%; without the two
 // rules 2.6% and 37%.
-static RowsPlan search_rows(int batch, int n, int k, int num_cus, bool fusable, int max_splits) {
+static RowsPlan search_rows(int batch, int n, int k, int num_cus, Fusable fusable, int max_splits) {
   const int nbt = (batch + 15) / 16;
   const int tiles = n / kTileRows;
   const int bt_small = nbt <= 2 ? nbt : 4;  // up to 64 sequences: one column group
@@ -915,7 +964,7 @@ static RowsPlan search_rows(int batch, int n, int k, int num_cus, bool fusable, 
     if (nbt > 4 && f.rt == 1) continue;
     const int rows = (tiles + f.rt - 1) / f.rt;
     for (int fused = 0; fused <= 1; ++fused) {
-      if (fused && (!fusable || f.rt % 2)) continue;
+      if (fused && (fusable == Fusable::kNo || (fusable == Fusable::kPairs && f.rt % 2))) continue;
       for (int splits = 1; splits <= (fused ? 1 : max_splits); ++splits) {
         const int64_t wgs = static_cast<int64_t>(cols > 1 ? (rows + 7) / 8 * 8 : rows) * cols * splits;
         // workgroups of one row tile and one column tile: several reside on a
@@ -963,16 +1012,16 @@ static RowsPlan search_rows(int batch, int n, int k, int num_cus, bool fusable, 
 // The search takes about 1 us, a tenth of a small call; a decode loop asks for
 // the same few sizes, so each thread keeps its last ones (a plan follows from
 // the sizes alone).
-RowsPlan plan_rows(int batch, int n, int k, int num_cus, bool fusable, int max_splits) {
+RowsPlan plan_rows(int batch, int n, int k, int num_cus, Fusable fusable, int max_splits) {
   struct Entry {
     int batch, n, k, num_cus, max_splits;
-    bool fusable;
+    Fusable fusable;
     RowsPlan plan;
   };
   constexpr unsigned kEntries = 16;
   static thread_local Entry kept[kEntries];
   Entry& e = kept[(static_cast<unsigned>(batch) * 7u + static_cast<unsigned>(n) / 16u + static_cast<unsigned>(k) / 32u * 3u +
-                   (fusable ? 5u : 0u)) % kEntries];
+                   5u * static_cast<unsigned>(fusable)) % kEntries];
   if (e.batch != batch || e.n != n || e.k != k || e.num_cus != num_cus || e.max_splits != max_splits ||
       e.fusable != fusable || !e.plan.grid)
     e = Entry{batch, n, k, num_cus, max_splits, fusable, search_rows(batch, n, k, num_cus, fusable, max_splits)};
@@ -1019,7 +1068,7 @@ hipError_t launch_rows_any(RowsArgs a, const RowsPlan& p, const Epilogue& e, hip
   a.col_groups = p.col_groups;
   a.splits = p.splits;
   a.split_grid = p.split_grid;
-  constexpr bool kPairs = std::is_same<Epilogue, PreludeArgs>::value;
+  constexpr bool kPairs = std::is_same<Epilogue, PreludeArgs>::value || std::is_same<Epilogue, GatedArgs>::value;
 #define PDA_ROWS(RT, BT, W, DX, KB, WD, SH) \
   if (p.rt == RT && p.bt == BT && p.waves == W && p.wide == WD && p.kb == KB && (p.col_groups > 1) == SH) \
     return launch_rows_as<RT, BT, W, DX, KB, WD, SH, Epilogue>(a, p, e, st);
@@ -1065,6 +1114,18 @@ hipError_t launch_rows_prelude(const RowsArgs& a, const RowsPlan& p, const Prelu
 }
 hipError_t launch_rows_residual(const RowsArgs& a, const RowsPlan& p, const OProjArgs& o, hipStream_t st) {
   return launch_rows_any(a, p, o, st);
+}
+
+hipError_t launch_rows_linear(const RowsArgs& a, const RowsPlan& p, const LinearArgs& e, bool gated, hipStream_t st) {
+  if (gated) return launch_rows_any(a, p, GatedArgs{e}, st);
+  return launch_rows_any(a, p, e, st);
+}
+
+hipError_t launch_linear_epilogue(const LinearArgs& a, const float* y, int splits, int batch, bool gated, hipStream_t st) {
+  const int64_t threads = static_cast<int64_t>(batch) * (a.features / 4);
+  const dim3 grid(static_cast<unsigned>((threads + kLinearThreads - 1) / kLinearThreads));
+  hipLaunchKernelGGL(linear_epilogue, grid, dim3(kLinearThreads), 0, st, a, y, splits, batch, gated ? 1 : 0);
+  return hipGetLastError();
 }
 
 hipError_t launch_prelude_epilogue(const PreludeArgs& a, hipStream_t st) {

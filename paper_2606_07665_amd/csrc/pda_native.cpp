@@ -43,6 +43,10 @@ struct Lib {
   decltype(&pda_pages_update) pages_update = nullptr;
   decltype(&pda_pages_compact) pages_compact = nullptr;
   decltype(&pda_pages_copy) pages_copy = nullptr;
+  decltype(&pda_linear) linear = nullptr;
+  decltype(&pda_moe_route) moe_route = nullptr;
+  decltype(&pda_moe_experts) moe_experts = nullptr;
+  decltype(&pda_block_norm) block_norm = nullptr;
 } g_lib;
 PyObject* g_raw_stream = nullptr;  // torch._C._cuda_getCurrentRawStream
 PyObject* g_device = nullptr;      // torch._C._cuda_getDevice
@@ -52,11 +56,13 @@ struct Checker {
   bool ok = true;
   int device = -1;
 
-  // The tensor if it is a plain one of this dtype and rank, else null.
-  const at::Tensor* take(PyObject* o, at::ScalarType dt, int64_t ndim) {
+  // The tensor if it is a plain one of this dtype and rank, else null; with
+  // `rows` its rows may lie apart.
+  const at::Tensor* take(PyObject* o, at::ScalarType dt, int64_t ndim, bool rows = false) {
     if (!ok || !THPVariable_CheckExact(o)) return reject();
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.defined() || t.dim() != ndim || t.scalar_type() != dt || !t.is_cuda() || !t.is_contiguous()) return reject();
+    if (!t.defined() || t.dim() != ndim || t.scalar_type() != dt || !t.is_cuda()) return reject();
+    if (!t.is_contiguous() && !(rows && t.stride(ndim - 1) == 1 && t.stride(0) >= t.size(1))) return reject();
     const int d = static_cast<int>(t.get_device());
     if (d < 0 || (device >= 0 && d != device)) return reject();
     device = d;
@@ -65,6 +71,13 @@ struct Checker {
   const at::Tensor* reject() {
     ok = false;
     return nullptr;
+  }
+  const at::Tensor* take_or_none(PyObject* o, at::ScalarType dt, int64_t ndim) {
+    return o == Py_None ? nullptr : take(o, dt, ndim);
+  }
+  bool truth(PyObject* o) {
+    if (o != Py_True && o != Py_False) ok = false;
+    return o == Py_True;
   }
   void same(int64_t a, int64_t b) { ok = ok && a == b; }
   int32_t i32(int64_t v) {
@@ -126,6 +139,7 @@ struct Checker {
 };
 
 const at::ScalarType kBf = at::ScalarType::BFloat16, kI32 = at::ScalarType::Int, kU8 = at::ScalarType::Byte;
+const at::ScalarType kF32 = at::ScalarType::Float;
 
 // k_cache, v_cache [N, P, Hkv, D], block_table [B, M], context_lens [B].
 struct Cache {
@@ -515,6 +529,124 @@ PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   });
 }
 
+void* address(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+
+// (x, w_packed, out, bias or None, residual or None, activation, gated, stream)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 8, [&]() -> int {
+    Checker c;
+    const at::Tensor* x = c.take(a[0], kBf, 2);
+    const at::Tensor* w = c.take(a[1], kBf, 2);
+    if (!c.ok || !THPVariable_CheckExact(a[2])) return kDeclined;
+    pda_linear_dims d;
+    d.out_f32 = THPVariable_Unpack(a[2]).scalar_type() == kF32;
+    const at::Tensor* out = c.take(a[2], d.out_f32 ? kF32 : kBf, 2);
+    const at::Tensor* bias = c.take_or_none(a[3], kBf, 1);
+    const at::Tensor* res = c.take_or_none(a[4], kBf, 2);
+    d.activation = c.integer(a[5]);
+    d.gated = c.truth(a[6]);
+    if (!c.ok) return kDeclined;
+    d.batch = c.i32(x->size(0)), d.in_features = c.i32(x->size(1)), d.out_features = c.i32(out->size(1));
+    const int64_t rows = out->size(1) * (d.gated ? 2 : 1);
+    c.same(out->size(0), x->size(0));
+    c.same(w->size(0), rows);
+    c.same(w->size(1), x->size(1));
+    if (bias) c.same(bias->size(0), rows);
+    if (res) c.ok = c.ok && res->sizes() == out->sizes();
+    void* st = c.stream(a[7], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    void *xp = address(x), *wp = address(w), *bp = address(bias), *rp = address(res), *op = address(out);
+    return released([&] { return g_lib.linear(xp, wp, bp, rp, op, &d, st); });
+  });
+}
+
+// (logits, expert_ids, expert_weights, select_bias or None, sigmoid, renormalise, scale, stream)
+PyObject* moe_route(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 8, [&]() -> int {
+    Checker c;
+    const at::Tensor* l = c.take(a[0], kF32, 2, /*rows=*/true);
+    const at::Tensor* ids = c.take(a[1], kI32, 2);
+    const at::Tensor* w = c.take(a[2], kF32, 2);
+    const at::Tensor* bias = c.take_or_none(a[3], kF32, 1);
+    pda_route_dims d;
+    d.sigmoid = c.integer(a[4]);
+    d.renormalise = c.truth(a[5]);
+    d.scale = c.number(a[6]);
+    if (!c.ok) return kDeclined;
+    d.tokens = c.i32(l->size(0)), d.num_experts = c.i32(l->size(1)), d.top_k = c.i32(ids->size(1));
+    d.logit_stride = d.tokens > 1 ? c.i32(l->stride(0)) : d.num_experts;
+    c.same(ids->size(0), l->size(0));
+    c.ok = c.ok && w->sizes() == ids->sizes();
+    if (bias) c.same(bias->size(0), l->size(1));
+    void* st = c.stream(a[7], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    float *lp = static_cast<float*>(address(l)), *bp = static_cast<float*>(address(bias)), *wp = static_cast<float*>(address(w));
+    int32_t* ip = ints(ids);
+    return released([&] { return g_lib.moe_route(lp, bp, ip, wp, &d, st); });
+  });
+}
+
+// (x, expert_ids, expert_weights, w_gate_up, w_down, out, residual or None, activation, stream)
+PyObject* moe_experts(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 9, [&]() -> int {
+    Checker c;
+    const at::Tensor* x = c.take(a[0], kBf, 2);
+    const at::Tensor* ids = c.take(a[1], kI32, 2);
+    const at::Tensor* w = c.take(a[2], kF32, 2);
+    const at::Tensor* gu = c.take(a[3], kBf, 3);
+    const at::Tensor* dn = c.take(a[4], kBf, 3);
+    const at::Tensor* out = c.take(a[5], kBf, 2);
+    const at::Tensor* res = c.take_or_none(a[6], kBf, 2);
+    pda_moe_dims d;
+    d.activation = c.integer(a[7]);
+    if (!c.ok) return kDeclined;
+    d.tokens = c.i32(x->size(0)), d.hidden = c.i32(x->size(1)), d.inter = c.i32(dn->size(2));
+    d.num_experts = c.i32(dn->size(0)), d.top_k = c.i32(ids->size(1));
+    c.same(ids->size(0), x->size(0));
+    c.same(dn->size(1), x->size(1));
+    c.same(gu->size(0), dn->size(0));
+    c.same(gu->size(1), 2 * dn->size(2));
+    c.same(gu->size(2), x->size(1));
+    c.ok = c.ok && w->sizes() == ids->sizes() && out->sizes() == x->sizes() && (!res || res->sizes() == x->sizes());
+    void* st = c.stream(a[8], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    void *xp = address(x), *gp = address(gu), *dp = address(dn), *rp = address(res), *op = address(out);
+    float* wp = static_cast<float*>(address(w));
+    int32_t* ip = ints(ids);
+    return released([&] { return g_lib.moe_experts(xp, ip, wp, gp, dp, rp, op, &d, st); });
+  });
+}
+
+// (y, residual or None, residual_out, normed_out or None, post_w, pre_w, gate or None, scale, weight_offset, eps, stream)
+PyObject* block_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return guarded(nargs, 11, [&]() -> int {
+    Checker c;
+    const at::Tensor* y = c.take(a[0], kBf, 2);
+    const at::Tensor* res = c.take_or_none(a[1], kBf, 2);
+    const at::Tensor* z = c.take(a[2], kBf, 2);
+    const at::Tensor* h = c.take_or_none(a[3], kBf, 2);
+    const at::Tensor* post = c.take_or_none(a[4], kBf, 1);
+    const at::Tensor* pre = c.take_or_none(a[5], kBf, 1);
+    if (!c.ok) return kDeclined;
+    const bool rows = a[6] != Py_None && THPVariable_CheckExact(a[6]) && THPVariable_Unpack(a[6]).dim() == 2;
+    const at::Tensor* gate = c.take_or_none(a[6], kBf, rows ? 2 : 1);
+    pda_block_norm_dims d;
+    d.gate_rows = rows;
+    d.scale = c.number(a[7]), d.weight_offset = c.number(a[8]), d.eps = c.number(a[9]);
+    if (!c.ok || (pre == nullptr) != (h == nullptr)) return kDeclined;
+    d.rows = c.i32(y->size(0)), d.hidden = c.i32(y->size(1));
+    c.ok = c.ok && z->sizes() == y->sizes() && (!res || res->sizes() == y->sizes()) && (!h || h->sizes() == y->sizes()) &&
+           (!gate || !rows || gate->sizes() == y->sizes());
+    for (const at::Tensor* t : {post, pre, rows ? nullptr : gate})
+      if (t) c.same(t->size(0), y->size(1));
+    void* st = c.stream(a[10], /*of_current=*/true);
+    if (!c.ok) return kDeclined;
+    void *yp = address(y), *rp = address(res), *pp = address(post), *np = address(pre), *gp = address(gate);
+    void *zp = address(z), *hp = address(h);
+    return released([&] { return g_lib.block_norm(yp, rp, pp, np, gp, zp, hp, &d, st); });
+  });
+}
+
 // ({name: address}, raw_stream, device): the loaded library's entry points,
 // torch's current raw stream of a device and its current device
 PyObject* init(PyObject*, PyObject* args) {
@@ -538,7 +670,9 @@ PyObject* init(PyObject*, PyObject* args) {
       !set("pda_o_proj_residual_norm", g_lib.o_proj) || !set("paged_decode_attention_sink", g_lib.attention_sink) ||
       !set("paged_decode_attention_kv4", g_lib.attention_kv4) || !set("pda_kv4_append", g_lib.kv4_append) ||
       !set("pda_kv4_read", g_lib.kv4_read) || !set("pda_pages_update", g_lib.pages_update) ||
-      !set("pda_pages_compact", g_lib.pages_compact) || !set("pda_pages_copy", g_lib.pages_copy))
+      !set("pda_pages_compact", g_lib.pages_compact) || !set("pda_pages_copy", g_lib.pages_copy) ||
+      !set("pda_linear", g_lib.linear) || !set("pda_moe_route", g_lib.moe_route) ||
+      !set("pda_moe_experts", g_lib.moe_experts) || !set("pda_block_norm", g_lib.block_norm))
     return nullptr;
   Py_INCREF(raw);
   Py_XDECREF(g_raw_stream);
@@ -552,7 +686,8 @@ PyObject* init(PyObject*, PyObject* args) {
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(attention), FAST(kv_append), FAST(attention_append), FAST(prelude), FAST(o_proj),
                           FAST(attention_sink), FAST(attention_kv4), FAST(kv4_tokens), FAST(pages_update),
-                          FAST(pages_compact), FAST(pages_copy),
+                          FAST(pages_compact), FAST(pages_copy), FAST(linear), FAST(moe_route), FAST(moe_experts),
+                          FAST(block_norm),
                           {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "pda_native", "Native marshalling of the binding's hot calls.", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};

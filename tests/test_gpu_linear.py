@@ -1,0 +1,173 @@
+"""GPU parity of pda_linear against the fp64 oracle, at bounds derived from its roundings."""
+import numpy as np
+import pytest
+import torch
+
+from _ffn import check, f64, gpu, linear_error, values
+from oracle import ffn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lib(gpu_lib):
+    return gpu_lib
+
+
+def build(b, k, n, gated, bias, residual, seed):
+    g = torch.Generator().manual_seed(seed)
+    rows = 2 * n if gated else n
+    x = values(g, b, k)
+    w = values(g, rows, k, std=k ** -0.5)
+    return x, w, values(g, rows, std=0.5) if bias else None, values(g, b, n) if residual else None
+
+
+def run(lib, b, k, n, act="none", gated=False, bias=False, residual=False, f32=False, in_place=False, seed=0):
+    x, w, bi, re = build(b, k, n, gated, bias, residual, seed + 131 * b + k + n)
+    res = gpu(re)
+    out = res if in_place else torch.full((b, n), float("nan"), dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+    got = lib.linear(gpu(x), lib.pack_weights(gpu(w)), out, bias=gpu(bi), residual=res, activation=act, gated=gated)
+    assert got is out
+    torch.cuda.synchronize()
+    none = lambda t: None if t is None else f64(t)
+    ref = ffn.linear(f64(x), f64(w), none(bi), none(re), act, gated)
+    bound = linear_error(f64(x), f64(w), none(bi), none(re), act, gated, ref, f32)
+    check(out, ref, bound, f"linear B={b} K={k} N={n} {act} gated={gated}")
+    return out
+
+
+# every form's batch, features off each tile height, k of one tile and of an odd number of them
+SHAPES = [(1, 32, 16), (1, 4096, 128), (2, 96, 48), (3, 64, 80), (7, 1024, 1040), (16, 2048, 512), (16, 4096, 8192),
+          (17, 992, 336), (31, 512, 2064), (32, 4096, 1024), (33, 640, 272), (48, 2048, 2048), (64, 2048, 128),
+          (64, 4096, 4096), (65, 1024, 528), (96, 512, 1040), (101, 2560, 2064), (128, 1024, 16), (129, 96, 4112),
+          (200, 4096, 1024), (255, 544, 784), (256, 2048, 4096), (256, 32, 16)]
+ids = ["%dx%dx%d" % s for s in SHAPES]
+
+
+@pytest.mark.parametrize("b,k,n", SHAPES, ids=ids)
+def test_plain_product(lib, b, k, n):
+    run(lib, b, k, n)
+
+
+@pytest.mark.parametrize("b,k,n", SHAPES, ids=ids)
+def test_gated_with_everything(lib, b, k, n):
+    run(lib, b, k, n, act="silu", gated=True, bias=True, residual=True)
+
+
+@pytest.mark.parametrize("b,k,n", SHAPES, ids=ids)
+def test_fp32_out_with_bias(lib, b, k, n):
+    run(lib, b, k, n, bias=True, f32=True)
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("b,k,n", [(5, 256, 64), (130, 1024, 528)])
+def test_activations(lib, act, gated, b, k, n):
+    run(lib, b, k, n, act=act, gated=gated, bias=True, residual=not gated)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("b,k,n", [(1, 64, 16), (40, 4096, 1040), (64, 8192, 128), (180, 512, 2064)])
+def test_in_place_residual_gives_the_same_bits(lib, gated, b, k, n):
+    a = run(lib, b, k, n, act="gelu", gated=gated, residual=True)
+    c = run(lib, b, k, n, act="gelu", gated=gated, residual=True, in_place=True)
+    assert torch.equal(a, c)
+
+
+def test_more_features_than_32_bit_offsets_reach(lib):
+    # 262144 features x 65536 of k would be 32 GiB; 262144 x 8224 reaches past 4 GiB of weights
+    k, n = 8224, 262144
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = torch.empty((n, k), dtype=torch.bfloat16, device="cuda").normal_(0, k ** -0.5, generator=g)
+    x = torch.empty((3, k), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    wp = lib.pack_weights(w)
+    out = torch.full((3, n), float("nan"), dtype=torch.float32, device="cuda")
+    lib.linear(x, wp, out)
+    torch.cuda.synchronize()
+    for rows in (slice(0, 64), slice(n // 2 - 32, n // 2 + 32), slice(n - 64, n)):
+        part = f64(w[rows])
+        ref = ffn.linear(f64(x), part)
+        check(f64(out[:, rows]), ref, linear_error(f64(x), part, None, None, "none", False, ref, True), f"rows {rows.start}")
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu", "none"])
+def test_extreme_products(lib, act):
+    # one feature per row of W: products that overflow the exponential, reach infinity, or are NaN
+    k, n = 32, 16
+    xs = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 3.0, -3.0, 9.0, -9.0, 80.0, -80.0, 1e4, -1e4, 1e30, -1e30,
+                       float("inf"), float("-inf"), float("nan")]).to(torch.bfloat16)
+    x = torch.zeros(len(xs), k, dtype=torch.bfloat16)
+    x[:, 5] = xs
+    w = torch.zeros(n, k, dtype=torch.bfloat16)
+    w[:, 5] = 1.0
+    out = torch.empty((len(xs), n), dtype=torch.bfloat16, device="cuda")
+    lib.linear(gpu(x), lib.pack_weights(gpu(w)), out, activation=act)
+    got = f64(out)[:, 3]
+    ref = ffn.activate(f64(xs), act)
+    # |z| 2^-24 of the exponential's argument, up to 88 (beyond, the value is 0 or x), and a bf16 half step
+    fin = np.isfinite(ref)
+    assert np.array_equal(np.isnan(ref), np.isnan(got)) and np.array_equal(ref[~fin & ~np.isnan(ref)], got[~fin & ~np.isnan(ref)])
+    assert (np.abs(got - ref)[fin] <= (2.0 ** -8 + 2.0 ** -17) * np.abs(ref[fin]) + 2.0 ** -126).all(), (got, ref)
+
+
+def test_what_is_not_finite_stays_in_its_row(lib):
+    b, k, n = 70, 256, 64
+    x, w, _, _ = build(b, k, n, False, False, False, 5)
+    wp = lib.pack_weights(gpu(w))
+    clean = lib.linear(gpu(x), wp, torch.empty((b, n), dtype=torch.bfloat16, device="cuda"))
+    x[17, 3], x[69, 255], x[0, 0] = float("nan"), float("inf"), float("-inf")
+    got = lib.linear(gpu(x), wp, torch.empty((b, n), dtype=torch.bfloat16, device="cuda"))
+    rows = [i for i in range(b) if i not in (0, 17, 69)]
+    assert torch.equal(got[rows], clean[rows]) and not torch.isfinite(got[[0, 17, 69]]).any()
+
+
+@pytest.mark.parametrize("b,k,n,gated,f32", [(4, 4096, 128, False, True), (64, 4096, 256, True, False), (12, 512, 4096, False, False)])
+def test_graph_replay(lib, b, k, n, gated, f32):
+    x, w, bi, re = (gpu(t) for t in build(b, k, n, gated, True, True, 7))
+    wp = lib.pack_weights(w)
+    out = torch.empty((b, n), dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+    call = lambda: lib.linear(x, wp, out, bias=bi, residual=re, activation="silu", gated=gated)
+    want = call().clone()
+    s = torch.cuda.Stream()
+    lib.linear_workspace_reserve(lib.linear_dims(b, k, n, "silu", gated, f32), stream=s)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        call()
+    for _ in range(3):
+        out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert torch.equal(call(), want)  # eager, on another stream, between the replays
+
+
+def test_offset_rows_give_the_same_bits(lib):
+    # bias, residual and out need only be 2-byte aligned
+    b, k, n = 9, 512, 80
+    x, w, bi, re = (gpu(t) for t in build(b, k, n, True, True, True, 8))
+    wp = lib.pack_weights(w)
+    want = lib.linear(x, wp, torch.empty_like(re), bias=bi, residual=re, activation="silu", gated=True)
+    buf = torch.empty(3 * (b * n + 2 * n) + 8, dtype=torch.bfloat16, device="cuda")
+    bi2 = buf[1:1 + 2 * n].copy_(bi)
+    re2 = buf[2 * n + 2:2 * n + 2 + b * n].copy_(re.flatten()).view(b, n)
+    out = buf[2 * n + b * n + 3:2 * n + 2 * b * n + 3].view(b, n)
+    assert torch.equal(lib.linear(x, wp, out, bias=bi2, residual=re2, activation="silu", gated=True), want)
+
+
+def test_nothing_else_is_written(lib):
+    b, k, n = 19, 96, 48
+    x, w, _, _ = (gpu(t) for t in build(b, k, n, True, False, False, 9))
+    buf = torch.full((b * n + 512,), 7.0, dtype=torch.bfloat16, device="cuda")
+    lib.linear(x, lib.pack_weights(w), buf[256:256 + b * n].view(b, n), gated=True)
+    torch.cuda.synchronize()
+    assert (buf[:256] == 7).all() and (buf[256 + b * n:] == 7).all()
+
+
+def test_empty_batch(lib):
+    w = lib.pack_weights(torch.zeros((16, 32), dtype=torch.bfloat16, device="cuda"))
+    out = lib.linear(torch.empty((0, 32), dtype=torch.bfloat16, device="cuda"), w,
+                     torch.empty((0, 16), dtype=torch.bfloat16, device="cuda"))
+    assert out.shape == (0, 16)
