@@ -1008,9 +1008,9 @@ def linear(x, w_packed, out, *, bias=None, residual=None, activation="none", gat
     bf = torch.bfloat16
     if out.dtype not in (bf, torch.float32):
         raise TypeError(f"out must be {bf} or {torch.float32}, got {out.dtype}")
-    sz = _validate([("x", x, bf, "B K"), ("out", out, out.dtype, "B N"), ("residual", residual, bf, "B N")])
-    _validate([("x", x, bf, "B K"), ("w_packed", w_packed, bf, "R K"), ("bias", bias, bf, "R")],
-              dict(sz, R=sz["N"] * (2 if gated else 1)))
+    known = dict(R=out.shape[1] * (2 if gated else 1)) if out.dim() == 2 else None
+    sz = _validate([("x", x, bf, "B K"), ("out", out, out.dtype, "B N"), ("residual", residual, bf, "B N"),
+                    ("w_packed", w_packed, bf, "R K"), ("bias", bias, bf, "R")], known)
     dims = linear_dims(sz["B"], sz["K"], sz["N"], activation, gated, out.dtype is torch.float32)
     with _current(x.device):
         _check(load().pda_linear(x.data_ptr(), w_packed.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(),
@@ -1052,11 +1052,10 @@ def moe_route(logits, expert_ids, expert_weights, *, scoring="softmax", renormal
         _check(rc)
     import torch
     f32 = torch.float32
+    if logits.dim() != 2:
+        raise ValueError(f"logits must be [T, E], got shape {tuple(logits.shape)}")
     sz = _validate([("expert_ids", expert_ids, torch.int32, "T J"), ("expert_weights", expert_weights, f32, "T J"),
-                    ("select_bias", select_bias, f32, "E")])
-    if logits.dim() != 2 or logits.shape[0] != sz["T"] or logits.shape[1] != sz.get("E", logits.shape[1]):
-        raise ValueError(f"logits must be [T, E] with T = {sz['T']}" + (f", E = {sz['E']}" if "E" in sz else "") +
-                         f", got shape {tuple(logits.shape)}")
+                    ("select_bias", select_bias, f32, "E")], dict(T=logits.shape[0], E=logits.shape[1]))
     if logits.dtype != f32:
         raise TypeError(f"logits must be {f32}, got {logits.dtype}")
     if logits.device != expert_ids.device:
@@ -1091,10 +1090,10 @@ def moe_experts(x, expert_ids, expert_weights, w_gate_up, w_down, out, *, residu
         _check(rc)
     import torch
     bf = torch.bfloat16
+    known = dict(R=2 * w_down.shape[2]) if w_down.dim() == 3 else None
     sz = _validate([("x", x, bf, "T H"), ("expert_ids", expert_ids, torch.int32, "T J"),
                     ("expert_weights", expert_weights, torch.float32, "T J"), ("w_down", w_down, bf, "E H F"),
-                    ("out", out, bf, "T H"), ("residual", residual, bf, "T H")])
-    _validate([("x", x, bf, "T H"), ("w_gate_up", w_gate_up, bf, "E R H")], dict(sz, R=2 * sz["F"]))
+                    ("w_gate_up", w_gate_up, bf, "E R H"), ("out", out, bf, "T H"), ("residual", residual, bf, "T H")], known)
     dims = moe_dims(sz["T"], sz["H"], sz["F"], sz["E"], sz["J"], activation)
     with _current(x.device):
         _check(load().pda_moe_experts(x.data_ptr(), expert_ids.data_ptr(), expert_weights.data_ptr(), w_gate_up.data_ptr(),
