@@ -843,8 +843,9 @@ int pda_moe_route(const float* logits, const float* select_bias, int32_t* expert
  * Sums are fp32; act(G x) * (U x) is rounded to bf16 between the two products
  * (the matrix cores' operand) and out once.  Only the experts that are asked for are
  * read.  What is not finite in a token reaches that token alone.  Uses the
- * (device, stream) workspace, tokens * top_k * (2 inter + 4 hidden) bytes
- * (pda_moe_workspace_reserve before graph capture).
+ * (device, stream) workspace: tokens * top_k * (2 inter + 4 hidden) bytes, and
+ * up to 32 hidden in place of the 4 but no more than 128 MB for them where the
+ * down products are cut (pda_moe_workspace_reserve before graph capture).
  */
 typedef struct {
   int32_t tokens;        /* 0 .. 256                                               */

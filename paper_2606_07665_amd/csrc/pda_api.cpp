@@ -937,9 +937,11 @@ int check_moe(const pda_moe_dims* dm) {
   return PDA_OK;
 }
 
-// h [pairs, inter] in bf16, then y [pairs, hidden] in fp32.
+// h [pairs, inter] in bf16, then y [splits, pairs, hidden] in fp32.
 int64_t moe_h_bytes(const pda_moe_dims& d) { return align256(int64_t{2} * d.tokens * d.top_k * d.inter); }
-int64_t moe_ws_bytes(const pda_moe_dims& d) { return moe_h_bytes(d) + align256(int64_t{4} * d.tokens * d.top_k * d.hidden); }
+int64_t moe_ws_bytes(const pda_moe_dims& d, int cus) {
+  return moe_h_bytes(d) + align256(4 * pda::moe_most_floats(d.tokens * d.top_k, d.hidden, cus));
+}
 
 // k splits of an output projection: only where the kernel that adds them
 // holds a row of z.
@@ -1912,7 +1914,7 @@ int pda_moe_experts(const void* x, const int32_t* expert_ids, const float* exper
   if ((rc = device_cus(dev, &cus))) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   void* ws = nullptr;
-  const int64_t need = moe_ws_bytes(d);
+  const int64_t need = moe_ws_bytes(d, cus);
   if ((rc = workspace_for(dev, st, need, need, &ws))) return rc;
   pda::ExpertsArgs a;
   a.x = static_cast<const uint16_t*>(x);
@@ -1942,8 +1944,10 @@ int pda_moe_workspace_reserve(const pda_moe_dims* dims, void* stream) {
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  int cus = 0;
+  if ((rc = device_cus(dev, &cus))) return rc;
   void* ptr = nullptr;
-  const int64_t need = moe_ws_bytes(*dims);
+  const int64_t need = moe_ws_bytes(*dims, cus);
   return workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr);
 }
 

@@ -34,10 +34,40 @@ struct ExpertsArgs {
   const uint16_t* residual;  // bf16 [tokens, hidden] or null
   uint16_t* out;             // bf16 [tokens, hidden]
   uint16_t* h;               // bf16 [pairs, inter] scratch
-  float* y;                  // fp32 [pairs, hidden] scratch
+  float* y;                  // fp32 [splits, pairs, hidden] scratch
   int tokens, hidden, inter, experts, top_k, activation;
+  bool weighted_h;           // h carries the pair's weight
+  int splits;                // parts of the down products' k range
 };
 hipError_t launch_experts(const ExpertsArgs& a, int num_cus, hipStream_t st);
+
+// Segments of up to `cols` pairs of one expert: the most that the pairs make.
+constexpr int kMoeCols = 128;
+inline int moe_most_segments(int pairs, int experts, int cols) {
+  const int most = experts < pairs ? experts : pairs;  // experts that any pair may ask for
+  return (pairs + most * (cols - 1)) / cols;
+}
+
+// Parts of the down products' k range: doubled while the workgroups (128 rows
+// of a segment) are fewer than four a CU and a part keeps 20 steps of 64 k.  8
+// experts of 14336, us: 200 tokens to 4096 rows 264, 246, 236 in 1, 2, 4 parts;
+// 33 tokens to 1024 rows 80, 50, 38; 16 experts of 2816, 64 tokens 25, 21.6,
+// 21.6; shorter ranges only lose (32 of 512, 256 tokens: 19, 26, 35).
+constexpr int kMaxMoeSplits = 8;
+inline int moe_splits(int pairs, int experts, int hidden, int inter, int num_cus) {
+  const int64_t workgroups = static_cast<int64_t>(moe_most_segments(pairs, experts, kMoeCols)) * ((hidden + 127) / 128);
+  const int steps = (inter + 63) / 64;
+  int splits = 1;
+  while (splits < kMaxMoeSplits && workgroups * splits < 4 * num_cus && steps / (2 * splits) >= 20) splits *= 2;
+  return splits;
+}
+// Floats of y that moe_splits() asks for, never less for more pairs: several
+// parts are fewer than 8 workgroups a CU, of 128 rows x 128 pairs.
+inline int64_t moe_most_floats(int pairs, int hidden, int num_cus) {
+  const int64_t one = static_cast<int64_t>(pairs) * hidden, bound = int64_t{8} * num_cus * 128 * kMoeCols;
+  const int64_t most = kMaxMoeSplits * one < bound ? kMaxMoeSplits * one : bound;
+  return one > most ? one : most;
+}
 
 constexpr int kMaxNormRows = 1 << 24;
 struct BlockNormArgs {

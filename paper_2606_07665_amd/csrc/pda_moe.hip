@@ -3,12 +3,12 @@
 //   out_t = residual_t + sum_j w_tj D_e (act(G_e x_t) * (U_e x_t)),  e = ids_tj.
 //
 // A token's choice of an expert is a pair.  A segment is up to 16 BT pairs of
-// one expert, the columns of its matrix products; the first kernel takes each
-// segment through a few row tiles of gate and up weights, the second through
-// row tiles of the down weights, and a third adds a token's pairs in order.
+// one expert, the columns of its matrix products.  The first kernel takes each
+// segment through the gate and up weights; then one kernel adds up the down
+// products of a token's few pairs, or one takes each segment through the down
+// weights and another adds a token's pairs.
 #include "pda_ffn.h"
 
-#include <atomic>
 #include <type_traits>
 
 #include "pda_device.h"
@@ -17,42 +17,69 @@
 namespace pda {
 namespace {
 
-// Weights in the packed order of rows_kernel (16 rows x 32 k, 1 KB, straight
-// into matrix-core registers), activations through a ring of two steps of
-// every wave in LDS, and the W waves dealing the 64-k steps among themselves,
-// as there; the rows that a column reads are found by its pair.
 enum class Stage { kGateUp, kDown };
 
-constexpr int kMoeWaves = 8;
-constexpr int kMoeSlots = 2;  // steps in a wave's ring, and steps per block of weights
-__host__ __device__ constexpr int moe_ring_bytes(int bt) { return kMoeWaves * kMoeSlots * bt * 2048; }
-__host__ __device__ constexpr int moe_sum_bytes(int rt, int bt) { return kMoeWaves * rt * bt * 1024; }
-// ids and counts, before the ring is used
-__host__ __device__ constexpr int moe_scratch_bytes() { return (kMaxMoePairs + kMaxExperts) * 4; }
-__host__ __device__ constexpr int moe_lds_bytes(int rt, int bt) {
-  int n = moe_ring_bytes(bt);
-  n = moe_sum_bytes(rt, bt) > n ? moe_sum_bytes(rt, bt) : n;
-  return moe_scratch_bytes() > n ? moe_scratch_bytes() : n;
+constexpr uint32_t kOutside = 0x80000000u;  // past any descriptor: reads zero
+
+// The segment search's ids, counts and list of pairs in LDS.
+constexpr int kScratchBytes = (kMaxMoePairs + kMaxExperts + 2 + 128) * 4;
+
+// The expert of segment `seg`, or -1 if there are fewer segments, and the pairs
+// of its columns: lane l of every wave holds that of column l + 64 i, -1 past
+// the last.  Every workgroup works this out for itself from the ids.
+//
+// Up to 64 pairs: segments go by first pair, in registers.  A wave holds the
+// ids, one a lane, and takes one expert after the other out of the mask of
+// pairs that are left; nothing goes through LDS.
+template <int kCols>
+__device__ __forceinline__ int find_segment_of_few(const ExpertsArgs& a, int seg, int (&cols)[(kCols + 63) / 64]) {
+  const int pairs = a.tokens * a.top_k, lane = threadIdx.x & 63;
+  int id = lane < pairs ? a.ids[lane] : -1;
+  if (id < 0 || id >= a.experts) id = -1;
+  uint64_t left = __ballot(id >= 0);
+  int at = 0;  // segments before
+  while (left) {
+    const int expert = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+    const uint64_t same = __ballot(id == expert);
+    const int n = (__popcll(same) + kCols - 1) / kCols;
+    if (seg < at + n) {
+      const int rank = __popcll(same & ((uint64_t{1} << lane) - 1)) - (seg - at) * kCols;
+      const int count = __popcll(same) - (seg - at) * kCols;
+      // each pair's lane sends its number to the column's; the others to lanes past them, never read
+      const bool sent = id == expert && rank >= 0 && rank < kCols;
+      const int got = kCols < 64 ? __builtin_amdgcn_ds_permute(4 * (sent ? rank : 63), lane)
+                                 : __builtin_amdgcn_ds_permute(4 * (sent ? rank : 63 - __popcll(~same & ((uint64_t{1} << lane) - 1))), lane);
+#pragma unroll
+      for (int i = 0; i < (kCols + 63) / 64; ++i) cols[i] = -1;
+      cols[0] = lane < kCols && lane < count ? got : -1;
+      return expert;
+    }
+    at += n;
+    left &= ~same;
+  }
+  return -1;
 }
 
-// The expert of segment `seg` and its columns' pairs, -1 past the last; false
-// if there are fewer segments.  Segments go by expert, then by pair.  Every
-// workgroup works this out for itself from the ids.
-template <int kCols>
-__device__ bool find_segment(const ExpertsArgs& a, int seg, unsigned char* lds, int* found, int* cols) {
+// More: segments go by expert, then by pair, from counts in LDS (the start of
+// `lds`, free again when every wave has passed the next barrier).
+template <int kCols, int W>
+__device__ __forceinline__ int find_segment_of_many(const ExpertsArgs& a, int seg, unsigned char* lds,
+                                                    int (&cols)[(kCols + 63) / 64]) {
   const int pairs = a.tokens * a.top_k;
   int* ids = reinterpret_cast<int*>(lds);
   int* count = ids + kMaxMoePairs;
+  int* found = count + kMaxExperts;
+  int* list = found + 2;
   const int tid = threadIdx.x;
-  for (int e = tid; e < a.experts; e += kMoeWaves * 64) count[e] = 0;
+  for (int e = tid; e < a.experts; e += W * 64) count[e] = 0;
   if (tid == 0) found[0] = -1;
+  if (tid < kCols) list[tid] = -1;
   __syncthreads();
-  for (int p = tid; p < pairs; p += kMoeWaves * 64) {
+  for (int p = tid; p < pairs; p += W * 64) {
     const int id = a.ids[p];
     ids[p] = id;
     if (id >= 0 && id < a.experts) atomicAdd(&count[id], 1);
   }
-  if (tid < kCols) cols[tid] = -1;
   __syncthreads();
   if (tid < 64) {
     // lane l counts the segments of its share of the experts
@@ -80,7 +107,7 @@ __device__ bool find_segment(const ExpertsArgs& a, int seg, unsigned char* lds, 
   }
   __syncthreads();
   const int expert = uniform(found[0]);
-  if (expert < 0) return false;
+  if (expert < 0) return -1;
   if (tid < 64) {
     const int first = uniform(found[1]);
     int seen = 0;
@@ -88,29 +115,76 @@ __device__ bool find_segment(const ExpertsArgs& a, int seg, unsigned char* lds, 
       const bool is = p0 + tid < pairs && ids[p0 + tid] == expert;
       const uint64_t m = __ballot(is);
       const int rank = seen + __popcll(m & ((uint64_t{1} << tid) - 1)) - first;
-      if (is && rank >= 0 && rank < kCols) cols[rank] = p0 + tid;
+      if (is && rank >= 0 && rank < kCols) list[rank] = p0 + tid;
       seen += __popcll(m);
     }
   }
   __syncthreads();
-  return true;
+#pragma unroll
+  for (int i = 0; i < (kCols + 63) / 64; ++i) cols[i] = (tid & 63) + 64 * i < kCols ? list[(tid & 63) + 64 * i] : -1;
+  return expert;
 }
 
-template <Stage kStage, int RT, int BT>
-__global__ __launch_bounds__(kMoeWaves * 64, RT * BT <= 4 ? 4 : 2) void experts_kernel(ExpertsArgs a, int row_groups) {
-  constexpr bool kUp = kStage == Stage::kGateUp;
-  constexpr int W = kMoeWaves, DX = kMoeSlots, KB = kMoeSlots;
-  constexpr int kSlot = BT * 2048, kLx = 2 * BT, kLw = 2 * RT;
-  constexpr uint32_t kOutside = 0x80000000u;  // past any descriptor: reads zero
-  static_assert(!kUp || RT % 2 == 0, "gate and up tiles go in pairs");
-  extern __shared__ __align__(1024) unsigned char lds[];
-  __shared__ int found[2];
-  __shared__ int cols[16 * BT];
+template <int kCols, int W>
+__device__ __forceinline__ int find_segment(const ExpertsArgs& a, int seg, unsigned char* lds, int (&cols)[(kCols + 63) / 64]) {
+  if (a.tokens * a.top_k <= 64) return find_segment_of_few<kCols>(a, seg, cols);
+  return find_segment_of_many<kCols, W>(a, seg, lds, cols);
+}
 
+// The pair of column c (the same for every lane, or not).
+template <int N>
+__device__ __forceinline__ int column(const int (&cols)[N], int c) {
+  int p = __shfl(cols[0], c & 63);
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    const int q = __shfl(cols[i], c & 63);
+    p = c >= 64 * i ? q : p;
+  }
+  return p;
+}
+
+// Weights in the packed order of rows_kernel (16 rows x 32 k, 1 KB, straight
+// into matrix-core registers).  A wave takes two row tiles (a gate and up pair,
+// or two of the down rows) over the whole k range, or with kSplit the waves of
+// a workgroup deal the steps (64 k) of the same two among themselves and add
+// their sums in LDS.  The workgroup's activations, gathered by the columns'
+// pairs, lie in LDS once for all its waves, kChunkBytes of the k range at a
+// time.  Each wave keeps D steps of weights in flight in registers, also while
+// a chunk arrives.  The down products' k range may be cut into a.splits parts,
+// whose sums the combination adds.
+//
+// What bounds it is the weights' way from memory, each of them once for up to
+// 128 tokens of an expert.  A wave of its own row tiles reads without a pause
+// from start to end; the form with the k range dealt over 8 waves and a ring of
+// activations for each, which this replaces, spent 2 us of every workgroup's 5
+// on its ramp and read the activations again for every 32 rows.  Measured
+// (128 experts of 768 x 2048, 8 a token; 64 of 1408, 6 a token; 8 of 14336 x
+// 4096, 2 a token), gate and up, then down, us, before -> now: 16 tokens 87 ->
+// 74, 63 -> 38 (6.4 and 6.2 TB/s); 58 tokens 211 -> 129, 126 -> 68; 200 tokens
+// 682 -> 412, 308 -> 236.
+//
+// BT = 8 column tiles were as fast as 1 and 4 for few columns (a segment's
+// products are compiled for each number of tiles in use) and read an expert of
+// more than 64 tokens once: 200 tokens 412 us, with BT = 4 485.  Two workgroups
+// of 4 waves a CU beat one of 8 with two chunks in LDS (412 and 404 us there,
+// but 35.5 and 41 where 16 experts have 64 tokens); 4 row tiles a wave were no
+// faster.
+constexpr int kMoeWaves = 4;
+
+template <Stage kStage, int BT, int D, bool kSplit, int kChunkBytes, int kWavesPerSimd>
+__global__ __launch_bounds__(kMoeWaves * 64, kWavesPerSimd) void experts_kernel(ExpertsArgs a, int row_groups) {
+  constexpr bool kUp = kStage == Stage::kGateUp;
+  constexpr int W = kMoeWaves, RT = 2;
+  static_assert(kChunkBytes >= kScratchBytes, "the ids fit in a chunk");
+  extern __shared__ __align__(1024) unsigned char lds[];
+
+  // part `sp` of the steps (kDown), row group rg of segment seg
+  const int sp = kUp ? 0 : static_cast<int>(blockIdx.y);
   const int seg = static_cast<int>(blockIdx.x) / row_groups;
   const int rg = static_cast<int>(blockIdx.x) - seg * row_groups;
-  if (!find_segment<16 * BT>(a, seg, lds, found, cols)) return;
-  const int64_t expert = uniform(found[0]);
+  int cols[(16 * BT + 63) / 64];
+  const int64_t expert = uniform(find_segment<16 * BT, W>(a, seg, lds, cols));
+  if (expert < 0) return;
 
   const int lane = threadIdx.x & 63;
   const int wv = uniform(threadIdx.x >> 6);
@@ -118,27 +192,21 @@ __global__ __launch_bounds__(kMoeWaves * 64, RT * BT <= 4 ? 4 : 2) void experts_
   const int k = kUp ? a.hidden : a.inter;
   const int n = kUp ? 2 * a.inter : a.hidden;
   const int kt_count = k / kTileK, tiles = n / kTileRows;
+  const int all_steps = (kt_count + 1) / 2;
+  const int begin = kUp ? 0 : sp * all_steps / a.splits;
+  const int steps = (kUp ? all_steps : (sp + 1) * all_steps / a.splits) - begin;  // of this part
+  const int group = kSplit ? rg : rg * W + wv;  // the wave's row tiles, RT * group on
+  // the wave's steps of the part: the q-th is q * kStride + first
+  constexpr int kStride = kSplit ? W : 1;
+  const int first = kSplit ? wv : 0;
+  const int count = steps > first ? (steps - first + kStride - 1) / kStride : 0;
 
-  // activations: the row of a column is its token's (kUp) or its pair's
-  const int pairs = a.tokens * a.top_k;
-  const __amdgpu_buffer_rsrc_t rx =
-      make_rsrc(kUp ? a.x : a.h, static_cast<uint32_t>(kUp ? a.tokens : pairs) * static_cast<uint32_t>(k) * 2u);
-  const int xpiece = (lane & 7) ^ (lane >> 3);
-  uint32_t xrow[kLx];
-#pragma unroll
-  for (int i = 0; i < kLx; ++i) {
-    const int p = cols[8 * i + (lane >> 3)];
-    const uint32_t row = static_cast<uint32_t>(kUp ? p / a.top_k : p);
-    xrow[i] = p < 0 ? kOutside : row * static_cast<uint32_t>(k) * 2u + xpiece * 16u;
-  }
-  __syncthreads();  // the ring takes the place of the ids
-  unsigned char* ring = lds + wv * (DX * kSlot);
-
+  // weights first: the loads are in flight while the activations come
   const uint16_t* w = kUp ? a.w_gate_up : a.w_down;
   __amdgpu_buffer_rsrc_t rw[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    int t = rg * RT + r;
+    int t = group * RT + r;
     if constexpr (kUp) {
       const int p = t >> 1;
       t = p < tiles >> 1 ? p + (r & 1) * (tiles >> 1) : tiles;
@@ -147,134 +215,314 @@ __global__ __launch_bounds__(kMoeWaves * 64, RT * BT <= 4 ? 4 : 2) void experts_
     rw[r] = make_rsrc(w + (expert * tiles + (t < tiles ? t : 0)) * kt_count * (kTileRows * kTileK),
                       t < tiles ? kt_count * 1024u : 0u);
   }
-  const int steps = ((kt_count + 1) / 2 + W - 1) / W;
-
-  auto issue_x = [&](int slot, int s) __attribute__((always_inline)) {
-    const int k0 = (wv + s * W) * kPairK;
-    const bool in = k0 + 8 * xpiece < k;
+  u32x4 wa[D][RT][2];
+  auto issue_w = [&](int slot, int q) __attribute__((always_inline)) {
+    // (k tiles past the end lie outside; those of the next part are not used)
+    const uint32_t at = static_cast<uint32_t>(begin + q * kStride + first) * 2048u + lane * 16u;
 #pragma unroll
-    for (int i = 0; i < kLx; ++i) {
-      const uint32_t off = in && xrow[i] != kOutside ? xrow[i] + k0 * 2u : kOutside;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rx, (__attribute__((address_space(3))) void*)(ring + slot * kSlot + i * 1024), 16, off, 0, 0, 0);
-    }
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        wa[slot][r][m] = __builtin_amdgcn_raw_buffer_load_b128(rw[r], at + m * 1024u, 0, kCachePolicyNT);
   };
-  u32x4 wa[2][KB][RT][2];
-  auto issue_w = [&](int buf, int blk) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < KB; ++i) {
-      const int kt = 2 * (wv + (blk * KB + i) * W);
-      uint32_t at[2];
+  for (int j = 0; j < D; ++j) issue_w(j, j);
+  __builtin_amdgcn_sched_barrier(0);
+
+  const int pairs = a.tokens * a.top_k;
+  const __amdgpu_buffer_rsrc_t rx =
+      make_rsrc(kUp ? a.x : a.h, static_cast<uint32_t>(kUp ? a.tokens : pairs) * static_cast<uint32_t>(k) * 2u);
+  // activations go into LDS 8 rows x 128 bytes a wave load, lane l fetching
+  // the 16-byte piece (l % 8) ^ (l / 8) of row l / 8: operand reads without
+  // bank conflicts
+  const int xpiece = (lane & 7) ^ (lane >> 3);
+  uint32_t xrow[2 * BT];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) at[j] = kt + j < kt_count ? static_cast<uint32_t>(kt + j) * 1024u + lane * 16u : kOutside;
+  for (int i = 0; i < 2 * BT; ++i) {
+    const int p = column(cols, 8 * i + (lane >> 3));
+    const uint32_t row = static_cast<uint32_t>(kUp ? p / a.top_k : p);
+    xrow[i] = p < 0 ? kOutside : row * static_cast<uint32_t>(k) * 2u + xpiece * 16u;
+  }
+  const int frag0 = (col >> 3) * 1024 + (col & 7) * 128 + ((kblk ^ (col & 7)) * 16);
+
+  // groups of 8 columns in use: pairs come first
+  int used8 = 1;
+#pragma unroll
+  for (int c = 1; c < 2 * BT; ++c) used8 += uniform(column(cols, 8 * c)) >= 0 ? 1 : 0;
+
+  // NT column tiles are in use
+  auto products = [&](auto nt) __attribute__((always_inline)) {
+    constexpr int NT = decltype(nt)::value;
+    constexpr int kSlot = NT * 2048;                                 // a step's activations
+    constexpr int kQ = kChunkBytes / kSlot / (kStride * D) * D;      // steps of a wave in a chunk
+    static_assert(kQ >= D, "a chunk holds every step in flight");
+    f32x4 acc[RT][NT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int c = 0; c < NT; ++c) acc[r][c] = f32x4{};
+    // the chunk from the waves' step q0 on
+    auto issue_chunk = [&](int q0) __attribute__((always_inline)) {
+      const int s0 = q0 * kStride;
+      const int s1 = s0 + kQ * kStride < steps ? s0 + kQ * kStride : steps;
+#pragma unroll
+      for (int i = 0; i < 2 * NT; ++i) {
+        // (columns without a pair keep what the LDS holds: nobody reads their sums)
+        if (i >= used8) break;
+        for (int s = s0 + wv; s < s1; s += W) {
+          const uint32_t k0 = static_cast<uint32_t>(begin + s) * kPairK;
+          const uint32_t off = static_cast<int>(k0) + 8 * xpiece < k && xrow[i] != kOutside ? xrow[i] + k0 * 2u : kOutside;
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(
+              rx, (__attribute__((address_space(3))) void*)(lds + (s - s0) * kSlot + i * 1024), 16, off, 0, 0, 0);
+        }
+      }
+    };
+    __syncthreads();  // the ids are done with
+    issue_chunk(0);
+    __builtin_amdgcn_s_waitcnt(kWaitLoads);
+    __syncthreads();
+    const int all = (steps + kStride - 1) / kStride;  // the most steps of a wave
+    for (int q0 = 0; q0 < all; q0 += kQ) {
+      const int end = q0 + kQ < count ? q0 + kQ : count;
+      const unsigned char* from = lds + first * kSlot;
+      auto step = [&](int j, int q) __attribute__((always_inline)) {
+        const unsigned char* at = from + (q - q0) * (kStride * kSlot);
+        u32x4 xb[NT][2];
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) xb[c][m] = *reinterpret_cast<const u32x4*>(at + c * 2048 + (frag0 ^ (m * 64)));
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+              acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[j][r][m]),
+                                                                  __builtin_bit_cast(bf16x8, xb[c][m]), acc[r][c], 0, 0, 0);
+      };
+      // whole rounds without a branch, so that the waits count the loads of
+      // every step in flight; then the last steps
+      int q = q0;
+      for (; q + D <= end; q += D) {
+#pragma unroll
+        for (int j = 0; j < D; ++j) {
+          step(j, q + j);
+          issue_w(j, q + j + D);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < D; ++j)
+        if (q + j < end) step(j, q + j);
+      if (q0 + kQ >= all) break;
+      __syncthreads();
+      issue_chunk(q0 + kQ);
+      __builtin_amdgcn_s_waitcnt(kWaitLoads);
+      __syncthreads();
+    }
+
+    // a column's pair and the four rows 4 kblk .. of row tile (or pair) r
+    auto emit = [&](int r, int p, f32x4 v, f32x4 up) __attribute__((always_inline)) {
+      if (p < 0) return;
+      if constexpr (kUp) {
+        const float scale = a.weighted_h ? a.weights[p] : 1.f;
+        const int f = 16 * (group * (RT / 2) + r) + 4 * kblk;
+        float h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = scale * activate(v[j], a.activation) * up[j];
+        if (f < a.inter) store_bf16<4>(a.h + static_cast<int64_t>(p) * a.inter + f, h);
+      } else {
+        const int o = 16 * (group * RT + r) + 4 * kblk;
+        if (o < a.hidden) *reinterpret_cast<f32x4*>(a.y + (static_cast<int64_t>(sp) * pairs + p) * a.hidden + o) = v;
+      }
+    };
+    int of[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) of[c] = column(cols, 16 * c + col);
+    constexpr int kR = kUp ? RT / 2 : RT;
+    if constexpr (kSplit) {
+      static_assert(W * RT * NT * 1024 <= kChunkBytes, "the waves' sums fit in a chunk");
+      f32x4* red = reinterpret_cast<f32x4*>(lds);  // [W][RT][NT][64 lanes]
+      __syncthreads();
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-          wa[buf][i][r][m] = __builtin_amdgcn_raw_buffer_load_b128(rw[r], at[m], 0, kCachePolicyNT);
-    }
-  };
-  f32x4 acc[RT][BT];
+        for (int c = 0; c < NT; ++c) red[((wv * RT + r) * NT + c) * 64 + lane] = acc[r][c];
+      __syncthreads();
+      auto total = [&](int r, int c) __attribute__((always_inline)) {
+        f32x4 v = red[(r * NT + c) * 64 + lane];
 #pragma unroll
-  for (int r = 0; r < RT; ++r)
+        for (int i = 1; i < W; ++i) v += red[((i * RT + r) * NT + c) * 64 + lane];
+        return v;
+      };
 #pragma unroll
-    for (int c = 0; c < BT; ++c) acc[r][c] = f32x4{};
-  const int frag0 = (col >> 3) * 1024 + (col & 7) * 128 + ((kblk ^ (col & 7)) * 16);
-  u32x4 xb[BT][2];
-
-  issue_w(0, 0);
-  __builtin_amdgcn_sched_barrier(0);
+      for (int r = 0; r < kR; ++r)
 #pragma unroll
-  for (int s = 0; s < DX; ++s) issue_x(s, s);
-  __builtin_amdgcn_sched_barrier(0);
-
-  auto block = [&](int buf, int blk, auto last) __attribute__((always_inline)) {
-    constexpr bool kLast = decltype(last)::value;
-    if constexpr (!kLast) {
-      issue_w(buf ^ 1, blk + 1);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int j = 0; j < KB; ++j) {
-      if constexpr (kLast) {
-        if (j == 0) __builtin_amdgcn_s_waitcnt(kWaitLoads);
-      } else {
-        // younger than the step's activations: the other step's, and this block's request for weights
-        constexpr int kYounger = (DX - 1) * kLx + KB * kLw;
-        static_assert(kYounger < 64, "vmcnt holds at most 63");
-        __builtin_amdgcn_s_waitcnt(wait_loads(kYounger));
-      }
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int c = 0; c < BT; ++c)
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-          xb[c][m] = *reinterpret_cast<const u32x4*>(ring + j * kSlot + c * 2048 + (frag0 ^ (m * 64)));
-      if constexpr (!kLast) {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the slot's operands are in registers
-        asm volatile("" ::: "memory");
-        issue_x(j, blk * KB + j + DX);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int c = 0; c < BT; ++c)
-#pragma unroll
-          for (int r = 0; r < RT; ++r)
-            acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[buf][j][r][m]),
-                                                                __builtin_bit_cast(bf16x8, xb[c][m]), acc[r][c], 0, 0, 0);
-    }
-  };
-  const int blocks = (steps + KB - 1) / KB;
-  int blk = 0;
-  for (; blk + 2 < blocks; blk += 2) {
-    block(0, blk, std::false_type{});
-    block(1, blk + 1, std::false_type{});
-  }
-  if (blk + 1 < blocks) {
-    block(0, blk, std::false_type{});
-    block(1, blk + 1, std::true_type{});
-  } else {
-    block(0, blk, std::true_type{});
-  }
-
-  // ---- the waves' sums meet in LDS
-  __builtin_amdgcn_s_waitcnt(kWaitLoads);
-  __syncthreads();
-  f32x4* red = reinterpret_cast<f32x4*>(lds);  // [W][RT][BT][64 lanes]
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int c = 0; c < BT; ++c) red[((wv * RT + r) * BT + c) * 64 + lane] = acc[r][c];
-  __syncthreads();
-  auto total = [&](int r, int c) __attribute__((always_inline)) {
-    f32x4 v = red[(r * BT + c) * 64 + lane];
-#pragma unroll
-    for (int i = 1; i < W; ++i) v += red[((i * RT + r) * BT + c) * 64 + lane];
-    return v;
-  };
-  constexpr int kItems = (kUp ? RT / 2 : RT) * BT;
-  for (int it = wv; it < kItems; it += W) {
-    const int r = it / BT, c = it % BT;
-    const int p = cols[16 * c + col];
-    if constexpr (kUp) {
-      const f32x4 g = total(2 * r, c), u = total(2 * r + 1, c);
-      const int f = 16 * (rg * (RT / 2) + r) + 4 * kblk;
-      float v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = activate(g[j], a.activation) * u[j];
-      if (p >= 0 && f < a.inter) store_bf16<4>(a.h + static_cast<int64_t>(p) * a.inter + f, v);
+        for (int c = 0; c < NT; ++c)
+          if ((r * NT + c) % W == wv) {
+            if constexpr (kUp)
+              emit(r, of[c], total(2 * r, c), total(2 * r + 1, c));
+            else
+              emit(r, of[c], total(r, c), f32x4{});
+          }
     } else {
-      const f32x4 v = total(r, c);
-      const int o = 16 * (rg * RT + r) + 4 * kblk;
-      if (p >= 0 && o < a.hidden) *reinterpret_cast<f32x4*>(a.y + static_cast<int64_t>(p) * a.hidden + o) = v;
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+          if constexpr (kUp)
+            emit(r, of[c], acc[2 * r][c], acc[2 * r + 1][c]);
+          else
+            emit(r, of[c], acc[r][c], f32x4{});
+        }
     }
+  };
+  const int used = (used8 + 1) / 2;
+  if constexpr (BT >= 8) {
+    if (used == 8) return products(std::integral_constant<int, 8>{});
+    if (used == 7) return products(std::integral_constant<int, 7>{});
+    if (used == 6) return products(std::integral_constant<int, 6>{});
+    if (used == 5) return products(std::integral_constant<int, 5>{});
   }
+  if constexpr (BT >= 4) {
+    if (used == 4) return products(std::integral_constant<int, 4>{});
+    if (used == 3) return products(std::integral_constant<int, 3>{});
+  }
+  if constexpr (BT >= 2) {
+    if (used == 2) return products(std::integral_constant<int, 2>{});
+  }
+  products(std::integral_constant<int, 1>{});
 }
 
-// A token's pairs in order, weighted, and the residual: four features a thread.
+// The second product of few pairs (up to 64, of up to 8 tokens), whole in one
+// kernel: h carries the pair's weight, the columns are the tokens, and a
+// workgroup adds up every expert's part of 8 rows, which the waves deal among
+// themselves by their (expert, 64 k) steps, a run of them each.  A token that
+// has not chosen an expert reads zeros in its steps (outside the descriptor, no
+// traffic), and takes nothing from their sums: zeros times a weight that is not
+// finite are none.
+//
+// A matrix instruction multiplies both k tiles of a step at once: rows 0-7 of
+// its operand and columns 0-7 of the other hold the first, rows and columns
+// 8-15 the second; of its results the two blocks on the diagonal are the
+// products, and their sum is the step's.  So 8 rows fill it, and twice as many
+// workgroups share the weights than with 16: 2048 rows over 8 experts of 768
+// 7.2 us, with 16 rows 9.2; 4 tokens 22.5 and 28.  The other form takes 8 us
+// and its combination 4 more, 24.3 with 4 tokens, 40.2 here and there with 8.
+template <int W, int D>
+__global__ __launch_bounds__(W * 64, W / 4) void experts_join_kernel(ExpertsArgs a) {
+  __shared__ f32x4 red[W][64];
+  const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+  const int col = lane & 15, kblk = lane >> 4;
+  const int token = col & 7;
+  const int pairs = a.tokens * a.top_k;
+  int id = lane < pairs ? a.ids[lane] : -1;
+  if (id < 0 || id >= a.experts) id = -1;
+  const int kt_count = a.inter / kTileK, steps_each = (kt_count + 1) / 2;
+  const int tile = static_cast<int>(blockIdx.x) >> 1, row8 = (static_cast<int>(blockIdx.x) & 1) * 8;  // rows 8 on or not
+  const int tiles = a.hidden / kTileRows;
+  const int token0 = (lane < pairs ? lane : 0) / a.top_k * a.top_k;  // the first pair of this lane's token
+  // the token's own earlier pairs, and the pairs of the column's token
+  const uint64_t before = ((uint64_t{1} << lane) - 1) & ~((uint64_t{1} << token0) - 1);
+  const uint64_t of_col = token < a.tokens ? ((uint64_t{1} << a.top_k) - 1) << (token * a.top_k) : 0;
+
+  // slots: an expert and one pair of each token that chose it (a second pair
+  // of the same token and expert comes in a slot of its own)
+  auto next_slot = [&](uint64_t& left, int& expert) -> uint64_t {
+    expert = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+    const uint64_t same = __ballot(id == expert) & left;
+    const uint64_t slot = __ballot(((same >> lane) & 1) && (same & before) == 0);
+    left &= ~slot;
+    return slot;
+  };
+  const uint64_t chosen_pairs = __ballot(id >= 0);
+  int slots = 0;
+  for (uint64_t left = chosen_pairs; left; ++slots) {
+    int e;
+    next_slot(left, e);
+  }
+  const int total = slots * steps_each;
+  const int s0 = static_cast<int>(static_cast<int64_t>(total) * wv / W);
+  const int s1 = static_cast<int>(static_cast<int64_t>(total) * (wv + 1) / W);
+
+  const __amdgpu_buffer_rsrc_t rh = make_rsrc(a.h, static_cast<uint32_t>(pairs) * static_cast<uint32_t>(a.inter) * 2u);
+  f32x4 acc = f32x4{}, sum = f32x4{};  // of the slot, of those before it
+  // what the wave loads next: the slot's descriptor and row, the step of it
+  uint64_t left = chosen_pairs;
+  int at = s0, slot_end = 0;
+  __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w_down, 0u);
+  uint32_t row = kOutside;
+  const uint32_t wlane = kblk * 256u + (row8 + (col & 7)) * 16u;
+  u32x4 wa[D], xb[D];
+  auto issue = [&](int j) __attribute__((always_inline)) {
+    while (at >= slot_end && left) {  // on to the slot of step `at`
+      int e;
+      const uint64_t slot = next_slot(left, e);
+      slot_end += steps_each;
+      if (at >= slot_end) continue;
+      const uint64_t mine = slot & of_col;
+      row = mine ? static_cast<uint32_t>(__builtin_ctzll(mine)) * static_cast<uint32_t>(a.inter) * 2u + kblk * 16u : kOutside;
+      rw = make_rsrc(a.w_down + (static_cast<int64_t>(e) * tiles + tile) * kt_count * (kTileRows * kTileK), kt_count * 1024u);
+    }
+    const int kt = 2 * (at - (slot_end - steps_each)) + (col >> 3);
+    const bool in = at < s1 && kt < kt_count;
+    wa[j] = __builtin_amdgcn_raw_buffer_load_b128(rw, in ? kt * 1024u + wlane : kOutside, 0, kCachePolicyNT);
+    xb[j] = __builtin_amdgcn_raw_buffer_load_b128(rh, in && row != kOutside ? row + kt * 64u : kOutside, 0, 0);
+    ++at;
+  };
+#pragma unroll
+  for (int j = 0; j < D; ++j) issue(j);
+  __builtin_amdgcn_sched_barrier(0);
+  // what it multiplies next
+  uint64_t left_now = chosen_pairs;
+  int end_now = 0;
+  bool chosen = false;  // the column's token has chosen the slot's expert
+  auto join = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] = chosen ? sum[q] + acc[q] : sum[q];
+    acc = f32x4{};
+  };
+  for (int s = s0; s < s1; s += D) {
+#pragma unroll
+    for (int j = 0; j < D; ++j) {
+      if (s + j >= end_now) {
+        join();
+        while (s + j >= end_now && left_now) {
+          int e;
+          chosen = (next_slot(left_now, e) & of_col) != 0;
+          end_now += steps_each;
+        }
+      }
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[j]), __builtin_bit_cast(bf16x8, xb[j]), acc,
+                                                    0, 0, 0);
+      issue(j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  join();
+  red[wv][lane] = sum;
+  __syncthreads();
+  if (wv != 0) return;
+  f32x4 all = red[0][lane];
+#pragma unroll
+  for (int i = 1; i < W; ++i) all += red[i][lane];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) all[q] += __shfl_xor(all[q], 40);  // the other block: column + 8, rows + 8
+  if (col >= 8 || kblk >= 2 || token >= a.tokens) return;
+  const int64_t out = static_cast<int64_t>(token) * a.hidden + 16 * tile + row8 + 4 * kblk;
+  float v[4] = {all[0], all[1], all[2], all[3]};
+  if (a.residual) {
+    uint32_t res[2];
+    load_bf16<4>(a.residual + out, res);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += unpack_bf16(res, j);
+  }
+  store_bf16<4>(a.out + out, v);
+}
+
+// A token's pairs in order, each the sum of its parts, weighted, and the
+// residual: four features a thread.
 __global__ __launch_bounds__(256) void combine_kernel(ExpertsArgs a) {
   const int per = a.hidden / 4;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
@@ -292,52 +540,54 @@ __global__ __launch_bounds__(256) void combine_kernel(ExpertsArgs a) {
     const int id = a.ids[p];
     if (id < 0 || id >= a.experts) continue;
     const float w = a.weights[p];
-    const f32x4 y = *reinterpret_cast<const f32x4*>(a.y + static_cast<int64_t>(p) * a.hidden + n);
+    const float* part = a.y + static_cast<int64_t>(p) * a.hidden + n;
+    f32x4 y = *reinterpret_cast<const f32x4*>(part);
+    for (int i = 1; i < a.splits; ++i)
+      y += *reinterpret_cast<const f32x4*>(part + static_cast<int64_t>(i) * a.tokens * a.top_k * a.hidden);
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] += w * y[q];
   }
   store_bf16<4>(a.out + o, v);
 }
 
-template <Stage kStage, int RT, int BT>
+template <Stage kStage, int BT, int D, bool kSplit, int kChunkBytes, int kWavesPerSimd>
 hipError_t experts_as(const ExpertsArgs& a, hipStream_t st) {
-  constexpr int lds = moe_lds_bytes(RT, BT);
-  auto* fn = &experts_kernel<kStage, RT, BT>;
-  if constexpr (lds > 64 * 1024) {
-    // the dynamic-LDS limit is raised once per device (bit = device ordinal)
-    static std::atomic<uint64_t> attr_set{0};
-    int dev = 0;
-    hipError_t err = hipGetDevice(&dev);
-    if (err != hipSuccess) return err;
-    const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
-    if (!bit || !(attr_set.load() & bit)) {
-      err = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-      if (err != hipSuccess) return err;
-      attr_set.fetch_or(bit);
-    }
-  }
-  const int pairs = a.tokens * a.top_k;
-  const int most = a.experts < pairs ? a.experts : pairs;  // experts that any pair may ask for
-  constexpr int kCols = 16 * BT;
-  const int segs = (pairs + most * (kCols - 1)) / kCols;
+  auto* fn = &experts_kernel<kStage, BT, D, kSplit, kChunkBytes, kWavesPerSimd>;
+  static_assert(kChunkBytes <= 64 * 1024, "within the default limit of dynamic LDS");
+  constexpr int kEach = 2 * (kSplit ? 1 : kMoeWaves);
   const int tiles = (kStage == Stage::kGateUp ? 2 * a.inter : a.hidden) / kTileRows;
-  const int row_groups = (tiles + RT - 1) / RT;
-  hipLaunchKernelGGL(fn, dim3(static_cast<unsigned>(segs) * row_groups), dim3(kMoeWaves * 64), lds, st, a, row_groups);
+  const int row_groups = (tiles + kEach - 1) / kEach;
+  const dim3 grid(static_cast<unsigned>(moe_most_segments(a.tokens * a.top_k, a.experts, 16 * BT)) * row_groups,
+                  kStage == Stage::kDown ? a.splits : 1);
+  hipLaunchKernelGGL(fn, grid, dim3(kMoeWaves * 64), kChunkBytes, st, a, row_groups);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_experts(const ExpertsArgs& a, int num_cus, hipStream_t st) {
-  (void)num_cus;
-  hipError_t e;
-  if (a.tokens <= 16) {
-    if ((e = experts_as<Stage::kGateUp, 2, 1>(a, st)) != hipSuccess) return e;
-    if ((e = experts_as<Stage::kDown, 2, 1>(a, st)) != hipSuccess) return e;
-  } else {
-    if ((e = experts_as<Stage::kGateUp, 2, 4>(a, st)) != hipSuccess) return e;
-    if ((e = experts_as<Stage::kDown, 2, 4>(a, st)) != hipSuccess) return e;
+hipError_t launch_experts(const ExpertsArgs& args, int num_cus, hipStream_t st) {
+  ExpertsArgs a = args;
+  const int pairs = a.tokens * a.top_k;
+  a.splits = moe_splits(pairs, a.experts, a.hidden, a.inter, num_cus);
+  a.weighted_h = a.tokens <= 8 && pairs <= 64;
+  // Where the pairs' gate and up tiles make fewer waves than two workgroups of
+  // four a CU have, the waves of a workgroup share each pair of tiles: 1
+  // token over 128 experts of 768 11.7 us (15.5 with a wave for each), 32 of
+  // 352 5.7 (9.7); 4 tokens over 128 36.7 (38.6), 8 over 64 of 1408 69 (68).
+  // Columns past 8 double the activations that a pair of tiles needs: then only
+  // a quarter as many waves (16 tokens over 16 experts 21.2, 19.3; over 8 of
+  // 352 6.3, 11).
+  const int64_t waves = static_cast<int64_t>(moe_most_segments(pairs, a.experts, 16)) * (a.inter / kTileRows);
+  hipError_t e = a.tokens <= 16 && waves <= int64_t{a.tokens <= 8 ? 8 : 2} * num_cus ? experts_as<Stage::kGateUp, 1, 2, true, 32 * 1024, 4>(a, st)
+                                                 : experts_as<Stage::kGateUp, 8, 4, false, 64 * 1024, 2>(a, st);
+  if (e != hipSuccess) return e;
+  if (a.weighted_h) {
+    constexpr int kJoinWaves = 8;
+    hipLaunchKernelGGL((experts_join_kernel<kJoinWaves, 4>), dim3(static_cast<unsigned>(a.hidden / 8)), dim3(kJoinWaves * 64), 0,
+                       st, a);
+    return hipGetLastError();
   }
+  if ((e = experts_as<Stage::kDown, 8, 4, false, 64 * 1024, 2>(a, st)) != hipSuccess) return e;
   const int64_t threads = static_cast<int64_t>(a.tokens) * (a.hidden / 4);
   hipLaunchKernelGGL(combine_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, a);
   return hipGetLastError();

@@ -170,7 +170,7 @@ def test_activations_without_residual(lib, act, t):
     check_experts(lib, build(t, 128, 96, 8, 2, seed=t, residual=False), act, what=act)
 
 
-@pytest.mark.parametrize("t,e,k", [(1, 3, 3), (16, 2, 4), (40, 3, 8), (90, 2, 2), (256, 1, 16)])
+@pytest.mark.parametrize("t,e,k", [(1, 3, 3), (3, 1, 16), (4, 2, 16), (16, 2, 4), (40, 3, 8), (64, 1, 1), (21, 2, 3), (90, 2, 2), (256, 1, 16)])
 def test_the_same_expert_twice_counts_twice(lib, t, e, k):
     check_experts(lib, build(t, 128, 64, e, k, seed=t + k, distinct=False), what="repeated")
 
@@ -226,6 +226,19 @@ def test_weights_of_experts_that_are_not_asked_for_do_not_matter(lib, t):
     want = call(lib, s)
     s["up"][7], s["down"][7] = float("nan"), float("inf")
     assert torch.equal(call(lib, s), want)
+
+
+@pytest.mark.parametrize("t", [6, 16, 45, 150])
+def test_weights_that_are_not_finite_reach_the_tokens_that_chose_them(lib, t):
+    s = build(t, 128, 96, 8, 2, seed=t)
+    s["ids"][s["ids"] == 5] = 6
+    s["ids"][1, 0], s["ids"][t - 1, 1] = 5, 5
+    want = call(lib, s)
+    s["down"][5] = float("nan")
+    s["up"][5, 7] = float("inf")
+    got = call(lib, s)
+    rows = [i for i in range(t) if i not in (1, t - 1)]
+    assert torch.equal(got[rows], want[rows]) and torch.isnan(got[[1, t - 1]]).all()
 
 
 @pytest.mark.parametrize("t,k", [(3, 2), (40, 4), (130, 8)])
