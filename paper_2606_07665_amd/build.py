@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "libpda.so")
 NATIVE_PATH = os.path.join(LIB_DIR, "pda_native.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("pda_kernels.hip", "pda_kv4.hip", "pda_pages.hip", "pda_append.hip", "pda_gemv.hip", "pda_ffn.hip", "pda_moe.hip", "pda_probe.hip", "pda_scratch.hip", "pda_api.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("pda_kernels.hip", "pda_kv4.hip", "pda_pages.hip", "pda_append.hip", "pda_gemv.hip", "pda_linear.hip", "pda_ffn.hip", "pda_moe.hip", "pda_probe.hip", "pda_scratch.hip", "pda_api.cpp")]
 NATIVE_SOURCE = os.path.join(CSRC, "pda_native.cpp")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")

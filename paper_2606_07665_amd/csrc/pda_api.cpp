@@ -908,12 +908,11 @@ int check_linear(const pda_linear_dims* dm) {
 int linear_rows(const pda_linear_dims& d) { return d.gated ? 2 * d.out_features : d.out_features; }
 
 pda::RowsPlan linear_plan(const pda_linear_dims& d, int cus) {
-  return pda::plan_rows(d.batch, linear_rows(d), d.in_features, cus, d.gated ? pda::Fusable::kPairs : pda::Fusable::kAny,
-                        pda::kMaxRowsSplits);
+  return pda::plan_linear(d.batch, linear_rows(d), d.in_features, cus, d.gated != 0);
 }
 
 int64_t linear_ws_bytes(const pda_linear_dims& d, int cus) {
-  return align256(pda::rows_most_floats(d.batch, linear_rows(d), cus, pda::kMaxRowsSplits) * 4);
+  return align256(pda::linear_most_floats(d.batch, linear_rows(d), cus) * 4);
 }
 
 int check_moe(const pda_moe_dims* dm) {
@@ -1807,10 +1806,7 @@ int pda_linear(const void* x, const void* w_packed, const void* bias, const void
   l.features = d.out_features;
   l.activation = d.activation;
   l.f32 = d.out_f32;
-  e = plan.fused ? pda::launch_rows_linear(g, plan, l, d.gated != 0, st) : pda::launch_rows(g, plan, st);
-  if (e != hipSuccess) return hip_fail(e, "linear kernel launch");
-  if (!plan.fused && (e = pda::launch_linear_epilogue(l, g.y, plan.splits, d.batch, d.gated != 0, st)) != hipSuccess)
-    return hip_fail(e, "linear epilogue launch");
+  if ((e = pda::launch_linear(g, plan, l, d.gated != 0, st)) != hipSuccess) return hip_fail(e, "linear kernel launch");
   return PDA_OK;
 }
 

@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "pda.h"
+#include "pda_gemv.h"
 
 namespace pda {
 namespace {
@@ -56,6 +57,15 @@ __device__ __forceinline__ void store_bf16(uint16_t* p, const float (&v)[N]) {
   for (int j = 0; j < N / 2; ++j)
     w[j] = f32_to_bf16(v[2 * j]) | (static_cast<uint32_t>(f32_to_bf16(v[2 * j + 1])) << 16);
   __builtin_memcpy(p, w, 2 * N);
+}
+
+// Four (or two) consecutive features of a linear product, from element `at` on.
+template <int N>
+__device__ __forceinline__ void store_features(const LinearArgs& e, int64_t at, const float (&v)[N]) {
+  if (e.f32)
+    __builtin_memcpy(static_cast<float*>(e.out) + at, v, 4 * N);
+  else
+    store_bf16<N>(static_cast<uint16_t*>(e.out) + at, v);
 }
 
 // The activations of a feed-forward layer: silu(x) = x / (1 + exp(-x)), gelu(x)

@@ -29,6 +29,7 @@ struct RowsPlan {
   int split_grid;  // workgroups of one split
   int grid;
   int ss_parts;    // partial sums of z^2 per row tile and sequence (o_proj)
+  bool stream;     // a linear product by linear_stream_kernel instead
 };
 constexpr int kMaxRowsSplits = 4;
 
@@ -124,6 +125,13 @@ struct RowsArgs {
   int row_groups, col_groups;
   int splits, split_grid;
 };
+
+// A linear product of any form: its plan, the most floats of y that the plans of
+// its batch and every smaller one have, and its launches.
+constexpr int kMaxStreamSplits = 8;
+RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated);
+int64_t linear_most_floats(int batch, int rows, int num_cus);
+hipError_t launch_linear(const RowsArgs& a, const RowsPlan& p, const LinearArgs& e, bool gated, hipStream_t st);
 
 hipError_t launch_pack(const uint16_t* w, uint16_t* wp, int n, int k, hipStream_t st);
 // y only

@@ -95,15 +95,6 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const uint16_t* __re
 // of the workgroup takes the same number of blocks with fixed wait counts.
 struct NoEpilogue {};
 
-// Four (or two) consecutive features of a linear product, from element `at` on.
-template <int N>
-__device__ __forceinline__ void store_features(const LinearArgs& e, int64_t at, const float (&v)[N]) {
-  if (e.f32)
-    __builtin_memcpy(static_cast<float*>(e.out) + at, v, 4 * N);
-  else
-    store_bf16<N>(static_cast<uint16_t*>(e.out) + at, v);
-}
-
 // waves per SIMD the register budget is set for
 constexpr int rows_min_waves(int rt, int bt, int w, int kb) { return w > 4 ? (rt * bt * kb <= 4 ? 4 : 2) : 1; }
 __host__ __device__ constexpr int rows_lds_bytes(int rt, int bt, int w, int dx) {
@@ -710,26 +701,30 @@ __global__ __launch_bounds__(kLinearThreads) void linear_epilogue(LinearArgs a, 
     if (gated) load_bf16<4>(a.bias + a.features + n, bias_up);
   }
   if (a.residual) load_bf16<4>(a.residual + b * a.features + n, res);
-  // every split is requested before any is added; those past the last re-read
+  // four splits are requested before any is added; those past the last re-read
   // it and are dropped
-  f32x4 part[kMaxRowsSplits], part_up[kMaxRowsSplits];
+  float g[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < splits; s0 += 4) {
+    f32x4 part[4], part_up[4];
 #pragma unroll
-  for (int s = 0; s < kMaxRowsSplits; ++s) {
-    const float* q = p + (s < splits ? s : splits - 1) * stride;
-    part[s] = *reinterpret_cast<const f32x4*>(q);
-    part_up[s] = *reinterpret_cast<const f32x4*>(q + (gated ? a.features : 0));
+    for (int s = 0; s < 4; ++s) {
+      const float* q = p + (s0 + s < splits ? s0 + s : splits - 1) * stride;
+      part[s] = *reinterpret_cast<const f32x4*>(q);
+      part_up[s] = *reinterpret_cast<const f32x4*>(q + (gated ? a.features : 0));
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        g[j] += s0 + s < splits ? part[s][j] : 0.f;
+        u[j] += s0 + s < splits ? part_up[s][j] : 0.f;
+      }
   }
   float v[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    float g = part[0][j], u = part_up[0][j];
-#pragma unroll
-    for (int s = 1; s < kMaxRowsSplits; ++s) {
-      g += s < splits ? part[s][j] : 0.f;
-      u += s < splits ? part_up[s][j] : 0.f;
-    }
-    v[j] = activate(g + unpack_bf16(bias, j), a.activation);
-    if (gated) v[j] *= u + unpack_bf16(bias_up, j);
+    v[j] = activate(g[j] + unpack_bf16(bias, j), a.activation);
+    if (gated) v[j] *= u[j] + unpack_bf16(bias_up, j);
     if (a.residual) v[j] += unpack_bf16(res, j);
   }
   store_features(a, b * a.features + n, v);

@@ -1,0 +1,311 @@
+// Linear products of more than 64 sequences with many output features, for
+// MI355X (gfx950, CDNA4, wave64), and the plan of every linear product.
+#include <atomic>
+#include <type_traits>
+
+#include "pda_device.h"
+#include "pda_gemv.h"
+
+namespace pda {
+namespace {
+
+constexpr uint32_t kOutside = 0x80000000u;  // past any descriptor: reads zero
+
+// y = x W^T over a packed W (16 rows x 32 k, 1 KB, straight into matrix-core
+// registers), with the whole epilogue, or one of a.splits parts of the k range.
+// A wave takes two row tiles (with a gate a pair) and all column tiles, NT of
+// them, over the part; the workgroup's activations lie in LDS once for its W
+// waves, kQ steps (64 k) at a time in two places, so that the next ones arrive
+// while the waves multiply.  Each wave keeps D steps of weights in flight.
+//
+// rows_kernel, whose waves deal the k range among themselves, reads 64 rows of
+// activations for every 128 rows of weights or fewer, and its waves' sums bound
+// its tiles; here every activation in LDS meets all of a workgroup's rows, and a
+// workgroup reads all sequences once.  What bounds this form is the CU: operand
+// reads of LDS (NT KB for every 2 KB of weights) and matrix instructions take
+// about 0.1 us a step and column tile for 256 rows and overlap little, so with
+// few row tiles rows_kernel, which needs no parts of k, stays ahead.  us a
+// product, rows_kernel -> here (5120 -> 20480, 101 sequences: 75.0 -> 54.1; 256:
+// 113.5 -> 97; 8192 -> 16384, 70: 74.3 -> 63.5, 128: 76.5 -> 73.8, 254: 113.4 ->
+// 96.8; 5120 -> 2 x 13824 gated, 70: 83.7 -> 65.0, 158: 108.5 -> 80.5; 14336 ->
+// 4096, 200: 53 -> 78; 4096 -> 14336, 67: 36.9 -> 31.2, 125: 40.3 -> 41.6).
+//
+// Each row group starts its part of the k range at a place of its own: rows of
+// 16 or 32 KB otherwise meet in the same channels (80 x 8192 -> 8192 39.6 ->
+// 34.5 us; no change elsewhere).  Four row tiles a wave halve the LDS reads, but
+// their sums and operands go past the 256 plain registers (101 sequences 46 us
+// as before, 200 twice as long).
+template <bool kGated, int RT, int NT, int W, int D, int kQ, int kWavesPerSimd>
+__global__ __launch_bounds__(W * 64, kWavesPerSimd) void linear_stream_kernel(RowsArgs a, LinearArgs e) {
+  constexpr int kSlot = NT * 2048;  // a step's activations
+  constexpr int kChunk = kQ * kSlot;
+  static_assert(D % kQ == 0, "a round is whole chunks");
+  extern __shared__ __align__(1024) unsigned char lds[];
+
+  // part `sp` of the steps, row group rg: parts go to the XCDs by turns, so that
+  // their activations are in few L2s
+  const int sp = static_cast<int>(blockIdx.x) % a.splits;
+  const int rg = static_cast<int>(blockIdx.x) / a.splits;
+  const int lane = threadIdx.x & 63;
+  const int wv = uniform(threadIdx.x >> 6);
+  const int col = lane & 15, kblk = lane >> 4;
+  const int kt_count = a.k / kTileK, tiles = a.n / kTileRows;
+  const int all_steps = (kt_count + 1) / 2;
+  const int begin = sp * all_steps / a.splits;
+  const int steps = (sp + 1) * all_steps / a.splits - begin;
+  const int group = rg * W + wv;  // the wave's RT row tiles
+  // the q-th step: each row group starts at a place of its own
+  const int rot = static_cast<int>(static_cast<int64_t>(rg) * steps * a.splits / static_cast<int>(gridDim.x));
+  auto step_of = [&](int q) __attribute__((always_inline)) {
+    const int s = q + rot;
+    return begin + (s < steps ? s : s - steps);
+  };
+
+  // row tile r of the wave: with a gate, even ones are the gate's and odd ones
+  // their up rows, tiles / 2 on
+  auto tile_of = [&](int r) __attribute__((always_inline)) {
+    const int t = group * RT + r;
+    if constexpr (!kGated) return t;
+    return t >> 1 < tiles >> 1 ? (t >> 1) + (r & 1) * (tiles >> 1) : tiles;
+  };
+  __amdgpu_buffer_rsrc_t rw[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int t = uniform(tile_of(r));
+    rw[r] = make_rsrc(a.wp + static_cast<int64_t>(t < tiles ? t : 0) * kt_count * (kTileRows * kTileK),
+                      t < tiles ? kt_count * 1024u : 0u);
+  }
+  u32x4 wa[D][RT][2];
+  auto issue_w = [&](int slot, int q) __attribute__((always_inline)) {
+    // (k tiles past the end lie outside; so do the steps of the next part)
+    const uint32_t at = (q < steps ? static_cast<uint32_t>(step_of(q)) * 2048u : kOutside) + lane * 16u;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        wa[slot][r][m] = __builtin_amdgcn_raw_buffer_load_b128(rw[r], at + m * 1024u, 0, kCachePolicyNT);
+  };
+#pragma unroll
+  for (int j = 0; j < D; ++j) issue_w(j, j);
+  __builtin_amdgcn_sched_barrier(0);
+
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.x, static_cast<uint32_t>(a.batch) * a.k * 2u);
+  const int xpiece = (lane & 7) ^ (lane >> 3);
+  const uint32_t xlane = static_cast<uint32_t>(lane >> 3) * a.k * 2u + xpiece * 16u;
+  const uint32_t xgroup = static_cast<uint32_t>(a.k) * 16u;  // bytes of 8 rows
+  const int groups8 = (a.batch + 7) / 8;
+  // the chunk from step q0 on; its 1 KB pieces (8 rows x 64 k) are dealt to the waves
+  auto issue_chunk = [&](int q0, unsigned char* to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < kQ; ++q) {
+      const uint32_t k0 = static_cast<uint32_t>(step_of(q0 + q)) * kPairK;
+      const bool in = q0 + q < steps && static_cast<int>(k0) + 8 * xpiece < a.k;
+#pragma unroll
+      for (int i = 0; i < (2 * NT + W - 1) / W; ++i) {
+        const int g = i * W + wv;
+        if (g >= 2 * NT) break;
+        const uint32_t off = in && g < groups8 ? xlane + g * xgroup + k0 * 2u : kOutside;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rx, (__attribute__((address_space(3))) void*)(to + q * kSlot + g * 1024), 16, off, 0, 0, 0);
+      }
+    }
+  };
+  const int frag0 = (col >> 3) * 1024 + (col & 7) * 128 + ((kblk ^ (col & 7)) * 16);
+  f32x4 acc[RT][NT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int c = 0; c < NT; ++c) acc[r][c] = f32x4{};
+
+  issue_chunk(0, lds);
+  __builtin_amdgcn_s_waitcnt(kWaitLoads);
+  __syncthreads();
+  // rounds of D steps, kQ to a chunk, the chunks in two places by turns; the
+  // next chunk arrives while the waves multiply
+  constexpr int kPhases = D / kQ;
+  constexpr int kPlaces = kPhases % 2 == 0 ? 1 : 2;  // rounds until the places repeat
+  auto round = [&](int q1, auto odd) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ph = 0; ph < kPhases; ++ph) {
+      const int q0 = q1 + ph * kQ;
+      const int place = (ph + (decltype(odd)::value ? kPhases : 0)) & 1;
+      const unsigned char* from = lds + place * kChunk;
+      const bool more = q0 + kQ < steps;
+      if (more) issue_chunk(q0 + kQ, lds + (place ^ 1) * kChunk);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int q = 0; q < kQ; ++q) {
+        // (steps past the end multiply zeros)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          u32x4 xb[NT];
+#pragma unroll
+          for (int c = 0; c < NT; ++c) xb[c] = *reinterpret_cast<const u32x4*>(from + q * kSlot + c * 2048 + (frag0 ^ (m * 64)));
+#pragma unroll
+          for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+              acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[ph * kQ + q][r][m]),
+                                                                  __builtin_bit_cast(bf16x8, xb[c]), acc[r][c], 0, 0, 0);
+        }
+        issue_w(ph * kQ + q, q0 + q + D);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!more) return false;
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(wait_loads(2 * RT * kQ));  // all but the loads after the chunk's
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+    return true;
+  };
+  for (int q1 = 0;; q1 += kPlaces * D) {
+    if (!round(q1, std::false_type{})) break;
+    if constexpr (kPlaces == 2)
+      if (!round(q1 + D, std::true_type{})) break;
+  }
+
+  if (a.splits > 1) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int t = tile_of(r);
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        const int b = 16 * c + col;
+        if (b < a.batch && t < tiles)
+          *reinterpret_cast<f32x4*>(a.y + (static_cast<int64_t>(sp) * a.batch + b) * a.n + 16 * t + 4 * kblk) = acc[r][c];
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < (kGated ? RT / 2 : RT); ++r) {
+    const int n = 16 * (group * (kGated ? RT / 2 : RT) + r) + 4 * kblk;
+    if (n >= e.features) continue;
+    uint32_t bias[2] = {0u, 0u}, bias_up[2] = {0u, 0u};
+    if (e.bias) {
+      load_bf16<4>(e.bias + n, bias);
+      if constexpr (kGated) load_bf16<4>(e.bias + e.features + n, bias_up);
+    }
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      const int64_t b = 16 * c + col;
+      if (b >= a.batch) continue;
+      float v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = activate(acc[kGated ? 2 * r : r][c][j] + unpack_bf16(bias, j), e.activation);
+        if constexpr (kGated) v[j] *= acc[2 * r + 1][c][j] + unpack_bf16(bias_up, j);
+      }
+      if (e.residual) {
+        uint32_t res[2];
+        load_bf16<4>(e.residual + b * e.features + n, res);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += unpack_bf16(res, j);
+      }
+      store_features(e, b * e.features + n, v);
+    }
+  }
+}
+
+template <bool kGated, int RT, int NT, int W, int D, int kQ, int kWavesPerSimd>
+hipError_t linear_stream_as(const RowsArgs& a, const LinearArgs& e, hipStream_t st) {
+  auto* fn = &linear_stream_kernel<kGated, RT, NT, W, D, kQ, kWavesPerSimd>;
+  constexpr int lds = 2 * kQ * NT * 2048;
+  if constexpr (lds > 64 * 1024) {
+    static std::atomic<uint64_t> attr_set{0};
+    int dev = 0;
+    hipError_t err = hipGetDevice(&dev);
+    if (err != hipSuccess) return err;
+    const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
+    if (!bit || !(attr_set.load() & bit)) {
+      err = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (err != hipSuccess) return err;
+      attr_set.fetch_or(bit);
+    }
+  }
+  const int groups = (a.n / kTileRows + RT * W - 1) / (RT * W);
+  hipLaunchKernelGGL(fn, dim3(static_cast<unsigned>(groups * a.splits)), dim3(W * 64), lds, st, a, e);
+  return hipGetLastError();
+}
+
+// The forms: 4 waves, two workgroups a CU, up to 128 sequences; then 8 waves
+// (more rows share the activations).
+constexpr int stream_waves(int batch) { return batch <= 128 ? 4 : 8; }
+
+template <bool kGated>
+hipError_t linear_stream_any(const RowsArgs& a, const LinearArgs& e, hipStream_t st) {
+  const int nt = (a.batch + 15) / 16;
+  if (nt <= 5) return linear_stream_as<kGated, 2, 5, 4, 4, 2, 2>(a, e, st);
+  if (nt <= 6) return linear_stream_as<kGated, 2, 6, 4, 4, 2, 2>(a, e, st);
+  if (nt <= 7) return linear_stream_as<kGated, 2, 7, 4, 4, 2, 2>(a, e, st);
+  if (nt <= 8) return linear_stream_as<kGated, 2, 8, 4, 4, 2, 2>(a, e, st);
+  if (nt <= 10) return linear_stream_as<kGated, 2, 10, 8, 4, 2, 2>(a, e, st);
+  if (nt <= 13) return linear_stream_as<kGated, 2, 13, 8, 4, 2, 2>(a, e, st);
+  if (nt <= 16) return linear_stream_as<kGated, 2, 16, 8, 2, 2, 2>(a, e, st);
+  return hipErrorInvalidValue;
+}
+
+int stream_groups(int waves, int rows) { return (rows / kTileRows + 2 * waves - 1) / (2 * waves); }
+
+// Parts of the k range: the fewest rounds of workgroups over the CUs for a
+// part's length, less a little for the sums of each.
+int stream_splits(int waves, int rows, int num_cus) {
+  const int groups = stream_groups(waves, rows);
+  int best = 1;
+  double best_cost = 0;
+  for (int s = 1; s <= kMaxStreamSplits; ++s) {
+    const double cost = static_cast<double>((groups * s + num_cus - 1) / num_cus) / s + 0.03 * s;
+    if (s == 1 || cost < best_cost) best = s, best_cost = cost;
+  }
+  return best;
+}
+
+bool stream_form(int batch, int rows, int num_cus) { return batch > 64 && rows >= 64 * num_cus; }
+
+}  // namespace
+
+// rows_kernel below 64 rows a CU, where the streaming form's gain ends (see
+// there), and up to 64 sequences.
+RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated) {
+  if (!stream_form(batch, rows, num_cus))
+    return plan_rows(batch, rows, k, num_cus, gated ? Fusable::kPairs : Fusable::kAny, kMaxRowsSplits);
+  RowsPlan p{};
+  p.stream = true;
+  p.waves = stream_waves(batch);
+  p.rt = 2 * p.waves;
+  p.bt = (batch + 15) / 16;
+  p.row_groups = stream_groups(p.waves, rows);
+  p.col_groups = 1;
+  p.splits = stream_splits(p.waves, rows, num_cus);
+  p.split_grid = p.row_groups;
+  p.grid = p.row_groups * p.splits;
+  p.fused = p.splits == 1;
+  return p;
+}
+
+int64_t linear_most_floats(int batch, int rows, int num_cus) {
+  int64_t most = rows_most_floats(batch < 64 ? batch : 64, rows, num_cus, kMaxRowsSplits);
+  if (batch <= 64) return most;
+  if (!stream_form(batch, rows, num_cus)) return rows_most_floats(batch, rows, num_cus, kMaxRowsSplits);
+  for (const int b : {batch < 128 ? batch : 128, batch}) {
+    const int64_t n = static_cast<int64_t>(stream_splits(stream_waves(b), rows, num_cus)) * b * rows;
+    most = n > most ? n : most;
+  }
+  return most;
+}
+
+hipError_t launch_linear(const RowsArgs& args, const RowsPlan& p, const LinearArgs& e, bool gated, hipStream_t st) {
+  RowsArgs a = args;
+  hipError_t err;
+  if (p.stream) {
+    a.splits = p.splits;
+    err = gated ? linear_stream_any<true>(a, e, st) : linear_stream_any<false>(a, e, st);
+  } else {
+    err = p.fused ? launch_rows_linear(a, p, e, gated, st) : launch_rows(a, p, st);
+  }
+  if (err != hipSuccess || p.fused) return err;
+  return launch_linear_epilogue(e, a.y, p.splits, a.batch, gated, st);
+}
+
+}  // namespace pda

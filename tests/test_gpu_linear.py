@@ -59,6 +59,25 @@ def test_fp32_out_with_bias(lib, b, k, n):
     run(lib, b, k, n, bias=True, f32=True)
 
 
+# many output features and more than 64 sequences: the form whose activations lie in LDS, at each number of
+# column tiles, k of less than a step, off a step, and of fewer steps than parts
+STREAM = [(65, 32, 16384), (80, 96, 16400), (81, 1056, 16384), (96, 160, 20480), (112, 640, 16640), (113, 2080, 16384),
+          (128, 352, 17408), (129, 1024, 16384), (160, 64, 16400), (161, 544, 20480), (208, 1120, 16384), (209, 96, 18432),
+          (256, 992, 16416)]
+
+
+@pytest.mark.parametrize("b,k,n", STREAM, ids=["%dx%dx%d" % s for s in STREAM])
+def test_many_features(lib, b, k, n):
+    assert lib.linear_plan(lib.linear_dims(b, k, n)).row_tiles == (8 if b <= 128 else 16)
+    run(lib, b, k, n, act="gelu_tanh", bias=True)
+    run(lib, b, k, n, f32=True, residual=True)
+
+
+@pytest.mark.parametrize("b,k,n", STREAM, ids=["%dx%dx%d" % s for s in STREAM])
+def test_many_features_gated(lib, b, k, n):
+    run(lib, b, k, (n // 2 + 15) // 16 * 16, act="silu", gated=True, bias=True, residual=True)
+
+
 @pytest.mark.parametrize("act", ["none", "silu", "gelu", "gelu_tanh", "relu"])
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("b,k,n", [(5, 256, 64), (130, 1024, 528)])
@@ -111,8 +130,9 @@ def test_extreme_products(lib, act):
     assert (np.abs(got - ref)[fin] <= (2.0 ** -8 + 2.0 ** -17) * np.abs(ref[fin]) + 2.0 ** -126).all(), (got, ref)
 
 
-def test_what_is_not_finite_stays_in_its_row(lib):
-    b, k, n = 70, 256, 64
+@pytest.mark.parametrize("n", [64, 16384])
+def test_what_is_not_finite_stays_in_its_row(lib, n):
+    b, k = 70, 256
     x, w, _, _ = build(b, k, n, False, False, False, 5)
     wp = lib.pack_weights(gpu(w))
     clean = lib.linear(gpu(x), wp, torch.empty((b, n), dtype=torch.bfloat16, device="cuda"))
@@ -122,7 +142,7 @@ def test_what_is_not_finite_stays_in_its_row(lib):
     assert torch.equal(got[rows], clean[rows]) and not torch.isfinite(got[[0, 17, 69]]).any()
 
 
-@pytest.mark.parametrize("b,k,n,gated,f32", [(4, 4096, 128, False, True), (64, 4096, 256, True, False), (12, 512, 4096, False, False)])
+@pytest.mark.parametrize("b,k,n,gated,f32", [(100, 512, 10240, True, False), (140, 640, 20480, False, True), (4, 4096, 128, False, True), (64, 4096, 256, True, False), (12, 512, 4096, False, False)])
 def test_graph_replay(lib, b, k, n, gated, f32):
     x, w, bi, re = (gpu(t) for t in build(b, k, n, gated, True, True, 7))
     wp = lib.pack_weights(w)
@@ -158,12 +178,12 @@ def test_offset_rows_give_the_same_bits(lib):
 
 
 def test_nothing_else_is_written(lib):
-    b, k, n = 19, 96, 48
-    x, w, _, _ = (gpu(t) for t in build(b, k, n, True, False, False, 9))
-    buf = torch.full((b * n + 512,), 7.0, dtype=torch.bfloat16, device="cuda")
-    lib.linear(x, lib.pack_weights(w), buf[256:256 + b * n].view(b, n), gated=True)
-    torch.cuda.synchronize()
-    assert (buf[:256] == 7).all() and (buf[256 + b * n:] == 7).all()
+    for b, k, n in ((19, 96, 48), (67, 64, 8208), (200, 128, 8192)):
+        x, w, _, _ = (gpu(t) for t in build(b, k, n, True, False, False, 9))
+        buf = torch.full((b * n + 512,), 7.0, dtype=torch.bfloat16, device="cuda")
+        lib.linear(x, lib.pack_weights(w), buf[256:256 + b * n].view(b, n), gated=True)
+        torch.cuda.synchronize()
+        assert (buf[:256] == 7).all() and (buf[256 + b * n:] == 7).all()
 
 
 def test_empty_batch(lib):
