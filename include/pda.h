@@ -840,9 +840,11 @@ int pda_moe_route(const float* logits, const float* select_bias, int32_t* expert
  *   residual        bf16 [tokens, hidden] or NULL.
  *   out             bf16 [tokens, hidden]; may be residual or x itself, otherwise
  *                   it lies apart from everything that is read.
- * Sums are fp32; act(G x) * (U x) is rounded to bf16 between the two products
- * (the matrix cores' operand) and out once.  Only the experts that are asked for are
- * read.  What is not finite in a token reaches that token alone.  Uses the
+ * Sums are fp32; act(G x) * (U x), for up to 8 tokens and 64 pairs with the
+ * weight w_tj, is rounded to bf16 between the two products (the matrix cores'
+ * operand) and out once.  Only the experts that are asked for are
+ * read.  What is not finite in a token reaches that token alone, in an
+ * expert's weights the tokens that chose it.  Uses the
  * (device, stream) workspace: tokens * top_k * (2 inter + 4 hidden) bytes, and
  * up to 32 hidden in place of the 4 but no more than 128 MB for them where the
  * down products are cut (pda_moe_workspace_reserve before graph capture).

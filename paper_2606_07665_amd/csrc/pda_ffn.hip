@@ -118,8 +118,10 @@ __global__ __launch_bounds__(kRouteWaves * 64) void route_kernel(RouteArgs a) {
     if constexpr (kBias) {
       const uint32_t hi = wave_max(static_cast<uint32_t>(best >> 32));
       mine = static_cast<uint32_t>(best >> 32) == hi;
-      const uint32_t lo = wave_max(mine ? static_cast<uint32_t>(best) : 0u);
-      mine = mine && static_cast<uint32_t>(best) == lo;
+      if (__popcll(__ballot(mine)) > 1) {
+        const uint32_t lo = wave_max(mine ? static_cast<uint32_t>(best) : 0u);
+        mine = mine && static_cast<uint32_t>(best) == lo;
+      }
     } else {
       mine = best == wave_max(best);
     }
@@ -259,6 +261,8 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t st) {
+  if (a.hidden <= 512) return block_norm_as<64, 1>(a, st);
+  if (a.hidden <= 1024) return block_norm_as<128, 1>(a, st);
   if (a.hidden <= 2048) return block_norm_as<256, 1>(a, st);
   if (a.hidden <= 4096) return block_norm_as<512, 1>(a, st);
   if (a.hidden <= 8192) return block_norm_as<1024, 1>(a, st);

@@ -156,7 +156,10 @@ def check_experts(lib, s, act="silu", what=""):
 SHAPES = [(1, 32, 32, 1, 1), (1, 256, 96, 8, 2), (1, 2048, 768, 16, 8), (2, 96, 352, 4, 4), (3, 1024, 160, 60, 4),
           (5, 544, 32, 8, 3), (15, 256, 224, 64, 6), (16, 512, 256, 8, 2), (17, 128, 480, 8, 1), (31, 288, 64, 5, 5),
           (33, 512, 96, 32, 8), (61, 320, 352, 16, 6), (64, 256, 512, 4, 2), (65, 256, 96, 2, 1), (100, 160, 288, 3, 2),
-          (129, 256, 64, 16, 4), (200, 512, 128, 8, 2), (256, 128, 96, 1, 1), (256, 64, 32, 200, 16)]
+          (129, 256, 64, 16, 4), (200, 512, 128, 8, 2), (256, 128, 96, 1, 1), (256, 64, 32, 200, 16),
+          # down products over long ranges, cut into 2, 4 and 8 parts, and few pairs in one kernel
+          (20, 64, 2816, 2, 1), (9, 160, 5152, 3, 2), (40, 96, 10272, 3, 2), (8, 96, 5152, 3, 3), (1, 64, 10272, 4, 2),
+          (12, 288, 96, 8, 1), (8, 1056, 352, 64, 8), (7, 128, 96, 1024, 9)]
 
 
 @pytest.mark.parametrize("t,h,f,e,k", SHAPES, ids=["-".join(map(str, s)) for s in SHAPES])
@@ -189,10 +192,11 @@ def test_ids_outside_add_nothing(lib, t):
     assert (call(lib, s) == 0).all()
 
 
-@pytest.mark.parametrize("t", [4, 30, 120])
+@pytest.mark.parametrize("t", [4, 8, 16, 30, 48, 64, 80, 96, 112, 128, 129, 250])
 def test_every_token_on_one_expert(lib, t):
+    # each number of column tiles, and a second segment
     s = build(t, 256, 160, 16, 2, seed=t)
-    s["ids"][:, 0], s["ids"][:, 1] = 11, 15
+    s["ids"][:, 0], s["ids"][:, 1] = 11, torch.arange(t) % 3
     check_experts(lib, s, what="one expert")
 
 
@@ -307,6 +311,40 @@ def test_nothing_else_is_written(lib):
     buf = torch.full((n + 512,), 7.0, dtype=torch.bfloat16, device="cuda")
     call(lib, s, out=buf[256:256 + n].view(21, 96))
     assert (buf[:256] == 7).all() and (buf[256 + n:] == 7).all()
+
+
+@pytest.mark.parametrize("t", [6, 40])
+def test_offset_rows_give_the_same_bits(lib, t):
+    # residual and out need only be 2-byte aligned, ids and weights 4-byte aligned
+    s = build(t, 96, 64, 4, 2, seed=t)
+    up, down = packed(lib, s["up"]), packed(lib, s["down"])
+    want = call(lib, s, up=up, down=down)
+    n = t * 96
+    buf = torch.empty(2 * n + 8, dtype=torch.bfloat16, device="cuda")
+    res, out = buf[1:1 + n].copy_(gpu(s["residual"]).flatten()).view(t, 96), buf[n + 3:2 * n + 3].view(t, 96)
+    ids = torch.empty(2 * t + 1, dtype=torch.int32, device="cuda")[1:].view(t, 2).copy_(s["ids"])
+    w = torch.empty(2 * t + 3, device="cuda")[3:].view(t, 2).copy_(s["weights"])
+    assert torch.equal(lib.moe_experts(gpu(s["x"]), ids, w, up, down, out, residual=res), want)
+
+
+def test_one_reserve_covers_every_call_below(gpu_lib):
+    # captured calls of other sizes fit the workspace that the largest one reserved
+    lib, t, h, f, e, k = gpu_lib, 64, 128, 2816, 4, 2
+    s = build(t, h, f, e, k, seed=5)
+    up, down = packed(lib, s["up"]), packed(lib, s["down"])
+    stream = torch.cuda.Stream()
+    lib.moe_workspace_reserve(lib.moe_dims(t, h, f, e, k), stream=stream)
+    for n, j in ((1, 1), (3, 2), (9, 2), (17, 1), (33, 2), (63, 2), (64, 2)):
+        x, ids, w = gpu(s["x"])[:n], gpu(s["ids"])[:n, :j].contiguous(), gpu(s["weights"])[:n, :j].contiguous()
+        want = lib.moe_experts(x, ids, w, up, down, torch.empty_like(x))
+        out = torch.empty_like(x)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            lib.moe_experts(x, ids, w, up, down, out)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
 
 
 def test_no_tokens(lib):
