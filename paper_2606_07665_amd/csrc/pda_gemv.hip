@@ -1064,6 +1064,7 @@ hipError_t launch_rows_any(RowsArgs a, const RowsPlan& p, const Epilogue& e, hip
   a.splits = p.splits;
   a.split_grid = p.split_grid;
   constexpr bool kPairs = std::is_same<Epilogue, PreludeArgs>::value || std::is_same<Epilogue, GatedArgs>::value;
+  constexpr bool kLinear = std::is_same<Epilogue, LinearArgs>::value || std::is_same<Epilogue, GatedArgs>::value;
 #define PDA_ROWS(RT, BT, W, DX, KB, WD, SH) \
   if (p.rt == RT && p.bt == BT && p.waves == W && p.wide == WD && p.kb == KB && (p.col_groups > 1) == SH) \
     return launch_rows_as<RT, BT, W, DX, KB, WD, SH, Epilogue>(a, p, e, st);
@@ -1075,6 +1076,14 @@ hipError_t launch_rows_any(RowsArgs a, const RowsPlan& p, const Epilogue& e, hip
     PDA_ROWS(1, 4, 8, 2, 4, false, false)
     PDA_ROWS(3, 4, 8, 2, 2, false, false)
     PDA_ROWS(3, 4, 8, 2, 2, false, true)
+  }
+  if constexpr (kLinear) {
+    // few row tiles, several column groups (few_rows_plan)
+    if constexpr (!kPairs) {
+      PDA_ROWS(1, 1, 8, 2, 2, false, true)
+    }
+    PDA_ROWS(2, 1, 8, 2, 2, false, true)
+    PDA_ROWS(2, 2, 8, 2, 2, false, true)
   }
   PDA_ROWS(2, 1, 8, 2, 2, false, false)
   PDA_ROWS(4, 1, 8, 2, 2, false, false)

@@ -261,6 +261,35 @@ int stream_splits(int waves, int rows, int num_cus) {
   return best;
 }
 
+// Products with few output features (a router's) of more than 16 sequences by
+// rows_kernel in small tiles, each column group with workgroups of its own: what
+// bounds them is a workgroup's way through its activations and weights, not the
+// chip, and the forms that take up to 64 sequences together leave most CUs idle.
+// One row and one column tile a workgroup while there is a CU for each, then two
+// row tiles, then two of both, while two such workgroups have a CU.  us a
+// product, the planner's form -> these: 64 sequences, 4096 -> 64 7.9 -> 4.2, 1024
+// -> 256 5.9 -> 3.2, 8192 -> 1024 11.3 -> 8.7, 4096 -> 2048 11.1 -> 7.4; 256, 4096
+// -> 256 10.0 -> 6.1, -> 1024 12.1 -> 9.5; 32, 4096 -> 2048 8.6 -> 6.1; 48, 8192
+// -> 2 x 2048 gated 21.7 -> 15.1.  With more workgroups the planner's forms are
+// level or ahead (256, 4096 -> 2048 12.3, 13.9).
+bool few_rows_plan(int batch, int rows, int num_cus, bool gated, RowsPlan* out) {
+  const int cols = (batch + 15) / 16, tiles = rows / kTileRows;
+  const int64_t ones = static_cast<int64_t>(tiles) * cols, pairs = static_cast<int64_t>((tiles + 1) / 2) * cols;
+  RowsPlan p{};
+  p.rt = !gated && ones <= num_cus ? 1 : 2;
+  p.bt = pairs <= num_cus ? 1 : 2;
+  if (cols <= p.bt || pairs > 2 * num_cus) return false;
+  p.waves = 8;
+  p.kb = 2;
+  p.fused = true;
+  p.row_groups = (tiles + p.rt - 1) / p.rt;
+  p.col_groups = (cols + p.bt - 1) / p.bt;
+  p.splits = 1;
+  p.split_grid = p.grid = (p.row_groups + 7) / 8 * 8 * p.col_groups;
+  *out = p;
+  return true;
+}
+
 bool stream_form(int batch, int rows, int num_cus) { return batch > 64 && rows >= 64 * num_cus; }
 
 }  // namespace
@@ -268,6 +297,8 @@ bool stream_form(int batch, int rows, int num_cus) { return batch > 64 && rows >
 // rows_kernel below 64 rows a CU, where the streaming form's gain ends (see
 // there), and up to 64 sequences.
 RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated) {
+  RowsPlan few;
+  if (few_rows_plan(batch, rows, num_cus, gated, &few)) return few;
   if (!stream_form(batch, rows, num_cus))
     return plan_rows(batch, rows, k, num_cus, gated ? Fusable::kPairs : Fusable::kAny, kMaxRowsSplits);
   RowsPlan p{};
