@@ -48,11 +48,24 @@ inline int moe_most_segments(int pairs, int experts, int cols) {
   return (pairs + most * (cols - 1)) / cols;
 }
 
+// Whether the waves of a workgroup share each pair of row tiles (`tiles` of them
+// an expert) instead of taking one each: where the pairs of tiles of all segments
+// (of up to 32 pairs) are too few to keep the chip's waves busy one by one.  us,
+// a pair of tiles a wave -> shared; gate and up: 1 token over 128 experts of 768
+// 15.5 -> 11.7, 4 tokens 38.6 -> 35.6, 24 tokens of 5 pairs over 8 of 480 14.8 ->
+// 9.2, 200 of 2 over 8 of 512 22.2 -> 10.9, 33 of 2 over 8 of 1024 (4096 features)
+// 35.2 -> 27.6, 93 of 3 over 64 of 384 (1680 workgroups) 23.2 -> 23.6; down: the
+// same 7.0 -> 6.5, 13.0 -> 6.9, 16.7 -> 15.0, 67 tokens of 8 over 32 (2538) 16.7 ->
+// 21.7.
+constexpr int kMoeFewCols = 32;
+inline bool moe_shares_tiles(int tokens, int pairs, int experts, int tiles, int num_cus) {
+  return static_cast<int64_t>(moe_most_segments(pairs, experts, kMoeFewCols)) * tiles <= (tokens <= 8 ? 8 : 5) * num_cus;
+}
+
 // Parts of the down products' k range: doubled while the workgroups (128 rows
-// of a segment) are fewer than four a CU and a part keeps 20 steps of 64 k.  8
-// experts of 14336, us: 200 tokens to 4096 rows 264, 246, 236 in 1, 2, 4 parts;
-// 33 tokens to 1024 rows 80, 50, 38; 16 experts of 2816, 64 tokens 25, 21.6,
-// 21.6; shorter ranges only lose (32 of 512, 256 tokens: 19, 26, 35).
+// of a segment) are fewer than four a CU and a part keeps 20 steps of 64 k: 8
+// experts of 14336, 200 tokens to 4096 rows, 264, 246 and 236 us in 1, 2 and 4
+// parts; shorter ranges only lose (32 of 512, 256 tokens: 19, 26, 35).
 constexpr int kMaxMoeSplits = 8;
 inline int moe_splits(int pairs, int experts, int hidden, int inter, int num_cus) {
   const int64_t workgroups = static_cast<int64_t>(moe_most_segments(pairs, experts, kMoeCols)) * ((hidden + 127) / 128);

@@ -586,18 +586,10 @@ hipError_t experts_as(const ExpertsArgs& a, hipStream_t st) {
 hipError_t launch_experts(const ExpertsArgs& args, int num_cus, hipStream_t st) {
   ExpertsArgs a = args;
   const int pairs = a.tokens * a.top_k;
-  a.splits = moe_splits(pairs, a.experts, a.hidden, a.inter, num_cus);
   a.weighted_h = a.tokens <= 8 && pairs <= 64;
-  // Where the pairs' gate and up tiles make fewer waves than two workgroups of
-  // four a CU have, the waves of a workgroup share each pair of tiles: 1
-  // token over 128 experts of 768 11.7 us (15.5 with a wave for each), 32 of
-  // 352 5.7 (9.7); 4 tokens over 128 36.7 (38.6), 8 over 64 of 1408 69 (68).
-  // Columns past 8 double the activations that a pair of tiles needs: then only
-  // a quarter as many waves (16 tokens over 16 experts 21.2, 19.3; over 8 of
-  // 352 6.3, 11).
-  const int64_t waves = static_cast<int64_t>(moe_most_segments(pairs, a.experts, 16)) * (a.inter / kTileRows);
-  hipError_t e = a.tokens <= 16 && waves <= int64_t{a.tokens <= 8 ? 8 : 2} * num_cus ? experts_as<Stage::kGateUp, 1, 2, true, 32 * 1024, 4>(a, st)
-                                                 : experts_as<Stage::kGateUp, 8, 4, false, 64 * 1024, 2>(a, st);
+  hipError_t e = moe_shares_tiles(a.tokens, pairs, a.experts, a.inter / kTileRows, num_cus)
+                     ? experts_as<Stage::kGateUp, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st)
+                     : experts_as<Stage::kGateUp, kMoeCols / 16, 4, false, 64 * 1024, 2>(a, st);
   if (e != hipSuccess) return e;
   if (a.weighted_h) {
     constexpr int kJoinWaves = 8;
@@ -605,7 +597,14 @@ hipError_t launch_experts(const ExpertsArgs& args, int num_cus, hipStream_t st) 
                        st, a);
     return hipGetLastError();
   }
-  if ((e = experts_as<Stage::kDown, 8, 4, false, 64 * 1024, 2>(a, st)) != hipSuccess) return e;
+  if (moe_shares_tiles(a.tokens, pairs, a.experts, a.hidden / (2 * kTileRows), num_cus)) {
+    a.splits = 1;
+    e = experts_as<Stage::kDown, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st);
+  } else {
+    a.splits = moe_splits(pairs, a.experts, a.hidden, a.inter, num_cus);
+    e = experts_as<Stage::kDown, kMoeCols / 16, 4, false, 64 * 1024, 2>(a, st);
+  }
+  if (e != hipSuccess) return e;
   const int64_t threads = static_cast<int64_t>(a.tokens) * (a.hidden / 4);
   hipLaunchKernelGGL(combine_kernel, dim3(static_cast<unsigned>((threads + kCombineThreads - 1) / kCombineThreads)),
                      dim3(kCombineThreads), 0, st, a);

@@ -157,7 +157,7 @@ SHAPES = [(1, 32, 32, 1, 1), (1, 256, 96, 8, 2), (1, 2048, 768, 16, 8), (2, 96, 
           (5, 544, 32, 8, 3), (15, 256, 224, 64, 6), (16, 512, 256, 8, 2), (17, 128, 480, 8, 1), (31, 288, 64, 5, 5),
           (33, 512, 96, 32, 8), (61, 320, 352, 16, 6), (64, 256, 512, 4, 2), (65, 256, 96, 2, 1), (100, 160, 288, 3, 2),
           (129, 256, 64, 16, 4), (200, 512, 128, 8, 2), (256, 128, 96, 1, 1), (256, 64, 32, 200, 16),
-          # down products over long ranges, cut into 2, 4 and 8 parts, and few pairs in one kernel
+          # down products over long ranges, whose waves share row tiles, and few pairs in one kernel
           (20, 64, 2816, 2, 1), (9, 160, 5152, 3, 2), (40, 96, 10272, 3, 2), (8, 96, 5152, 3, 3), (1, 64, 10272, 4, 2),
           (12, 288, 96, 8, 1), (8, 1056, 352, 64, 8), (7, 128, 96, 1024, 9)]
 
@@ -165,6 +165,34 @@ SHAPES = [(1, 32, 32, 1, 1), (1, 256, 96, 8, 2), (1, 2048, 768, 16, 8), (2, 96, 
 @pytest.mark.parametrize("t,h,f,e,k", SHAPES, ids=["-".join(map(str, s)) for s in SHAPES])
 def test_experts(lib, t, h, f, e, k):
     check_experts(lib, build(t, h, f, e, k, seed=sum((t, h, f, e, k))), what=f"{t} tokens")
+
+
+def reference_on_gpu(s):
+    """As reference(), for the larger shapes: fp64 products of the device, an expert at a time, silu; the
+    bound without the fp32 errors of h, which are far below its rounding."""
+    x, w, ids = s["x"].cuda().double(), s["weights"].cuda().double(), s["ids"].cuda()
+    f = s["down"].shape[2]
+    ref = torch.zeros_like(x) if s["residual"] is None else s["residual"].cuda().double()
+    size, var = ref.abs(), torch.zeros_like(ref)
+    for e in range(s["down"].shape[0]):
+        t, j = torch.nonzero(ids == e, as_tuple=True)
+        up, down = s["up"][e].cuda().double(), s["down"][e].cuda().double()
+        g = x[t] @ up[:f].t()
+        h = g / (1 + torch.exp(-g)) * (x[t] @ up[f:].t())
+        c = w[t, j][:, None]
+        ref.index_add_(0, t, c * (h @ down.t()))
+        size.index_add_(0, t, c * (h.abs() @ down.abs().t()))
+        var.index_add_(0, t, c ** 2 * ((HALF * h / 3 ** 0.5) ** 2 @ (down ** 2).t()))
+    bound = 6 * var.sqrt() + 2 * F32 * (chain(f) + s["ids"].shape[1] + 8) * size
+    return f64(ref), f64(bound + HALF * (ref.abs() + bound)) + TINY
+
+
+# the down products' range cut into 2, 4 and 8 parts; many tokens of one expert
+@pytest.mark.parametrize("t,h,f,e,k", [(100, 4096, 2816, 8, 2), (120, 4096, 5152, 8, 2), (90, 16384, 10272, 1, 1),
+                                       (256, 2048, 1024, 4, 3)])
+def test_experts_of_long_ranges(lib, t, h, f, e, k):
+    s = build(t, h, f, e, k, seed=t)
+    check(call(lib, s), *reference_on_gpu(s), f"{t} tokens")
 
 
 @pytest.mark.parametrize("act", ["none", "silu", "gelu", "gelu_tanh", "relu"])
