@@ -128,7 +128,7 @@ struct RowsArgs {
 
 // A linear product of any form: its plan, the most floats of y that the plans of
 // its batch and every smaller one have, and its launches.
-constexpr int kMaxStreamSplits = 8;
+constexpr int kMaxStreamSplits = 6;
 RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated);
 int64_t linear_most_floats(int batch, int rows, int num_cus);
 hipError_t launch_linear(const RowsArgs& a, const RowsPlan& p, const LinearArgs& e, bool gated, hipStream_t st);

@@ -24,9 +24,9 @@ constexpr uint32_t kOutside = 0x80000000u;  // past any descriptor: reads zero
 // workgroup reads all sequences once.  What bounds this form is the CU: operand
 // reads of LDS (NT KB for every 2 KB of weights) and matrix instructions take
 // about 0.1 us a step and column tile for 256 rows and overlap little, so with
-// few row tiles rows_kernel, which needs no parts of k, stays ahead.  us a
-// product, rows_kernel -> here (5120 -> 20480, 101 sequences: 75.0 -> 54.1; 256:
-// 113.5 -> 97; 8192 -> 16384, 70: 74.3 -> 63.5, 128: 76.5 -> 73.8, 254: 113.4 ->
+// few row tiles rows_kernel, which needs no parts of k, stays ahead (the choice:
+// stream_splits).  us a product, rows_kernel -> here (5120 -> 20480, 101 sequences: 75.0 -> 54.1; 256:
+// 113.5 -> 88; 8192 -> 16384, 70: 74.3 -> 63.5, 128: 76.5 -> 73.8, 254: 113.4 ->
 // 96.8; 5120 -> 2 x 13824 gated, 70: 83.7 -> 65.0, 158: 108.5 -> 80.5; 14336 ->
 // 4096, 200: 53 -> 78; 4096 -> 14336, 67: 36.9 -> 31.2, 125: 40.3 -> 41.6).
 //
@@ -248,17 +248,43 @@ hipError_t linear_stream_any(const RowsArgs& a, const LinearArgs& e, hipStream_t
 
 int stream_groups(int waves, int rows) { return (rows / kTileRows + 2 * waves - 1) / (2 * waves); }
 
-// Parts of the k range: the fewest rounds of workgroups over the CUs for a
-// part's length, less a little for the sums of each.
-int stream_splits(int waves, int rows, int num_cus) {
-  const int groups = stream_groups(waves, rows);
-  int best = 1;
-  double best_cost = 0;
-  for (int s = 1; s <= kMaxStreamSplits; ++s) {
-    const double cost = static_cast<double>((groups * s + num_cus - 1) / num_cus) / s + 0.03 * s;
-    if (s == 1 || cost < best_cost) best = s, best_cost = cost;
+// Most parts of the k range: 512 rows to a CU, parts together, which bounds the
+// workspace of their sums (1/2 MB a sequence); more were not the shortest anywhere.
+int stream_most_splits(int waves, int rows, int num_cus) {
+  const int most = 16 / waves * num_cus / stream_groups(waves, rows);
+  return most < 1 ? 1 : most < kMaxStreamSplits ? most : kMaxStreamSplits;
+}
+
+// How a product of more than 64 sequences runs: by rows_kernel (0), or by
+// linear_stream_kernel in so many parts of the k range, whichever these models
+// of the measured times say is shorter, in us of a chip of 256 CUs:
+//   rows_kernel: the matrix work of whole groups of 64 sequences or the read of
+//     the weights, and 5;
+//   here: the busiest CU's workgroups, 0.047 for 64 k of 128 rows and a column
+//     tile (the weights count as 4 more), or the read, and 11; with parts their
+//     sums' way through memory too.
+// Over 136 products (80 to 250 sequences, k 1024 to 16384, 2048 to 57344 rows) in
+// rows_kernel and 1, 2, 3, 4 and 6 parts the choice is 1.0% behind the best of
+// the six on average, 32% at most; rows_kernel always is 12.1% behind, a choice by the
+// rounds of workgroups alone 7.4%, and 98% at most (57344 x 1024, 126 sequences: 1 part
+// 36.7, 4 parts 72.8, rows_kernel 56.5).  Below 40 rows a CU rows_kernel is ahead
+// or level everywhere (8192 x 8192, 250: 58 against 65).
+int stream_splits(int batch, int rows, int k, int num_cus) {
+  if (batch <= 64 || rows < 40 * num_cus) return 0;
+  const double weights = static_cast<double>(rows) * k, scale = 256.0 / num_cus;
+  const double read = weights * 2 * scale / 8e6;
+  double best = weights * ((batch + 63) / 64 * 64) * scale / 2.5e8;
+  best = (best > read ? best : read) + 5;
+  int splits = 0;
+  const int waves = stream_waves(batch), groups = stream_groups(waves, rows), cols = (batch + 15) / 16;
+  for (int s = 1; s <= stream_most_splits(waves, rows, num_cus); ++s) {
+    const int most = (groups * s + num_cus - 1) / num_cus;
+    double t = most * 0.047 * (waves / 4) * (cols + 4) * k / kPairK / s;
+    t = (t > read ? t : read) + 11;
+    if (s > 1) t += static_cast<double>(s) * batch * rows * 4 * scale / 2.6e6;
+    if (t < best) best = t, splits = s;
   }
-  return best;
+  return splits;
 }
 
 // Products with few output features (a router's) of more than 16 sequences by
@@ -290,17 +316,13 @@ bool few_rows_plan(int batch, int rows, int num_cus, bool gated, RowsPlan* out) 
   return true;
 }
 
-bool stream_form(int batch, int rows, int num_cus) { return batch > 64 && rows >= 64 * num_cus; }
-
 }  // namespace
 
-// rows_kernel below 64 rows a CU, where the streaming form's gain ends (see
-// there), and up to 64 sequences.
 RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated) {
   RowsPlan few;
   if (few_rows_plan(batch, rows, num_cus, gated, &few)) return few;
-  if (!stream_form(batch, rows, num_cus))
-    return plan_rows(batch, rows, k, num_cus, gated ? Fusable::kPairs : Fusable::kAny, kMaxRowsSplits);
+  const int splits = stream_splits(batch, rows, k, num_cus);
+  if (!splits) return plan_rows(batch, rows, k, num_cus, gated ? Fusable::kPairs : Fusable::kAny, kMaxRowsSplits);
   RowsPlan p{};
   p.stream = true;
   p.waves = stream_waves(batch);
@@ -308,7 +330,7 @@ RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated) {
   p.bt = (batch + 15) / 16;
   p.row_groups = stream_groups(p.waves, rows);
   p.col_groups = 1;
-  p.splits = stream_splits(p.waves, rows, num_cus);
+  p.splits = splits;
   p.split_grid = p.row_groups;
   p.grid = p.row_groups * p.splits;
   p.fused = p.splits == 1;
@@ -316,11 +338,11 @@ RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated) {
 }
 
 int64_t linear_most_floats(int batch, int rows, int num_cus) {
-  int64_t most = rows_most_floats(batch < 64 ? batch : 64, rows, num_cus, kMaxRowsSplits);
+  int64_t most = rows_most_floats(batch, rows, num_cus, kMaxRowsSplits);
   if (batch <= 64) return most;
-  if (!stream_form(batch, rows, num_cus)) return rows_most_floats(batch, rows, num_cus, kMaxRowsSplits);
   for (const int b : {batch < 128 ? batch : 128, batch}) {
-    const int64_t n = static_cast<int64_t>(stream_splits(stream_waves(b), rows, num_cus)) * b * rows;
+    const int splits = stream_most_splits(stream_waves(b), rows, num_cus);
+    const int64_t n = splits > 1 ? static_cast<int64_t>(splits) * b * rows : 0;
     most = n > most ? n : most;
   }
   return most;

@@ -59,8 +59,8 @@ def test_fp32_out_with_bias(lib, b, k, n):
     run(lib, b, k, n, bias=True, f32=True)
 
 
-# many output features and more than 64 sequences: the form whose activations lie in LDS, at each number of
-# column tiles, k of less than a step, off a step, and of fewer steps than parts
+# many output features and more than 64 sequences, little k: each number of column tiles, k of less than a step and off
+# a step
 STREAM = [(65, 32, 16384), (80, 96, 16400), (81, 1056, 16384), (96, 160, 20480), (112, 640, 16640), (113, 2080, 16384),
           (128, 352, 17408), (129, 1024, 16384), (160, 64, 16400), (161, 544, 20480), (208, 1120, 16384), (209, 96, 18432),
           (256, 992, 16416)]
@@ -68,7 +68,6 @@ STREAM = [(65, 32, 16384), (80, 96, 16400), (81, 1056, 16384), (96, 160, 20480),
 
 @pytest.mark.parametrize("b,k,n", STREAM, ids=["%dx%dx%d" % s for s in STREAM])
 def test_many_features(lib, b, k, n):
-    assert lib.linear_plan(lib.linear_dims(b, k, n)).row_tiles == (8 if b <= 128 else 16)
     run(lib, b, k, n, act="gelu_tanh", bias=True)
     run(lib, b, k, n, f32=True, residual=True)
 
@@ -76,6 +75,23 @@ def test_many_features(lib, b, k, n):
 @pytest.mark.parametrize("b,k,n", STREAM, ids=["%dx%dx%d" % s for s in STREAM])
 def test_many_features_gated(lib, b, k, n):
     run(lib, b, k, (n // 2 + 15) // 16 * 16, act="silu", gated=True, bias=True, residual=True)
+
+
+# the form whose activations lie in LDS for all of a workgroup's rows, at each number of column tiles it has a kernel
+# for and its next lower one, whole and in 2 to 6 parts of k, k off a step, rows off a workgroup's, and its least k
+SHARED = [(65, 4128, 10240, 3), (80, 1120, 28672, 1), (81, 4160, 12304, 2), (96, 2080, 20496, 1), (112, 6176, 10256, 3),
+          (113, 544, 61440, 1), (128, 2080, 28688, 1), (129, 4128, 10240, 6), (129, 2080, 28672, 2), (160, 4128, 12304, 5),
+          (161, 2080, 40960, 1), (208, 4128, 10256, 6), (209, 544, 65552, 1), (256, 4160, 16400, 3), (70, 96, 262144, 1)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("b,k,n,parts", SHARED, ids=["%dx%dx%d" % s[:3] for s in SHARED])
+def test_shared_activations(lib, b, k, n, parts, gated):
+    n = n // 32 * 16 if gated else n
+    plan = lib.linear_plan(lib.linear_dims(b, k, n, "silu" if gated else "none", gated))
+    assert (plan.row_tiles, plan.col_tiles, plan.col_groups) == (8 if b <= 128 else 16, (b + 15) // 16, 1)
+    assert gated or plan.k_splits == parts
+    run(lib, b, k, n, act="silu" if gated else "none", gated=gated, bias=True, residual=not gated)
 
 
 @pytest.mark.parametrize("act", ["none", "silu", "gelu", "gelu_tanh", "relu"])
