@@ -25,10 +25,11 @@ constexpr uint32_t kOutside = 0x80000000u;  // past any descriptor: reads zero
 // reads of LDS (NT KB for every 2 KB of weights) and matrix instructions take
 // about 0.1 us a step and column tile for 256 rows and overlap little, so with
 // few row tiles rows_kernel, which needs no parts of k, stays ahead (the choice:
-// stream_splits).  us a product, rows_kernel -> here (5120 -> 20480, 101 sequences: 75.0 -> 54.1; 256:
-// 113.5 -> 88; 8192 -> 16384, 70: 74.3 -> 63.5, 128: 76.5 -> 73.8, 254: 113.4 ->
-// 96.8; 5120 -> 2 x 13824 gated, 70: 83.7 -> 65.0, 158: 108.5 -> 80.5; 14336 ->
-// 4096, 200: 53 -> 78; 4096 -> 14336, 67: 36.9 -> 31.2, 125: 40.3 -> 41.6).
+// stream_splits).  us a product, rows_kernel -> here: 5120 -> 20480, 101 75.0 -> 54.1, 256
+// 113.5 -> 88; 8192 -> 16384, 70 74.3 -> 63.5, 128 76.5 -> 73.8, 254 113.4 ->
+// 96.8; 5120 -> 2 x 13824 gated, 70 83.7 -> 65.0, 158 108.5 -> 80.5; 14336 ->
+// 4096, 200 53 -> 78; 4096 -> 14336, 67 36.9 -> 31.2, 125 40.3 -> 41.6 (sequences
+// after the sizes).
 //
 // Each row group starts its part of the k range at a place of its own: rows of
 // 16 or 32 KB otherwise meet in the same channels (80 x 8192 -> 8192 39.6 ->
@@ -292,19 +293,25 @@ int stream_splits(int batch, int rows, int k, int num_cus) {
 // bounds them is a workgroup's way through its activations and weights, not the
 // chip, and the forms that take up to 64 sequences together leave most CUs idle.
 // One row and one column tile a workgroup while there is a CU for each, then two
-// row tiles, then two of both, while two such workgroups have a CU.  us a
-// product, the planner's form -> these: 64 sequences, 4096 -> 64 7.9 -> 4.2, 1024
-// -> 256 5.9 -> 3.2, 8192 -> 1024 11.3 -> 8.7, 4096 -> 2048 11.1 -> 7.4; 256, 4096
-// -> 256 10.0 -> 6.1, -> 1024 12.1 -> 9.5; 32, 4096 -> 2048 8.6 -> 6.1; 48, 8192
-// -> 2 x 2048 gated 21.7 -> 15.1.  With more workgroups the planner's forms are
-// level or ahead (256, 4096 -> 2048 12.3, 13.9).
-bool few_rows_plan(int batch, int rows, int num_cus, bool gated, RowsPlan* out) {
+// row tiles, then two of both.  Past one round of workgroups, or where a
+// workgroup's way is long, the planner's forms, which share it or split k, are
+// level or ahead.  us a product, the planner's form -> these, weights cold:
+//   one of each: 20 sequences, 4096 -> 256 6.8 -> 5.5, 8192 -> 512 7.9 -> 10.1;
+//     200, 2048 -> 256 9.1 -> 4.7, 14336 -> 256 19.7 -> 16.9;
+//   two row tiles: 24, 4096 -> 2560 8.1 -> 9.1; 64, 4096 -> 2048 11.7 -> 9.3; 128,
+//     8192 -> 1024 16.4 -> 14.4, 14336 -> 1024 19.9 -> 22.8;
+//   two of both: 40, 4096 -> 4096 12.3 -> 11.4, -> 4640 (304 workgroups) 14.2 ->
+//     17.0; 128, 4096 -> 2048 16.2 -> 12.0; 64, 8192 -> 4096 21.5 -> 23.1.
+bool few_rows_plan(int batch, int rows, int k, int num_cus, bool gated, RowsPlan* out) {
   const int cols = (batch + 15) / 16, tiles = rows / kTileRows;
+  if (cols < 2) return false;
   const int64_t ones = static_cast<int64_t>(tiles) * cols, pairs = static_cast<int64_t>((tiles + 1) / 2) * cols;
   RowsPlan p{};
   p.rt = !gated && ones <= num_cus ? 1 : 2;
   p.bt = pairs <= num_cus ? 1 : 2;
   if (cols <= p.bt || pairs > 2 * num_cus) return false;
+  if (cols == 2 && (p.rt == 2 || k > 6144)) return false;
+  if (p.rt == 2 && k > (p.bt == 1 ? 8192 : 4096)) return false;
   p.waves = 8;
   p.kb = 2;
   p.fused = true;
@@ -312,6 +319,7 @@ bool few_rows_plan(int batch, int rows, int num_cus, bool gated, RowsPlan* out) 
   p.col_groups = (cols + p.bt - 1) / p.bt;
   p.splits = 1;
   p.split_grid = p.grid = (p.row_groups + 7) / 8 * 8 * p.col_groups;
+  if (p.grid > num_cus) return false;
   *out = p;
   return true;
 }
@@ -320,7 +328,7 @@ bool few_rows_plan(int batch, int rows, int num_cus, bool gated, RowsPlan* out) 
 
 RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated) {
   RowsPlan few;
-  if (few_rows_plan(batch, rows, num_cus, gated, &few)) return few;
+  if (few_rows_plan(batch, rows, k, num_cus, gated, &few)) return few;
   const int splits = stream_splits(batch, rows, k, num_cus);
   if (!splits) return plan_rows(batch, rows, k, num_cus, gated ? Fusable::kPairs : Fusable::kAny, kMaxRowsSplits);
   RowsPlan p{};
