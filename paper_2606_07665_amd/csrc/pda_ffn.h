@@ -56,10 +56,16 @@ inline int moe_most_segments(int pairs, int experts, int cols) {
 // 9.2, 200 of 2 over 8 of 512 22.2 -> 10.9, 33 of 2 over 8 of 1024 (4096 features)
 // 35.2 -> 27.6, 93 of 3 over 64 of 384 (1680 workgroups) 23.2 -> 23.6; down: the
 // same 7.0 -> 6.5, 13.0 -> 6.9, 16.7 -> 15.0, 67 tokens of 8 over 32 (2538) 16.7 ->
-// 21.7.
+// 21.7.  Up to twice as many stay ahead where an expert has few pairs and the
+// products' k range is long (cold weights; gate and up of 2240 features: 33 tokens
+// of 4 over 16 of 2272, 2698 workgroups, 59.2 -> 53.7; 33 of 3 over 64 of 512, 2080,
+// 40.4 -> 32.6; 80 of 4 over 16 of 1056, 1650, 56.0 -> 54.0; 128 of 6 over 32 of 512,
+// 24 pairs each, 1760, 37.3 -> 38.0; down: 33 of 4 over 16 of 2272, 1330, 36.5 ->
+// 30.9; k 512: 33 of 6 over 32, 2368, 15.9 -> 18.7).
 constexpr int kMoeFewCols = 32;
-inline bool moe_shares_tiles(int tokens, int pairs, int experts, int tiles, int num_cus) {
-  return static_cast<int64_t>(moe_most_segments(pairs, experts, kMoeFewCols)) * tiles <= (tokens <= 8 ? 8 : 5) * num_cus;
+inline bool moe_shares_tiles(int tokens, int pairs, int experts, int tiles, int k, int num_cus) {
+  const int a_cu = k >= 1536 && pairs <= 20 * experts ? 11 : tokens <= 8 ? 8 : 5;
+  return static_cast<int64_t>(moe_most_segments(pairs, experts, kMoeFewCols)) * tiles <= static_cast<int64_t>(a_cu) * num_cus;
 }
 
 // Parts of the down products' k range: doubled while the workgroups (128 rows

@@ -587,7 +587,7 @@ hipError_t launch_experts(const ExpertsArgs& args, int num_cus, hipStream_t st) 
   ExpertsArgs a = args;
   const int pairs = a.tokens * a.top_k;
   a.weighted_h = a.tokens <= 8 && pairs <= 64;
-  hipError_t e = moe_shares_tiles(a.tokens, pairs, a.experts, a.inter / kTileRows, num_cus)
+  hipError_t e = moe_shares_tiles(a.tokens, pairs, a.experts, a.inter / kTileRows, a.hidden, num_cus)
                      ? experts_as<Stage::kGateUp, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st)
                      : experts_as<Stage::kGateUp, kMoeCols / 16, 4, false, 64 * 1024, 2>(a, st);
   if (e != hipSuccess) return e;
@@ -597,7 +597,7 @@ hipError_t launch_experts(const ExpertsArgs& args, int num_cus, hipStream_t st) 
                        st, a);
     return hipGetLastError();
   }
-  if (moe_shares_tiles(a.tokens, pairs, a.experts, a.hidden / (2 * kTileRows), num_cus)) {
+  if (moe_shares_tiles(a.tokens, pairs, a.experts, a.hidden / (2 * kTileRows), a.inter, num_cus)) {
     a.splits = 1;
     e = experts_as<Stage::kDown, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st);
   } else {
