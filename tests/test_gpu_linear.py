@@ -202,6 +202,44 @@ def test_nothing_else_is_written(lib):
         assert (buf[:256] == 7).all() and (buf[256 + b * n:] == 7).all()
 
 
+# each form in use: 1 row and column tile a workgroup, 2 x 1, 2 x 2, the planner's with k split, activations shared
+# whole, in 3 and in 6 parts
+FORMS = [(36, 1024, 256), (40, 2048, 2048), (40, 2048, 4096), (24, 8192, 2560), (70, 1120, 28672), (70, 4128, 10240),
+         (129, 4128, 10240)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("b,k,n", FORMS, ids=["%dx%dx%d" % s for s in FORMS])
+def test_forms_in_use(lib, b, k, n, gated):
+    n = n // 32 * 16 if gated else n
+    x, w, bi, re = (gpu(t) for t in build(b, k, n, gated, True, True, 11))
+    wp = lib.pack_weights(w)
+    kw = dict(bias=bi, activation="silu", gated=gated)
+    want = lib.linear(x, wp, torch.empty_like(re), residual=re, **kw)
+    # in the residual's place, between guards, captured on a stream whose reserve was for more sequences
+    buf = torch.full((b * n + 512,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[256:256 + b * n].view(b, n)
+    stream = torch.cuda.Stream()
+    lib.linear_workspace_reserve(lib.linear_dims(256, k, n, "silu", gated), stream=stream)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        lib.linear(x, wp, out, residual=out, **kw)
+    for _ in range(3):
+        out.copy_(re)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert torch.equal(lib.linear(x, wp, torch.empty_like(re), residual=re, **kw), want)
+    assert (buf[:256] == 7).all() and (buf[256 + b * n:] == 7).all()
+    # what is not finite stays in its sequence
+    x[b - 1, k - 1], x[3, 0], x[17, k // 2] = float("inf"), float("nan"), float("-inf")
+    got = lib.linear(x, wp, torch.empty_like(re), residual=re, **kw)
+    rows = [i for i in range(b) if i not in (3, 17, b - 1)]
+    assert torch.equal(got[rows], want[rows]) and torch.isnan(got[3]).all()
+
+
 def test_empty_batch(lib):
     w = lib.pack_weights(torch.zeros((16, 32), dtype=torch.bfloat16, device="cuda"))
     out = lib.linear(torch.empty((0, 32), dtype=torch.bfloat16, device="cuda"), w,
