@@ -571,6 +571,7 @@ std::map<std::pair<int, hipStream_t>, Workspace> g_ws;
 // captured before may write to, until pda_release_workspaces.  (Each buffer is
 // at least 5/4 of the one before: four times the last one are kept at most.)
 int workspace_for(int dev, hipStream_t st, int64_t least, int64_t most, void** out) {
+  most = std::max(most, least);  // never less than this call writes, whatever its caller worked out
   std::lock_guard<std::mutex> lock(g_ws_mu);
   Workspace& ws = g_ws[{dev, st}];
   *out = ws.ptr;

@@ -538,12 +538,15 @@ __global__ __launch_bounds__(W * 64, rows_min_waves(RT, BT, W, KB)) void rows_ke
         total(kWide ? m.acc_r : 2 * m.acc_r, m.c, m.group, m.sub, v);
         total(kWide ? m.acc_r : 2 * m.acc_r + 1, m.c, kWide ? m.group + 2 : 0, m.sub, up);
 #pragma unroll
-        for (int j = 0; j < kRows; ++j)
-          v[j] = activate(v[j] + unpack_bf16(raw[t], j), e.activation) * (up[j] + unpack_bf16(raw[t] + kHalf, j));
+        for (int j = 0; j < kRows; ++j) v[j] += unpack_bf16(raw[t], j);
+        activate(v, e.activation);
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) v[j] *= up[j] + unpack_bf16(raw[t] + kHalf, j);
       } else {
         total(m.acc_r, m.c, m.group, m.sub, v);
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) v[j] = activate(v[j] + unpack_bf16(raw[t], j), e.activation);
+        for (int j = 0; j < kRows; ++j) v[j] += unpack_bf16(raw[t], j);
+        activate(v, e.activation);
       }
       // (adding an absent residual's zeros would turn a -0 into a 0)
       if (e.residual) {
@@ -722,8 +725,10 @@ __global__ __launch_bounds__(kLinearThreads) void linear_epilogue(LinearArgs a, 
   }
   float v[4];
 #pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = g[j] + unpack_bf16(bias, j);
+  activate(v, a.activation);
+#pragma unroll
   for (int j = 0; j < 4; ++j) {
-    v[j] = activate(g[j] + unpack_bf16(bias, j), a.activation);
     if (gated) v[j] *= u[j] + unpack_bf16(bias_up, j);
     if (a.residual) v[j] += unpack_bf16(res, j);
   }

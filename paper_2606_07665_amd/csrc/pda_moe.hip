@@ -328,9 +328,10 @@ __global__ __launch_bounds__(kMoeWaves * 64, kWavesPerSimd) void experts_kernel(
       if constexpr (kUp) {
         const float scale = a.weighted_h ? a.weights[p] : 1.f;
         const int f = 16 * (group * (RT / 2) + r) + 4 * kblk;
-        float h[4];
+        float h[4] = {v[0], v[1], v[2], v[3]};
+        activate(h, a.activation);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) h[j] = scale * activate(v[j], a.activation) * up[j];
+        for (int j = 0; j < 4; ++j) h[j] = scale * h[j] * up[j];
         if (f < a.inter) store_bf16<4>(a.h + static_cast<int64_t>(p) * a.inter + f, h);
       } else {
         const int o = 16 * (group * RT + r) + 4 * kblk;
