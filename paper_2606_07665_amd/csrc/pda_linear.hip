@@ -1,6 +1,7 @@
-// Linear products of more than 64 sequences with many output features, for
+// Linear products of more than 32 sequences with many output features, for
 // MI355X (gfx950, CDNA4, wave64), and the plan of every linear product.
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "pda_device.h"
@@ -23,13 +24,9 @@ constexpr uint32_t kOutside = 0x80000000u;  // past any descriptor: reads zero
 // its tiles; here every activation in LDS meets all of a workgroup's rows, and a
 // workgroup reads all sequences once.  What bounds this form is the CU: operand
 // reads of LDS (NT KB for every 2 KB of weights) and matrix instructions take
-// about 0.1 us a step and column tile for 256 rows and overlap little, so with
+// about 0.08 us a step and column tile for 256 rows and overlap little, so with
 // few row tiles rows_kernel, which needs no parts of k, stays ahead (the choice:
-// stream_splits).  us a product, rows_kernel -> here: 5120 -> 20480, 101 75.0 -> 54.1, 256
-// 113.5 -> 88; 8192 -> 16384, 70 74.3 -> 63.5, 128 76.5 -> 73.8, 254 113.4 ->
-// 96.8; 5120 -> 2 x 13824 gated, 70 83.7 -> 65.0, 158 108.5 -> 80.5; 14336 ->
-// 4096, 200 53 -> 78; 4096 -> 14336, 67 36.9 -> 31.2, 125 40.3 -> 41.6 (sequences
-// after the sizes).
+// stream_splits, with both sides' times).
 //
 // Each row group starts its part of the k range at a place of its own: rows of
 // 16 or 32 KB otherwise meet in the same channels (80 x 8192 -> 8192 39.6 ->
@@ -263,6 +260,7 @@ constexpr int stream_waves(int batch) { return batch <= 128 ? 4 : 8; }
 template <bool kGated>
 hipError_t linear_stream_any(const RowsArgs& a, const LinearArgs& e, hipStream_t st) {
   const int nt = (a.batch + 15) / 16;
+  if (nt <= 4) return linear_stream_as<kGated, 2, 4, 4, 4, 2, 2>(a, e, st);
   if (nt <= 5) return linear_stream_as<kGated, 2, 5, 4, 4, 2, 2>(a, e, st);
   if (nt <= 6) return linear_stream_as<kGated, 2, 6, 4, 4, 2, 2>(a, e, st);
   if (nt <= 7) return linear_stream_as<kGated, 2, 7, 4, 4, 2, 2>(a, e, st);
@@ -282,33 +280,37 @@ int stream_most_splits(int waves, int rows, int num_cus) {
   return most < 1 ? 1 : most < kMaxStreamSplits ? most : kMaxStreamSplits;
 }
 
-// How a product of more than 64 sequences runs: by rows_kernel (0), or by
+// How a product of more than 32 sequences runs: by rows_kernel (0), or by
 // linear_stream_kernel in so many parts of the k range, whichever these models
-// of the measured times say is shorter, in us of a chip of 256 CUs:
-//   rows_kernel: the matrix work of whole groups of 64 sequences or the read of
-//     the weights, and 5;
-//   here: the busiest CU's workgroups, 0.047 for 64 k of 128 rows and a column
-//     tile (the weights count as 4 more), or the read, and 11; with parts their
-//     sums' way through memory too.
-// Over 136 products (80 to 250 sequences, k 1024 to 16384, 2048 to 57344 rows) in
-// rows_kernel and 1, 2, 3, 4 and 6 parts the choice is 1.0% behind the best of
-// the six on average, 32% at most; rows_kernel always is 12.1% behind, a choice by the
-// rounds of workgroups alone 7.4%, and 98% at most (57344 x 1024, 126 sequences: 1 part
-// 36.7, 4 parts 72.8, rows_kernel 56.5).  Below 40 rows a CU rows_kernel is ahead
-// or level everywhere (8192 x 8192, 250: 58 against 65).
+// of the measured times say is shorter, in us of a chip of 256 CUs.  Each joins, as
+// the root of the squares, its products and the read of the weights:
+//   rows_kernel: whole groups of 64 sequences at 3.6e8 outputs x k a us, the read
+//     at 6.4 TB/s; 4.4, and 2.4 a million outputs of those groups.
+//   here: the busiest CU's workgroups, 0.036 for 64 k of 128 rows and a column
+//     tile (the weights count as 5 more), the read at 6.5 TB/s, less by the root of
+//     the CUs without a workgroup; 4.7; whole, 0.12 for the epilogue of 128 rows and a
+//     column tile, in parts 5.4 for the second kernel and the parts' sums, written
+//     and read, at 3 MB a us.
+// With weights out of every cache the models are 8% off, and the choice over 246
+// products (80 to 250 sequences, k 256 to 8192, 8192 to 57344 rows) is 0.4% behind
+// the best of rows_kernel and 1, 2, 3, 4 and 6 parts on average, 13% at most;
+// rows_kernel always is 24.2% behind.  Over 120 of 36 to 64 sequences, not in parts,
+// 0.5%, and 11.8% (us, rows_kernel, whole, 3 parts: 80, 256 -> 57344 30.9, 12.5, -;
+// 101, 5120 -> 20480 with GELU -, 64.0, 54.5; 250, 2048 -> 28672 75.0, 62.7, 83.2, in
+// two 58.8; 64, 4096 -> 20480 40.0, 44.4, 45.7).
 int stream_splits(int batch, int rows, int k, int num_cus) {
-  if (batch <= 64 || rows < 40 * num_cus) return 0;
-  const double weights = static_cast<double>(rows) * k, scale = 256.0 / num_cus;
-  const double read = weights * 2 * scale / 8e6;
-  double best = weights * ((batch + 63) / 64 * 64) * scale / 2.5e8;
-  best = (best > read ? best : read) + 5;
+  if (batch <= 32 || rows < 40 * num_cus) return 0;
+  const double scale = 256.0 / num_cus, weights = scale * rows * k, outputs = scale * rows * ((batch + 63) / 64 * 64);
+  auto joined = [](double a, double b) { return std::sqrt(a * a + b * b); };
+  double best = joined(outputs * k / 3.6e8, weights * 2 / 6.4e6) + 2.4e-6 * outputs + 4.4;
   int splits = 0;
   const int waves = stream_waves(batch), groups = stream_groups(waves, rows), cols = (batch + 15) / 16;
-  for (int s = 1; s <= stream_most_splits(waves, rows, num_cus); ++s) {
-    const int most = (groups * s + num_cus - 1) / num_cus;
-    double t = most * 0.047 * (waves / 4) * (cols + 4) * k / kPairK / s;
-    t = (t > read ? t : read) + 11;
-    if (s > 1) t += static_cast<double>(s) * batch * rows * 4 * scale / 2.6e6;
+  const int most = batch <= 64 ? 1 : stream_most_splits(waves, rows, num_cus);
+  for (int s = 1; s <= most; ++s) {
+    const double busiest = (groups * s + num_cus - 1) / num_cus * (waves / 4);
+    const double used = groups * s < num_cus ? std::sqrt(static_cast<double>(groups * s) / num_cus) : 1.0;
+    const double t = joined(busiest * 0.036 * (cols + 5) * k / kPairK / s, weights * 2 / 6.5e6 / used) + 4.7 +
+                     (s == 1 ? busiest * 0.12 * cols : scale * s * batch * rows * 4 / 3e6 + 5.4);
     if (t < best) best = t, splits = s;
   }
   return splits;
@@ -373,7 +375,7 @@ RowsPlan plan_linear(int batch, int rows, int k, int num_cus, bool gated) {
 
 int64_t linear_most_floats(int batch, int rows, int num_cus) {
   int64_t most = rows_most_floats(batch, rows, num_cus, kMaxRowsSplits);
-  if (batch <= 64) return most;
+  if (batch <= 64) return most;  // (streamed whole)
   for (const int b : {batch < 128 ? batch : 128, batch}) {
     const int splits = stream_most_splits(stream_waves(b), rows, num_cus);
     const int64_t n = splits > 1 ? static_cast<int64_t>(splits) * b * rows : 0;

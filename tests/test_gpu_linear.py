@@ -78,10 +78,11 @@ def test_many_features_gated(lib, b, k, n):
 
 
 # the form whose activations lie in LDS for all of a workgroup's rows, at each number of column tiles it has a kernel
-# for and its next lower one, whole and in 2 to 6 parts of k, k off a step, rows off a workgroup's, and its least k
-SHARED = [(65, 4128, 10240, 3), (80, 1120, 28672, 1), (81, 4160, 12304, 2), (96, 2080, 20496, 1), (112, 6176, 10256, 3),
-          (113, 544, 61440, 1), (128, 2080, 28688, 1), (129, 4128, 10240, 6), (129, 2080, 28672, 2), (160, 4128, 12304, 5),
-          (161, 2080, 40960, 1), (208, 4128, 10256, 6), (209, 544, 65552, 1), (256, 4160, 16400, 3), (70, 96, 262144, 1)]
+# for and its next lower one, whole and in 2 to 6 parts of k, k off a step and of less than one, rows off a workgroup's
+SHARED = [(33, 96, 61456, 1), (36, 1120, 20480, 1), (64, 544, 28688, 1), (65, 1120, 28672, 1), (80, 6176, 12304, 5),
+          (96, 8224, 10256, 3), (96, 32, 20496, 1), (96, 2080, 20496, 1), (113, 544, 61440, 1), (128, 2080, 28688, 1), (129, 2080, 28672, 2),
+          (129, 4128, 16400, 3), (129, 6176, 12304, 5), (160, 8224, 10240, 6), (161, 2080, 40960, 1), (208, 8224, 10256, 6),
+          (209, 544, 65552, 1), (256, 1056, 40976, 1), (70, 96, 262144, 1)]
 
 
 @pytest.mark.parametrize("gated", [False, True])
@@ -203,9 +204,9 @@ def test_nothing_else_is_written(lib):
 
 
 # each form in use: 1 row and column tile a workgroup, 2 x 1, 2 x 2, the planner's with k split, activations shared
-# whole, in 3 and in 6 parts
-FORMS = [(36, 1024, 256), (40, 2048, 2048), (40, 2048, 4096), (24, 8192, 2560), (70, 1120, 28672), (70, 4128, 10240),
-         (129, 4128, 10240)]
+# whole and in 3 to 6 parts
+FORMS = [(36, 1024, 256), (40, 2048, 2048), (40, 2048, 4096), (24, 8192, 2560), (70, 1120, 28672), (40, 544, 28672),
+         (96, 8224, 10256), (129, 4128, 16400), (129, 8224, 10240)]
 
 
 @pytest.mark.parametrize("gated", [False, True])
