@@ -217,8 +217,9 @@ __global__ __launch_bounds__(kMoeWaves * 64, kWavesPerSimd) void experts_kernel(
   }
   u32x4 wa[D][RT][2];
   auto issue_w = [&](int slot, int q) __attribute__((always_inline)) {
-    // (k tiles past the end lie outside; those of the next part are not used)
-    const uint32_t at = static_cast<uint32_t>(begin + q * kStride + first) * 2048u + lane * 16u;
+    // (k tiles past the end lie outside; so do those of the next part)
+    const int s = q * kStride + first;
+    const uint32_t at = s < steps ? static_cast<uint32_t>(begin + s) * 2048u + lane * 16u : kOutside;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -278,48 +279,96 @@ __global__ __launch_bounds__(kMoeWaves * 64, kWavesPerSimd) void experts_kernel(
       }
     };
     __syncthreads();  // the ids are done with
-    issue_chunk(0);
-    __builtin_amdgcn_s_waitcnt(kWaitLoads);
-    __syncthreads();
-    const int all = (steps + kStride - 1) / kStride;  // the most steps of a wave
-    for (int q0 = 0; q0 < all; q0 += kQ) {
-      const int end = q0 + kQ < count ? q0 + kQ : count;
-      const unsigned char* from = lds + first * kSlot;
-      auto step = [&](int j, int q) __attribute__((always_inline)) {
-        const unsigned char* at = from + (q - q0) * (kStride * kSlot);
-        u32x4 xb[NT][2];
+    // a step's products: the weights of slot j, the activations at `at`
+    auto multiply = [&](int j, const unsigned char* at) __attribute__((always_inline)) {
+      u32x4 xb[NT][2];
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) xb[c][m] = *reinterpret_cast<const u32x4*>(at + c * 2048 + (frag0 ^ (m * 64)));
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int c = 0; c < NT; ++c)
 #pragma unroll
-          for (int m = 0; m < 2; ++m) xb[c][m] = *reinterpret_cast<const u32x4*>(at + c * 2048 + (frag0 ^ (m * 64)));
+          for (int r = 0; r < RT; ++r)
+            acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[j][r][m]),
+                                                                __builtin_bit_cast(bf16x8, xb[c][m]), acc[r][c], 0, 0, 0);
+    };
+    if constexpr (!kSplit && NT >= 3) {
+      // a whole chunk of many columns is only a few steps, and no weights are in
+      // flight behind it when it has come: two steps at a time in two places, the next
+      // ones on their way, in whole rounds without a branch (what lies past the end is
+      // zeros).  us: 80 tokens of 5 over 8 experts of 1056 (3584 features) 68.1 -> 64.5,
+      // 128 of 2 over 8 of 14336 (4096) 575.7 -> 561.1, fewer columns level.
+      static_assert(D == 4 && W == 4 && 4 * kSlot <= kChunkBytes, "two places of two steps");
+      uint32_t xgroup[NT];  // the wave's share: half of the groups of one of two steps
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int c = 0; c < NT; ++c)
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-              acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[j][r][m]),
-                                                                  __builtin_bit_cast(bf16x8, xb[c][m]), acc[r][c], 0, 0, 0);
-      };
-      // whole rounds without a branch, so that the waits count the loads of
-      // every step in flight; then the last steps
-      int q = q0;
-      for (; q + D <= end; q += D) {
-#pragma unroll
-        for (int j = 0; j < D; ++j) {
-          step(j, q + j);
-          issue_w(j, q + j + D);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int i = 0; i < NT; ++i) {
+        const int p = column(cols, 8 * ((wv >> 1) * NT + i) + (lane >> 3));
+        const uint32_t row = static_cast<uint32_t>(kUp ? p / a.top_k : p);
+        xgroup[i] = p < 0 ? kOutside : row * static_cast<uint32_t>(k) * 2u + xpiece * 16u;
       }
+      auto issue_two = [&](int q0, int place) __attribute__((always_inline)) {
+        const int s = q0 + (wv & 1);
+        const uint32_t k0 = static_cast<uint32_t>(begin + s) * kPairK;
+        const bool in = s < steps && static_cast<int>(k0) + 8 * xpiece < k;
+        unsigned char* to = lds + (2 * place + (wv & 1)) * kSlot + (wv >> 1) * (NT * 1024);
 #pragma unroll
-      for (int j = 0; j < D; ++j)
-        if (q + j < end) step(j, q + j);
-      if (q0 + kQ >= all) break;
-      __syncthreads();
-      issue_chunk(q0 + kQ);
+        for (int i = 0; i < NT; ++i) {
+          const uint32_t off = in && xgroup[i] != kOutside ? xgroup[i] + k0 * 2u : kOutside;
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void*)(to + i * 1024), 16, off, 0, 0, 0);
+        }
+      };
+      issue_two(0, 0);
       __builtin_amdgcn_s_waitcnt(kWaitLoads);
       __syncthreads();
+      for (int q1 = 0; q1 < steps; q1 += D) {
+#pragma unroll
+        for (int ph = 0; ph < 2; ++ph) {
+          issue_two(q1 + 2 * ph + 2, ph ^ 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int q = 2 * ph; q < 2 * ph + 2; ++q) {
+            multiply(q, lds + q * kSlot);
+            issue_w(q, q1 + q + D);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_s_waitcnt(wait_loads(4 * RT));  // all but the weights after the activations
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+        }
+      }
+    } else {
+      issue_chunk(0);
+      __builtin_amdgcn_s_waitcnt(kWaitLoads);
+      __syncthreads();
+      const int all = (steps + kStride - 1) / kStride;  // the most steps of a wave
+      for (int q0 = 0; q0 < all; q0 += kQ) {
+        const int end = q0 + kQ < count ? q0 + kQ : count;
+        const unsigned char* from = lds + first * kSlot;
+        auto step = [&](int j, int q) __attribute__((always_inline)) { multiply(j, from + (q - q0) * (kStride * kSlot)); };
+        // whole rounds without a branch, so that the waits count the loads of
+        // every step in flight; then the last steps
+        int q = q0;
+        for (; q + D <= end; q += D) {
+#pragma unroll
+          for (int j = 0; j < D; ++j) {
+            step(j, q + j);
+            issue_w(j, q + j + D);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < D; ++j)
+          if (q + j < end) step(j, q + j);
+        if (q0 + kQ >= all) break;
+        __syncthreads();
+        issue_chunk(q0 + kQ);
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+        __syncthreads();
+      }
     }
 
     // a column's pair and the four rows 4 kblk .. of row tile (or pair) r
