@@ -845,9 +845,12 @@ int pda_moe_route(const float* logits, const float* select_bias, int32_t* expert
  * operand) and out once.  Only the experts that are asked for are
  * read.  What is not finite in a token reaches that token alone, in an
  * expert's weights the tokens that chose it.  Uses the
- * (device, stream) workspace: tokens * top_k * (2 inter + 4 hidden) bytes, and
- * up to 32 hidden in place of the 4 but no more than 128 MB for them where the
- * down products are cut (pda_moe_workspace_reserve before graph capture).
+ * (device, stream) workspace (pda_moe_workspace_reserve before graph capture):
+ * tokens * top_k * 2 inter bytes for what lies between the two products, and 4
+ * hidden a pair for each part of the down products' sums, none for up to 8 tokens
+ * and 64 pairs.  A call that needs more than there is asks for what covers every
+ * smaller call too: 32 hidden a pair, up to 128 MB, but never less than 4 hidden a
+ * pair (pda_moe_plan has both figures).
  */
 typedef struct {
   int32_t tokens;        /* 0 .. 256                                               */
@@ -893,11 +896,11 @@ int pda_block_norm(const void* y, const void* residual, const void* post_w, cons
                    void* residual_out, void* normed_out, const pda_block_norm_dims* dims, void* stream);
 
 /*
- * pda_prelude_plan, pda_o_proj_plan, pda_linear_plan [library interface] --
- * host-only dry runs of the planner of the projection y = x W^T in a prelude
- * (qk_norm: with norm weights), in an output projection and in a product with
- * its epilogue, as pda_plan for attention.  No HIP
- * call.  (A prelude whose outputs lie over x or the weights runs unfused,
+ * pda_prelude_plan, pda_o_proj_plan, pda_linear_plan, pda_moe_plan [library
+ * interface] -- host-only dry runs of the planner of the projection y = x W^T in a
+ * prelude (qk_norm: with norm weights), in an output projection and in a product
+ * with its epilogue, and of the experts' products, as pda_plan for attention.  No
+ * HIP call.  (A prelude whose outputs lie over x or the weights runs unfused,
  * whatever the plan says.)  Errors as for the calls' arguments; batch 0 gives
  * all zeros.
  */
@@ -916,6 +919,17 @@ typedef struct {
 int pda_prelude_plan(const pda_prelude_dims* dims, int32_t qk_norm, int32_t num_cus, pda_projection* out);
 int pda_o_proj_plan(int32_t batch, int32_t in_features, int32_t hidden, int32_t num_cus, pda_projection* out);
 int pda_linear_plan(const pda_linear_dims* dims, int32_t num_cus, pda_projection* out);
+typedef struct {
+  int32_t shared_up;            /* 1: the waves of a workgroup share the row tiles of
+                                   the gate and up products                        */
+  int32_t shared_down;          /* 1: and of the down products                     */
+  int32_t joined;               /* 1: down products and their sums in one kernel   */
+  int32_t k_splits;             /* parts of the down products' k range             */
+  int64_t call_bytes;           /* of the workspace that the call writes           */
+  int64_t workspace_bytes;      /* that the call asks for: enough for every smaller
+                                   number of tokens and top_k as well              */
+} pda_experts;
+int pda_moe_plan(const pda_moe_dims* dims, int32_t num_cus, pda_experts* out);
 
 #ifdef __cplusplus
 }

@@ -77,6 +77,12 @@ class MoeDims(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in ("tokens", "hidden", "inter", "num_experts", "top_k", "activation")]
 
 
+class Experts(ctypes.Structure):
+    """pda_experts of include/pda.h."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("shared_up", "shared_down", "joined", "k_splits")] + \
+               [(name, ctypes.c_int64) for name in ("call_bytes", "workspace_bytes")]
+
+
 class BlockNormDims(ctypes.Structure):
     """pda_block_norm_dims of include/pda.h."""
     _fields_ = [(name, ctypes.c_int32) for name in ("rows", "hidden", "gate_rows")] + \
@@ -184,9 +190,10 @@ def _declare(lib: ctypes.CDLL) -> None:
     lib.pda_moe_route.argtypes = [vp] * 4 + [ctypes.POINTER(RouteDims), vp]
     lib.pda_moe_experts.argtypes = [vp] * 7 + [ctypes.POINTER(MoeDims), vp]
     lib.pda_moe_workspace_reserve.argtypes = [ctypes.POINTER(MoeDims), vp]
+    lib.pda_moe_plan.argtypes = [ctypes.POINTER(MoeDims), i32, ctypes.POINTER(Experts)]
     lib.pda_block_norm.argtypes = [vp] * 7 + [ctypes.POINTER(BlockNormDims), vp]
     for fn in (lib.pda_linear, lib.pda_linear_workspace_reserve, lib.pda_linear_plan, lib.pda_moe_route,
-               lib.pda_moe_experts, lib.pda_moe_workspace_reserve, lib.pda_block_norm):
+               lib.pda_moe_experts, lib.pda_moe_workspace_reserve, lib.pda_moe_plan, lib.pda_block_norm):
         fn.restype = ctypes.c_int
     lib.pda_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
     lib.pda_kv_append_n.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]
@@ -1109,6 +1116,13 @@ def moe_dims(tokens, hidden, inter, num_experts, top_k, activation="silu") -> Mo
 
 def moe_workspace_reserve(dims: MoeDims, stream=None) -> None:
     _check(load().pda_moe_workspace_reserve(ctypes.byref(dims), _stream_ptr(stream)))
+
+
+def moe_plan(dims: MoeDims, num_cus: int = 256) -> Experts:
+    """How the experts' products of these dims run, and what they write of the workspace (no HIP call)."""
+    p = Experts()
+    _check(load().pda_moe_plan(ctypes.byref(dims), num_cus, ctypes.byref(p)))
+    return p
 
 
 def block_norm(y, residual, residual_out, normed_out=None, *, post_w=None, pre_w=None, gate=None, scale=1.0,

@@ -937,8 +937,14 @@ int check_moe(const pda_moe_dims* dm) {
   return PDA_OK;
 }
 
-// h [pairs, inter] in bf16, then y [splits, pairs, hidden] in fp32.
+pda::ExpertsPlan moe_plan(const pda_moe_dims& d, int cus) {
+  return pda::plan_experts(d.tokens, d.hidden, d.inter, d.num_experts, d.top_k, cus);
+}
+
+// h [pairs, inter] in bf16, then y [splits, pairs, hidden] in fp32: what a call
+// writes, and what covers every call of fewer tokens or choices.
 int64_t moe_h_bytes(const pda_moe_dims& d) { return align256(int64_t{2} * d.tokens * d.top_k * d.inter); }
+int64_t moe_call_bytes(const pda_moe_dims& d, const pda::ExpertsPlan& p) { return moe_h_bytes(d) + align256(4 * p.y_floats); }
 int64_t moe_ws_bytes(const pda_moe_dims& d, int cus) {
   return moe_h_bytes(d) + align256(4 * pda::moe_most_floats(d.tokens * d.top_k, d.hidden, cus));
 }
@@ -1910,10 +1916,10 @@ int pda_moe_experts(const void* x, const int32_t* expert_ids, const float* exper
   int cus = 0;
   if ((rc = device_cus(dev, &cus))) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const pda::ExpertsPlan plan = moe_plan(d, cus);
   void* ws = nullptr;
-  const int64_t need = moe_ws_bytes(d, cus);
-  if ((rc = workspace_for(dev, st, need, need, &ws))) return rc;
-  pda::ExpertsArgs a;
+  if ((rc = workspace_for(dev, st, moe_call_bytes(d, plan), moe_ws_bytes(d, cus), &ws))) return rc;
+  pda::ExpertsArgs a{};
   a.x = static_cast<const uint16_t*>(x);
   a.ids = expert_ids;
   a.weights = expert_weights;
@@ -1929,7 +1935,7 @@ int pda_moe_experts(const void* x, const int32_t* expert_ids, const float* exper
   a.experts = d.num_experts;
   a.top_k = d.top_k;
   a.activation = d.activation;
-  if ((e = pda::launch_experts(a, cus, st)) != hipSuccess) return hip_fail(e, "experts kernel launch");
+  if ((e = pda::launch_experts(a, plan, st)) != hipSuccess) return hip_fail(e, "experts kernel launch");
   return PDA_OK;
 }
 
@@ -1946,6 +1952,24 @@ int pda_moe_workspace_reserve(const pda_moe_dims* dims, void* stream) {
   void* ptr = nullptr;
   const int64_t need = moe_ws_bytes(*dims, cus);
   return workspace_for(dev, static_cast<hipStream_t>(stream), need, need, &ptr);
+}
+
+int pda_moe_plan(const pda_moe_dims* dims, int32_t num_cus, pda_experts* out) {
+  g_err.clear();
+  if (!out) return fail(PDA_ERR_NULL, "pda_moe_plan: NULL output pointer");
+  int rc = check_moe(dims);
+  if (rc) return rc;
+  if (num_cus <= 0) return fail(PDA_ERR_SHAPE, "num_cus must be positive");
+  *out = pda_experts{};
+  if (dims->tokens == 0) return PDA_OK;
+  const pda::ExpertsPlan p = moe_plan(*dims, num_cus);
+  out->shared_up = p.shared_up;
+  out->shared_down = p.shared_down;
+  out->joined = p.joined;
+  out->k_splits = p.splits;
+  out->call_bytes = moe_call_bytes(*dims, p);
+  out->workspace_bytes = moe_ws_bytes(*dims, num_cus);
+  return PDA_OK;
 }
 
 int pda_block_norm(const void* y, const void* residual, const void* post_w, const void* pre_w, const void* gate,

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <cstdint>
 
+#include "pda_gemv.h"
+
 namespace pda {
 
 constexpr int kMaxExperts = 1024;
@@ -39,7 +41,6 @@ struct ExpertsArgs {
   bool weighted_h;           // h carries the pair's weight
   int splits;                // parts of the down products' k range
 };
-hipError_t launch_experts(const ExpertsArgs& a, int num_cus, hipStream_t st);
 
 // Segments of up to `cols` pairs of one expert: the most that the pairs make.
 constexpr int kMoeCols = 128;
@@ -87,6 +88,25 @@ inline int64_t moe_most_floats(int pairs, int hidden, int num_cus) {
   const int64_t most = kMaxMoeSplits * one < bound ? kMaxMoeSplits * one : bound;
   return one > most ? one : most;
 }
+
+// How a call runs: what it launches and what it writes of the workspace.
+struct ExpertsPlan {
+  bool shared_up, shared_down;  // waves share row tiles, of the gate and up or of the down products
+  bool joined;                  // down products and combination in one kernel; h carries the pair's weight
+  int splits;                   // parts of the down products' k range
+  int64_t y_floats;             // of y
+};
+inline ExpertsPlan plan_experts(int tokens, int hidden, int inter, int experts, int top_k, int num_cus) {
+  const int pairs = tokens * top_k;
+  ExpertsPlan p{};
+  p.shared_up = moe_shares_tiles(tokens, pairs, experts, inter / kTileRows, hidden, num_cus);
+  p.joined = tokens <= 8 && pairs <= 64;
+  p.shared_down = !p.joined && moe_shares_tiles(tokens, pairs, experts, hidden / (2 * kTileRows), inter, num_cus);
+  p.splits = p.joined || p.shared_down ? 1 : moe_splits(pairs, experts, hidden, inter, num_cus);
+  p.y_floats = p.joined ? 0 : static_cast<int64_t>(p.splits) * pairs * hidden;
+  return p;
+}
+hipError_t launch_experts(const ExpertsArgs& a, const ExpertsPlan& p, hipStream_t st);
 
 constexpr int kMaxNormRows = 1 << 24;
 struct BlockNormArgs {

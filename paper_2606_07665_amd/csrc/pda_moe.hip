@@ -633,27 +633,21 @@ hipError_t experts_as(const ExpertsArgs& a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_experts(const ExpertsArgs& args, int num_cus, hipStream_t st) {
+hipError_t launch_experts(const ExpertsArgs& args, const ExpertsPlan& p, hipStream_t st) {
   ExpertsArgs a = args;
-  const int pairs = a.tokens * a.top_k;
-  a.weighted_h = a.tokens <= 8 && pairs <= 64;
-  hipError_t e = moe_shares_tiles(a.tokens, pairs, a.experts, a.inter / kTileRows, a.hidden, num_cus)
-                     ? experts_as<Stage::kGateUp, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st)
-                     : experts_as<Stage::kGateUp, kMoeCols / 16, 4, false, 64 * 1024, 2>(a, st);
+  a.weighted_h = p.joined;
+  a.splits = p.splits;
+  hipError_t e = p.shared_up ? experts_as<Stage::kGateUp, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st)
+                             : experts_as<Stage::kGateUp, kMoeCols / 16, 4, false, 64 * 1024, 2>(a, st);
   if (e != hipSuccess) return e;
-  if (a.weighted_h) {
+  if (p.joined) {
     constexpr int kJoinWaves = 8;
     hipLaunchKernelGGL((experts_join_kernel<kJoinWaves, 4>), dim3(static_cast<unsigned>(a.hidden / 8)), dim3(kJoinWaves * 64), 0,
                        st, a);
     return hipGetLastError();
   }
-  if (moe_shares_tiles(a.tokens, pairs, a.experts, a.hidden / (2 * kTileRows), a.inter, num_cus)) {
-    a.splits = 1;
-    e = experts_as<Stage::kDown, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st);
-  } else {
-    a.splits = moe_splits(pairs, a.experts, a.hidden, a.inter, num_cus);
-    e = experts_as<Stage::kDown, kMoeCols / 16, 4, false, 64 * 1024, 2>(a, st);
-  }
+  e = p.shared_down ? experts_as<Stage::kDown, kMoeFewCols / 16, 2, true, 32 * 1024, 4>(a, st)
+                    : experts_as<Stage::kDown, kMoeCols / 16, 4, false, 64 * 1024, 2>(a, st);
   if (e != hipSuccess) return e;
   const int64_t threads = static_cast<int64_t>(a.tokens) * (a.hidden / 4);
   hipLaunchKernelGGL(combine_kernel, dim3(static_cast<unsigned>((threads + kCombineThreads - 1) / kCombineThreads)),
