@@ -244,10 +244,25 @@ hipError_t route_as(const RouteArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// A launch takes fewer than 2^32 threads: more rows (of 8192 features 4194304, 68
+// GB) go in several.
+constexpr int64_t kNormThreadsALaunch = int64_t{1} << 31;
 template <int kThreads, int kPasses>
-hipError_t block_norm_as(const BlockNormArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((block_norm_kernel<kThreads, kPasses>), dim3(static_cast<unsigned>(a.rows)), dim3(kThreads), 0, st, a);
-  return hipGetLastError();
+hipError_t block_norm_as(BlockNormArgs a, hipStream_t st) {
+  constexpr int kMost = static_cast<int>(kNormThreadsALaunch / kThreads);
+  for (int left = a.rows; left > 0; left -= kMost) {
+    a.rows = left < kMost ? left : kMost;
+    hipLaunchKernelGGL((block_norm_kernel<kThreads, kPasses>), dim3(static_cast<unsigned>(a.rows)), dim3(kThreads), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t on = static_cast<int64_t>(a.rows) * a.hidden;
+    a.y += on;
+    a.z += on;
+    if (a.residual) a.residual += on;
+    if (a.gate) a.gate += a.rows * a.gate_stride;
+    if (a.h) a.h += on;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
