@@ -767,9 +767,10 @@ int pda_o_proj_workspace_reserve(int32_t batch, int32_t in_features, int32_t hid
  *   out       bf16 [batch, out_features], or fp32 with out_f32 (a router's
  *             logits); in bf16 it may be residual itself, otherwise it lies
  *             apart from everything that is read.
- * Sums and the epilogue are fp32; y is rounded once.  Uses the (device,
- * stream) workspace where the product is split along in_features
- * (pda_linear_workspace_reserve before graph capture).
+ * Sums and the epilogue are fp32; y is rounded once.  The same call gives the
+ * same bits; the order of the sums depends on the batch, and so may a row's
+ * last bits.  Uses the (device, stream) workspace where the product is split
+ * along in_features (pda_linear_workspace_reserve before graph capture).
  *
  * Activations: none, silu(x) = x / (1 + exp(-x)), gelu(x) = x (1 + erf(x /
  * sqrt 2)) / 2, its tanh form, and max(x, 0).
@@ -842,15 +843,17 @@ int pda_moe_route(const float* logits, const float* select_bias, int32_t* expert
  *                   it lies apart from everything that is read.
  * Sums are fp32; act(G x) * (U x), for up to 8 tokens and 64 pairs with the
  * weight w_tj, is rounded to bf16 between the two products (the matrix cores'
- * operand) and out once.  Only the experts that are asked for are
- * read.  What is not finite in a token reaches that token alone, in an
- * expert's weights the tokens that chose it.  Uses the
- * (device, stream) workspace (pda_moe_workspace_reserve before graph capture):
- * tokens * top_k * 2 inter bytes for what lies between the two products, and 4
- * hidden a pair for each part of the down products' sums, none for up to 8 tokens
- * and 64 pairs.  A call that needs more than there is asks for what covers every
- * smaller call too: 32 hidden a pair, up to 128 MB, but never less than 4 hidden a
- * pair (pda_moe_plan has both figures).
+ * operand) and out once.  The same call gives the same bits; a token's last
+ * bits may depend on the other tokens of the batch and on their number, which
+ * decide the order of the sums.  Only the experts that are asked for are read.
+ * What is not finite in a token reaches that token alone, in an expert's weights
+ * the tokens that chose it.
+ * Uses the (device, stream) workspace (pda_moe_workspace_reserve before graph
+ * capture): 2 inter bytes a pair (of tokens * top_k) for what lies between the two
+ * products, and 4 hidden for each part of the down products' sums, none for up to
+ * 8 tokens and 64 pairs.  It asks for what covers every smaller call too: 32
+ * hidden a pair, up to 128 MB, but not below 4 hidden a pair (pda_moe_plan has
+ * both figures).
  */
 typedef struct {
   int32_t tokens;        /* 0 .. 256                                               */

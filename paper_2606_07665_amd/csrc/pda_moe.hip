@@ -451,7 +451,9 @@ __global__ __launch_bounds__(kMoeWaves * 64, kWavesPerSimd) void experts_kernel(
 // themselves by their (expert, 64 k) steps, a run of them each.  A token that
 // has not chosen an expert reads zeros in its steps (outside the descriptor, no
 // traffic), and takes nothing from their sums: zeros times a weight that is not
-// finite are none.
+// finite are none.  The sums' order follows from the slots of the whole batch, so
+// that a token's last bits may depend on the others' choices; the same ids give
+// the same bits.
 //
 // A matrix instruction multiplies both k tiles of a step at once: rows 0-7 of
 // its operand and columns 0-7 of the other hold the first, rows and columns
