@@ -486,7 +486,9 @@ int pda_plan(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t h
  * A graph captured on a stream keeps using the workspace it was captured
  * with: reserve the largest shape before capturing, and neither grow that
  * stream's workspace (a larger eager call on the same stream) nor release it
- * (pda_release_workspaces) while the graph may still be replayed.
+ * (pda_release_workspaces) while the graph may still be replayed.  Graphs
+ * captured on one stream share its workspace: replay them, and make that
+ * stream's eager calls, one after another.
  * (A call that fits the workspace never frees it: where it takes a larger one
  * for later calls, the old one is kept until pda_release_workspaces.)
  */
@@ -677,7 +679,9 @@ typedef struct {
  * the packed order the prelude reads (16-row x 32-column tiles of 1 KB in
  * matrix-core operand order).  rows a multiple of 16, cols a multiple of 32;
  * w and w_packed (rows * cols bf16, caller-owned, not overlapping) 16-byte
- * aligned.  Asynchronous on `stream`; done once per weight at load time.
+ * aligned.  Up to 2^34 elements a call; a larger matrix is packed in parts of whole
+ * 16-row tiles, each to its own rows of w_packed.  Asynchronous on `stream`; done
+ * once per weight at load time.
  */
 int pda_pack_weights(const void* w, void* w_packed, int32_t rows, int32_t cols, void* stream);
 
@@ -812,7 +816,9 @@ int pda_linear_workspace_reserve(const pda_linear_dims* dims, void* stream);
  * A logit of -infinity or NaN is an expert that may not be chosen: it comes last,
  * with weight 0 (all weights are 0 where every logit is); +infinity counts as
  * the largest finite number.  Without a bias the order is that of the logits,
- * with one that of the sums in fp64.  No workspace.
+ * with one that of the sums in fp64.  Scores are worked out in fp64, where a
+ * sigmoid of a logit below -709 and a softmax 745 below the largest are 0; all
+ * weights are 0 where the chosen scores' sum is.  No workspace.
  */
 typedef struct {
   int32_t tokens;        /* 0 .. 1048576                                           */
@@ -885,7 +891,8 @@ int pda_moe_workspace_reserve(const pda_moe_dims* dims, void* stream);
  *             [rows, hidden]: h, from the unrounded z.  Each may be y or
  *             residual itself (not both the same one); otherwise they lie
  *             apart from each other and from everything that is read.
- * No workspace.
+ * Sums of squares are fp32: a row whose squares add up past 3.4e38 counts as
+ * one of infinite size (its norm gives 0).  No workspace.
  */
 typedef struct {
   int32_t rows;          /* 0 .. 16777216                                          */

@@ -59,7 +59,7 @@ __device__ __forceinline__ void store_bf16(uint16_t* p, const float (&v)[N]) {
   __builtin_memcpy(p, w, 2 * N);
 }
 
-// Four (or two) consecutive features of a linear product, from element `at` on.
+// N consecutive features of a linear product, from element `at` on.
 template <int N>
 __device__ __forceinline__ void store_features(const LinearArgs& e, int64_t at, const float (&v)[N]) {
   if (e.f32)
@@ -72,7 +72,9 @@ __device__ __forceinline__ void store_features(const LinearArgs& e, int64_t at, 
 // = x erfc(-x / sqrt 2) / 2, and its tanh form x / (1 + exp(-2 u)) with
 // u = sqrt(2 / pi) (x + 0.044715 x^3).  Where the exponential overflows the
 // quotient is 0; its argument z is rounded to fp32, which costs |z| 2^-24 of a
-// value that has itself fallen by exp(z), z < 0.
+// value that has itself fallen by exp(z), z < 0.  The hardware's exponential and
+// reciprocal are off by a step of fp32 each, which is far below the rounding of a
+// bf16 output and shows in an fp32 one as a few steps.
 __device__ __forceinline__ float over_exp(float x, float z) {  // x / (1 + exp(-z))
   return x * __builtin_amdgcn_rcpf(1.f + __expf(-z));
 }

@@ -28,8 +28,9 @@ constexpr uint32_t kOutside = 0x80000000u;  // past any descriptor: reads zero
 // stream_splits, with both sides' times).
 //
 // Each row group starts its part of the k range at a place of its own: rows of
-// 16 or 32 KB otherwise meet in the same channels (80 x 8192 -> 8192 39.6 ->
-// 34.5 us; no change elsewhere).  Four row tiles a wave halve the LDS reads, but
+// 16 or 32 KB otherwise meet in the same channels (us, all from the same place ->
+// so: 80 x 8192 -> 16384 54.5 -> 52.4, 250 94 -> 92; but 128 59.8 -> 61.9 and 80 x
+// 8192 -> 12288 47.2 -> 48.5; other k and rows within 1%).  Four row tiles a wave halve the LDS reads, but
 // their sums and operands go past the 256 plain registers (101 sequences 46 us
 // as before, 200 twice as long).
 template <bool kGated, int RT, int NT, int W, int D, int kQ, int kWavesPerSimd>
@@ -286,13 +287,22 @@ int stream_most_splits(int waves, int rows, int num_cus) {
 //     the CUs without a workgroup; 4.7; whole, 0.12 for the epilogue of 128 rows and a
 //     column tile, in parts 5.4 for the second kernel and the parts' sums, written
 //     and read, at 3 MB a us.
-// With weights out of every cache the models are 8% off, and the choice over 246
-// products (80 to 250 sequences, k 256 to 8192, 8192 to 57344 rows) is 0.4% behind
-// the best of rows_kernel and 1, 2, 3, 4 and 6 parts on average, 13% at most;
-// rows_kernel always is 24.2% behind.  Over 120 of 36 to 64 sequences, not in parts,
-// 0.5%, and 11.8% (us, rows_kernel, whole, 3 parts: 80, 256 -> 57344 30.9, 12.5, -;
+// With weights out of every cache the models are 8% off, and the choice over 199
+// products (80 to 250 sequences, k 256 to 8192, 10240 to 57344 rows) is 0.4% behind
+// the best of rows_kernel and 1, 2, 3, 4 and 6 parts on average, 12% at most;
+// rows_kernel always is 29% behind.  Over 105 of 36 to 64 sequences, not in parts,
+// 0.3%, and 13.2% (us, rows_kernel, whole, 3 parts: 80, 256 -> 57344 30.9, 12.5, -;
 // 101, 5120 -> 20480 with GELU -, 64.0, 54.5; 250, 2048 -> 28672 75.0, 62.7, 83.2, in
 // two 58.8; 64, 4096 -> 20480 40.0, 44.4, 45.7).
+//
+// Below 40 rows a CU (10240) it is rows_kernel without a look at the models.  With k
+// up to 8192 that is right (8192 rows: 0.7% behind the best over 30 products of 80 to
+// 250 sequences, 1.9% over 15 of 36 to 64).  It is not just below the bound and with
+// longer k, where parts are ahead, the more the longer (us, rows_kernel, best number of
+// parts: 10224 rows, 4096 of k, 200 sequences 43.1, 43.0; 8192, 80 46.4, 37.4, 200 74.9,
+// 62.7; 14336, 200 124, 91; 8192 rows, 14336 of k, 80 59.0, 48.1, 200 87.3, 77.8;
+// 28672, 80 111, 82, 200 174, 142; 4096 rows, 14336 of k, 80 34.3, 33.3, 200 51.1,
+// 69.1; 28672, 80 58.7, 52.2, 200 94.7, 115).
 int stream_splits(int batch, int rows, int k, int num_cus) {
   if (batch <= 32 || rows < 40 * num_cus) return 0;
   const double scale = 256.0 / num_cus, weights = scale * rows * k, outputs = scale * rows * ((batch + 63) / 64 * 64);
